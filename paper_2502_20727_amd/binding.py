@@ -1,4 +1,4 @@
-"""ctypes binding of the SPD C ABI (include/spd.h, include/spd_testing.h): same names, argument marshalling only.
+"""ctypes binding of the SPD C ABI (include/spd.h, include/spd_q8.h, include/spd_testing.h): same names, argument marshalling only.
 
 Every step of the decoder-block path runs inside the HIP library; this module turns NumPy
 arrays / torch tensors / Python ints into the pointers and sizes the C calls take and turns
@@ -15,10 +15,11 @@ import numpy as np
 from . import build
 from .workloads import Workload
 
-SPD_F32, SPD_BF16 = 0, 1
+SPD_F32, SPD_BF16, SPD_F16, SPD_E4M3 = 0, 1, 2, 3
 SPD_OK, SPD_EINVAL, SPD_EUNSUPPORTED, SPD_EHIP, SPD_ETOOBIG = 0, -1, -2, -3, -4
 SPD_STATIC_WORKSPACE_BYTES = 64 << 20
 SPD_ALL_RANKS = -1
+SPD_Q8_MAX_K = 131071
 SPD_MAX_BATCH = 64
 
 
@@ -56,6 +57,19 @@ class spd_layer_weights(C.Structure):
 
 class spd_taps(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q", "attn", "y", "u")]
+
+
+class spd_pages_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "dtype",
+                                         "cache_dtype", "max_ctx")] + [("rope_base", C.c_float)]
+
+
+class spd_pages_sizes(C.Structure):
+    _fields_ = [("pool_bytes", C.c_size_t), ("rope_bytes", C.c_size_t)]
+
+
+class spd_pages_plan_info(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("tokens", C.c_int32), ("held", C.c_int64), ("workspace_bytes", C.c_size_t)]
 
 
 _lib = None
@@ -107,6 +121,29 @@ _PROTOS = {
     "spd_prefill_attention_workgroups": (C.c_int, [C.c_int32]),
     "spd_decode_qkv_slices": (C.c_int, [C.c_void_p, C.c_int32]),
     "spd_gemm_tile_of": (C.c_int, [C.c_int32] * 7 + [C.POINTER(C.c_int32), C.POINTER(C.c_int32)]),
+    "spd_pages_create": (C.c_int, [C.POINTER(spd_pages_config), C.POINTER(C.c_void_p)]),
+    "spd_pages_destroy": (None, [C.c_void_p]),
+    "spd_pages_get_sizes": (C.c_int, [C.c_void_p, C.POINTER(spd_pages_sizes)]),
+    "spd_pages_rope_table": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "spd_pages_plan": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                                 C.c_void_p, C.c_size_t, C.POINTER(C.c_size_t)]),
+    "spd_pages_plan_get_info": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(spd_pages_plan_info)]),
+    "spd_pages_write": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_int64, C.c_void_p]),
+    "spd_pages_read": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "spd_pages_attention": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                                      C.c_void_p, C.c_void_p]),
+    "spd_q8_norm": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_float,
+                              C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "spd_q8_rows": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "spd_q8_swiglu": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "spd_q8_weight_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
+    "spd_q8_pack": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]),
+    "spd_q8_pack_codes": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "spd_q8_unpack": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "spd_q8_matmul_workspace": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "spd_q8_matmul": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
 }
 EXPORTS = tuple(_PROTOS)
 STAGES = {"prep": 0, "qkv": 1, "attn": 2, "o": 3, "gateup": 4, "down": 5}
@@ -429,6 +466,211 @@ def spd_gemm_tile_of(TN: int, TM: int, rn: int, rm: int, tile0: int, n_tiles: in
     return tn.value, tm.value
 
 
+# --------------------------------------------------------------------------- 8-bit serving operators (spd_q8.h)
+
+def spd_pages_create(cfg: spd_pages_config) -> int:
+    out = C.c_void_p()
+    _check(lib().spd_pages_create(C.byref(cfg), C.byref(out)), "spd_pages_create")
+    return out.value
+
+
+def spd_pages_destroy(pages: int) -> None:
+    lib().spd_pages_destroy(pages)
+
+
+def spd_pages_get_sizes(pages: int) -> spd_pages_sizes:
+    s = spd_pages_sizes()
+    _check(lib().spd_pages_get_sizes(pages, C.byref(s)), "spd_pages_get_sizes")
+    return s
+
+
+def spd_pages_rope_table(pages: int) -> np.ndarray:
+    """The rotary table, fp32, flat: [max_ctx][head_dim / 2][cos, sin]."""
+    out = np.empty(spd_pages_get_sizes(pages).rope_bytes // 4, dtype=np.float32)
+    _check(lib().spd_pages_rope_table(pages, out.ctypes.data), "spd_pages_rope_table")
+    return out
+
+
+def spd_pages_plan(pages: int, positions: Sequence[int], q_lens: Sequence[int], page_table, window: int = 0,
+                   sinks: int = 0) -> np.ndarray:
+    """The plan of a step (bytes on the host).  page_table: int32 [batch, entries], or a list of lists of pages."""
+    pos, lens = (np.ascontiguousarray(x, dtype=np.int32) for x in (positions, q_lens))
+    if pos.shape != lens.shape or pos.ndim != 1:
+        raise ValueError("positions and q_lens are lists of one length")
+    if isinstance(page_table, np.ndarray):
+        table = np.ascontiguousarray(page_table, dtype=np.int32)
+    else:
+        table = np.zeros((len(pos), max([len(r) for r in page_table], default=0)), dtype=np.int32)
+        for b, r in enumerate(page_table):
+            table[b, :len(r)] = r
+    if table.ndim != 2 or table.shape[0] != len(pos):
+        raise ValueError("page_table has a row for each sequence")
+    if table.size == 0:                       # (an address that is not NULL)
+        table = np.zeros((len(pos), 1), dtype=np.int32)
+    need = C.c_size_t(0)
+
+    def call(out, n):
+        _check(lib().spd_pages_plan(pages, len(pos), pos.ctypes.data, lens.ctypes.data, table.ctypes.data, table.shape[1], int(window),
+                                    int(sinks), out, n, C.byref(need)), "spd_pages_plan")
+    call(None, 0)
+    plan = np.empty(need.value, dtype=np.uint8)
+    call(plan.ctypes.data, plan.size)
+    return plan
+
+
+def spd_pages_plan_get_info(pages: int, plan: np.ndarray) -> spd_pages_plan_info:
+    i = spd_pages_plan_info()
+    _check(lib().spd_pages_plan_get_info(pages, plan.ctypes.data, C.byref(i)), "spd_pages_plan_get_info")
+    return i
+
+
+def _type(t) -> int:
+    """SPD_* code of a torch tensor's element type."""
+    import torch
+    codes = {torch.float32: SPD_F32, torch.bfloat16: SPD_BF16, torch.float16: SPD_F16}
+    if t.dtype not in codes:
+        raise TypeError(f"float32, bfloat16 or float16 elements wanted, not {t.dtype}")
+    return codes[t.dtype]
+
+
+def _rows(t, rows: int, cols: int, what: str):
+    """(address, row stride) of a device matrix whose rows are contiguous; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a [{rows}, {cols}] matrix with contiguous rows wanted, not {tuple(t.shape)} with strides {t.stride()}")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+
+
+def _like(t, other, what: str):
+    if t is not None and t.dtype != other.dtype:
+        raise TypeError(f"{what}: {other.dtype} wanted, not {t.dtype}")
+
+
+def spd_pages_write(pages: int, plan: "PagePlan", qkv, rope, pool, q_out=None, stream=None) -> None:
+    """qkv [tokens, (q_heads + 2 kv_heads) head_dim]; q_out [tokens, q_heads head_dim] in the pool's 16-bit type, or None."""
+    p, ld = _rows(qkv, plan.info.tokens, qkv.shape[-1], "qkv")
+    c = plan.pages.cfg
+    if qkv.shape[-1] < (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim:
+        raise ValueError("qkv: rows too short")
+    qo, ld_q = _rows(q_out, plan.info.tokens, c.n_q_heads * c.head_dim, "q_out")
+    if q_out is not None and _type(q_out) != c.dtype:
+        raise TypeError("q_out: the pool's 16-bit type wanted")
+    _check(lib().spd_pages_write(pages, plan.host.ctypes.data, plan.device.data_ptr(), _type(qkv), p, ld, _ptr(rope), _ptr(pool), qo, ld_q,
+                                 _stream_ptr(stream)), "spd_pages_write")
+
+
+def spd_pages_read(pages: int, plan: "PagePlan", pool, k_out, v_out, stream=None) -> None:
+    """k_out, v_out [held, kv_heads, head_dim]: every position of every sequence, one after the other."""
+    c = plan.pages.cfg
+    want = (plan.info.held, c.n_kv_heads, c.head_dim)
+    if tuple(k_out.shape) != want or tuple(v_out.shape) != want:
+        raise ValueError(f"k_out, v_out: {want} wanted")
+    _like(v_out, k_out, "v_out")
+    _check(lib().spd_pages_read(pages, plan.host.ctypes.data, plan.device.data_ptr(), _ptr(pool), _type(k_out), _ptr(k_out), _ptr(v_out),
+                                _stream_ptr(stream)), "spd_pages_read")
+
+
+def spd_pages_attention(pages: int, plan: "PagePlan", q, pool, out, workspace=None, stream=None) -> None:
+    """q, out [tokens, q_heads head_dim] in the pool's 16-bit type, rows may be strided."""
+    c = plan.pages.cfg
+    qp, ld_q = _rows(q, plan.info.tokens, c.n_q_heads * c.head_dim, "q")
+    op, ld_o = _rows(out, plan.info.tokens, c.n_q_heads * c.head_dim, "out")
+    if _type(q) != c.dtype or _type(out) != c.dtype:
+        raise TypeError("q, out: the pool's 16-bit type wanted")
+    if workspace is not None and workspace.numel() * workspace.element_size() < plan.info.workspace_bytes:
+        raise ValueError("workspace: too small for the plan")
+    _check(lib().spd_pages_attention(pages, plan.host.ctypes.data, plan.device.data_ptr(), qp, ld_q, _ptr(pool), op, ld_o, _ptr(workspace),
+                                     _stream_ptr(stream)), "spd_pages_attention")
+
+
+def _codes(codes, scales, rows: int, n: int):
+    import torch
+    if codes.dtype != torch.int8 or scales.dtype != torch.float32 or scales.numel() != rows or not scales.is_contiguous():
+        raise TypeError("codes: int8, scales: contiguous float32, one a row")
+    return _rows(codes, rows, n, "codes")
+
+
+def spd_q8_norm(x, add, gain, eps: float, sum_out, codes, scales, stream=None) -> None:
+    """codes, scales <- RMSNorm(x + add) * gain in 8 bits; sum_out <- x + add.  add and sum_out may be None."""
+    import torch
+    rows, n = x.shape
+    px, lx = _rows(x, rows, n, "x")
+    pa, la = _rows(add, rows, n, "add")
+    ps, ls = _rows(sum_out, rows, n, "sum_out")
+    pc, lc = _codes(codes, scales, rows, n)
+    _like(add, x, "add")
+    _like(sum_out, x, "sum_out")
+    if gain.dtype != torch.float32 or gain.numel() != n:
+        raise TypeError("gain: float32, one a column")
+    _check(lib().spd_q8_norm(_type(x), rows, n, px, lx, pa, la, _ptr(gain), float(eps), ps, ls, pc, lc, _ptr(scales), _stream_ptr(stream)),
+           "spd_q8_norm")
+
+
+def spd_q8_rows(x, codes, scales, stream=None) -> None:
+    rows, n = x.shape
+    px, lx = _rows(x, rows, n, "x")
+    pc, lc = _codes(codes, scales, rows, n)
+    _check(lib().spd_q8_rows(_type(x), rows, n, px, lx, pc, lc, _ptr(scales), _stream_ptr(stream)), "spd_q8_rows")
+
+
+def spd_q8_swiglu(x, codes, scales, stream=None) -> None:
+    """x [rows, 2 n]: gates, then ups."""
+    rows, n = x.shape[0], x.shape[1] // 2
+    px, lx = _rows(x, rows, 2 * n, "x")
+    pc, lc = _codes(codes, scales, rows, n)
+    _check(lib().spd_q8_swiglu(_type(x), rows, n, px, lx, pc, lc, _ptr(scales), _stream_ptr(stream)), "spd_q8_swiglu")
+
+
+def spd_q8_weight_bytes(K: int, N: int) -> int:
+    return lib().spd_q8_weight_bytes(K, N)
+
+
+def spd_q8_pack(w: np.ndarray, out: Optional[np.ndarray] = None) -> np.ndarray:
+    """Quantises and packs fp32 weights [K, N] (y = x W)."""
+    assert w.dtype == np.float32 and w.ndim == 2 and w.flags.c_contiguous
+    K, N = w.shape
+    if out is None:
+        out = np.empty(spd_q8_weight_bytes(K, N), dtype=np.uint8)
+    _check(lib().spd_q8_pack(K, N, w.ctypes.data, N, out.ctypes.data), "spd_q8_pack")
+    return out
+
+
+def spd_q8_pack_codes(w: np.ndarray, w_scale: np.ndarray, out: Optional[np.ndarray] = None) -> np.ndarray:
+    assert w.dtype == np.int8 and w.ndim == 2 and w.flags.c_contiguous and w_scale.dtype == np.float32 and w_scale.shape == w.shape[1:]
+    K, N = w.shape
+    if out is None:
+        out = np.empty(spd_q8_weight_bytes(K, N), dtype=np.uint8)
+    _check(lib().spd_q8_pack_codes(K, N, w.ctypes.data, N, np.ascontiguousarray(w_scale).ctypes.data, out.ctypes.data), "spd_q8_pack_codes")
+    return out
+
+
+def spd_q8_unpack(K: int, N: int, packed: np.ndarray):
+    """(codes int8 [K, N], scales fp32 [N]) of packed weights."""
+    w, s = np.empty((K, N), dtype=np.int8), np.empty(N, dtype=np.float32)
+    _check(lib().spd_q8_unpack(K, N, packed.ctypes.data, w.ctypes.data, N, s.ctypes.data), "spd_q8_unpack")
+    return w, s
+
+
+def spd_q8_matmul_workspace(rows: int, K: int, N: int) -> int:
+    return lib().spd_q8_matmul_workspace(rows, K, N)
+
+
+def spd_q8_matmul(codes, scales, packed, N: int, add, out, workspace=None, stream=None) -> None:
+    """out [rows, N] <- (codes [rows, K] times the packed K x N weights) * scales (+ add)."""
+    rows, K = codes.shape
+    pc, lc = _codes(codes, scales, rows, K)
+    pa, la = _rows(add, rows, N, "add")
+    po, lo = _rows(out, rows, N, "out")
+    _like(add, out, "add")
+    if packed.numel() * packed.element_size() < spd_q8_weight_bytes(K, N):
+        raise ValueError("packed: too small for a %d x %d matrix" % (K, N))
+    if workspace is not None and workspace.numel() * workspace.element_size() < spd_q8_matmul_workspace(rows, K, N):
+        raise ValueError("workspace: too small")
+    _check(lib().spd_q8_matmul(rows, K, N, pc, lc, _ptr(scales), _ptr(packed), _type(out), pa, la, po, lo, _ptr(workspace),
+                               _stream_ptr(stream)), "spd_q8_matmul")
+
+
 # --------------------------------------------------------------------------- device-memory plumbing
 
 class DeviceShard:
@@ -492,3 +734,43 @@ class DeviceShard:
 
     def rank_arg(self) -> int:
         return SPD_ALL_RANKS if len(self.ranks) > 1 else self.ranks[0]
+
+
+class DevicePages:
+    """A pool of pages on the device with its handle and rotary table.  Holds memory only."""
+
+    def __init__(self, cfg: spd_pages_config, device, pool=None, rope: bool = True):
+        import torch
+        self.cfg = cfg
+        self.ctx = None
+        self.ctx = spd_pages_create(cfg)
+        self.sizes = spd_pages_get_sizes(self.ctx)
+        self.device = device
+        if pool is not None and pool.numel() * pool.element_size() < self.sizes.pool_bytes:
+            raise ValueError("pool: too small for the configuration")
+        self.pool = pool if pool is not None else torch.zeros(self.sizes.pool_bytes, dtype=torch.uint8, device=device)
+        self.rope = torch.from_numpy(spd_pages_rope_table(self.ctx)).to(device) if rope else None
+
+    def close(self):
+        if self.ctx:
+            spd_pages_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class PagePlan:
+    """The plan of a step, on the host and on the device, and its scratch."""
+
+    def __init__(self, pages: DevicePages, positions: Sequence[int], q_lens: Sequence[int], page_table, window: int = 0, sinks: int = 0):
+        import torch
+        self.pages = pages
+        self.host = spd_pages_plan(pages.ctx, positions, q_lens, page_table, window, sinks)
+        self.info = spd_pages_plan_get_info(pages.ctx, self.host)
+        self.device = torch.from_numpy(self.host).to(pages.device)
+        n = self.info.workspace_bytes
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=pages.device) if n else None

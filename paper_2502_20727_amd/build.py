@@ -17,7 +17,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 HIP_LIB = os.path.join(PKG_DIR, "libspd_hip.so")
 INPUTS_LIB = os.path.join(PKG_DIR, "libspd_inputs.so")
 
-HIP_SOURCES = ["spd_host.cpp", "spd_kernels_f32.hip", "spd_kernels_bf16.hip", "spd_forward.hip"]
+HIP_SOURCES = ["spd_host.cpp", "spd_pages_host.cpp", "spd_q8_host.cpp", "spd_kernels_f32.hip", "spd_kernels_bf16.hip",
+               "spd_forward.hip", "spd_pages.hip", "spd_q8.hip"]
 
 
 def _run(cmd):

@@ -13,15 +13,6 @@ namespace {
 // what the last failing HIP call of this thread was (spd_last_hip_error())
 thread_local char g_hip_msg[256] = "";
 
-#define SPD_HIP(x)                                                                                              \
-    do {                                                                                                        \
-        const hipError_t e_ = (x);                                                                              \
-        if (e_ != hipSuccess) {                                                                                 \
-            std::snprintf(g_hip_msg, sizeof(g_hip_msg), "%s (%s) at %s:%d", hipGetErrorName(e_), #x, __FILE__, __LINE__); \
-            return SPD_EHIP;                                                                                    \
-        }                                                                                                       \
-    } while (0)
-
 // launch errors are read with hipGetLastError(), which also returns whatever an earlier, unrelated
 // call of this thread left behind: every entry point starts from a clean slate
 inline void clear_stale_hip_error() { (void)hipGetLastError(); }
@@ -249,6 +240,10 @@ int block_forward_impl(const spd_ctx *ctx, int32_t layer, int32_t spd_flag, int3
 }
 
 }  // namespace
+
+void spd_note_hip_error(hipError_t e, const char *call, const char *file, int line) {
+    std::snprintf(g_hip_msg, sizeof(g_hip_msg), "%s (%s) at %s:%d", hipGetErrorName(e), call, file, line);
+}
 
 extern "C" {
 

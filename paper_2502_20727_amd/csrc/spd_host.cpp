@@ -6,7 +6,6 @@
 #include <cmath>
 #include <cstring>
 #include <new>
-#include <thread>
 
 #include "spd_internal.h"
 
@@ -64,24 +63,6 @@ inline float from_f16(uint16_t b) {
     u |= sign;
     std::memcpy(&v, &u, 4);
     return v;
-}
-
-template <class F>
-void parallel_for(int n, F f) {
-    int nt = (int)std::thread::hardware_concurrency();
-    if (nt < 1) nt = 1;
-    if (nt > 16) nt = 16;
-    if (nt > n) nt = n;
-    if (nt <= 1) {
-        for (int i = 0; i < n; ++i) f(i);
-        return;
-    }
-    std::vector<std::thread> th;
-    for (int t = 0; t < nt; ++t)
-        th.emplace_back([=]() {
-            for (int i = t; i < n; i += nt) f(i);
-        });
-    for (auto &t : th) t.join();
 }
 
 void compute_dims(const spd_config &c, spd_dims &D) {
@@ -209,7 +190,7 @@ template <class Src>
 bool pack_frags(uint16_t *dst, int n_tiles, int k_tiles, int shift, Src src) {
     const float up = std::ldexp(1.0f, shift);
     std::vector<int> bad(n_tiles, 0);
-    parallel_for(n_tiles, [&](int nt) {
+    spd_parallel_for(n_tiles, [&](int nt) {
         uint16_t scratch;
         for (int kt = 0; kt < k_tiles; ++kt) {
             uint16_t *fr = dst + spd_frag_index(nt, kt, k_tiles);
@@ -228,7 +209,7 @@ bool pack_frags(uint16_t *dst, int n_tiles, int k_tiles, int shift, Src src) {
 
 template <class Dst>
 void unpack_frags(const uint16_t *srcp, int n_tiles, int k_tiles, float down, Dst dst) {
-    parallel_for(n_tiles, [&](int nt) {
+    spd_parallel_for(n_tiles, [&](int nt) {
         for (int kt = 0; kt < k_tiles; ++kt) {
             const uint16_t *fr = srcp + spd_frag_index(nt, kt, k_tiles);
             for (int c = 0; c < 32; ++c)
@@ -429,7 +410,7 @@ int spd_pack_shard_local(const spd_ctx *ctx, const spd_layer_weights *w, void *p
         const int c = D.gud_cols, KT = h / 32;
         const float up = std::ldexp(1.0f, k_gu);
         std::vector<int> bad(D.gud_groups, 0);
-        parallel_for(D.gud_groups, [&](int p) {
+        spd_parallel_for(D.gud_groups, [&](int p) {
             uint16_t scratch;
             for (int kt = 0; kt < KT; ++kt)
                 for (int t = 0; t < 2; ++t) {
@@ -565,7 +546,7 @@ int spd_kv_pack(const spd_ctx *ctx, const float *k, const float *v, int32_t batc
     const int d = D.d;
     const size_t per_head = (size_t)D.max_ctx * d;
     std::vector<int> bad(batch * D.kv, 0);
-    parallel_for(batch * D.kv, [&](int bh) {
+    spd_parallel_for(batch * D.kv, [&](int bh) {
         const float *ks = k + (size_t)bh * n_pos * d, *vs = v + (size_t)bh * n_pos * d;
         if (D.dtype == SPD_F32) {
             float *kd = (float *)cache_host + (size_t)bh * per_head;
@@ -593,7 +574,7 @@ int spd_kv_unpack(const spd_ctx *ctx, const void *cache_host, int32_t batch, int
     if (batch < 0 || batch > D.max_batch || n_pos < 0 || n_pos > D.max_ctx) return SPD_EINVAL;
     const int d = D.d;
     const size_t per_head = (size_t)D.max_ctx * d;
-    parallel_for(batch * D.kv, [&](int bh) {
+    spd_parallel_for(batch * D.kv, [&](int bh) {
         float *ks = k + (size_t)bh * n_pos * d, *vs = v + (size_t)bh * n_pos * d;
         if (D.dtype == SPD_F32) {
             std::memcpy(ks, (const float *)cache_host + (size_t)bh * per_head, (size_t)n_pos * d * 4);

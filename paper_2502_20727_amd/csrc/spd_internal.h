@@ -6,6 +6,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <thread>
 #include <vector>
 
 #include "spd.h"
@@ -196,7 +197,44 @@ struct spd_positions {
     int32_t pos[SPD_MAX_BATCH];
 };
 
+// f(0) .. f(n - 1) on a few threads of the host
+template <class F>
+void spd_parallel_for(int n, F f) {
+    int nt = (int)std::thread::hardware_concurrency();
+    if (nt < 1) nt = 1;
+    if (nt > 16) nt = 16;
+    if (nt > n) nt = n;
+    if (nt <= 1) {
+        for (int i = 0; i < n; ++i) f(i);
+        return;
+    }
+    std::vector<std::thread> th;
+    th.reserve(nt);
+    int started = 0;
+    try {
+        for (; started < nt; ++started)
+            th.emplace_back([=, t = started]() {
+                for (int i = t; i < n; i += nt) f(i);
+            });
+    } catch (...) {      // no more threads: their shares are done here
+    }
+    for (int t = started; t < nt; ++t)
+        for (int i = t; i < n; i += nt) f(i);
+    for (auto &t : th) t.join();
+}
+
 inline size_t spd_align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// Keeps what a failing HIP call of this thread was, for spd_last_hip_error().  The macro leaves an entry point with SPD_EHIP.
+void spd_note_hip_error(hipError_t e, const char *call, const char *file, int line);
+#define SPD_HIP(x)                                              \
+    do {                                                        \
+        const hipError_t e_ = (x);                              \
+        if (e_ != hipSuccess) {                                 \
+            spd_note_hip_error(e_, #x, __FILE__, __LINE__);     \
+            return SPD_EHIP;                                    \
+        }                                                       \
+    } while (0)
 
 // Stage selection and timing of one call (test and benchmark aid, declared in spd_testing.h): a call
 // launches the stages whose bit is set in `stages`; with a timer, every launch of the timer's stage is
