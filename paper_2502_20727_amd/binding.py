@@ -8,6 +8,7 @@ the stream.  If the HIP library cannot be loaded this module raises: there is no
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -72,7 +73,8 @@ class spd_pages_plan_info(C.Structure):
     _fields_ = [("batch", C.c_int32), ("tokens", C.c_int32), ("held", C.c_int64), ("workspace_bytes", C.c_size_t)]
 
 
-_lib = None
+_lib = _torch = None
+_TYPES: Dict[object, int] = {}       # SPD_* codes of torch's element types
 
 _PROTOS = {
     "spd_create": (C.c_int, [C.POINTER(spd_config), C.POINTER(C.c_void_p)]),
@@ -153,14 +155,16 @@ SPD_STAGE_EMPTY = len(STAGES)
 
 def lib():
     """The loaded HIP library.  Raises if it is missing and cannot be built."""
-    global _lib
+    global _lib, _torch
     if _lib is None:
         path = build.ensure_hip()
         # PyTorch ships its own HIP runtime.  The library must bind to the same one as the tensors it
         # is handed, so torch (when installed) is imported before the library is loaded: loaded the
         # other way round, the process holds two runtimes and this library's calls see no device.
         try:
-            import torch  # noqa: F401
+            import torch
+            _torch = torch
+            _TYPES.update({torch.float32: SPD_F32, torch.bfloat16: SPD_BF16, torch.float16: SPD_F16})
         except ImportError:
             pass
         l = C.CDLL(path)
@@ -335,10 +339,18 @@ def spd_kv_unpack(ctx: int, cache_host: np.ndarray, batch: int, n_pos: int, kv_h
 
 # --------------------------------------------------------------------------- device calls
 
+def _current_stream() -> int:
+    """torch's current stream on its current device, without the object around it (which takes longer than a small launch)."""
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None:
+        return torch.cuda.current_stream().cuda_stream
+    return raw(device())
+
+
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -526,20 +538,23 @@ def spd_pages_plan_get_info(pages: int, plan: np.ndarray) -> spd_pages_plan_info
 
 def _type(t) -> int:
     """SPD_* code of a torch tensor's element type."""
-    import torch
-    codes = {torch.float32: SPD_F32, torch.bfloat16: SPD_BF16, torch.float16: SPD_F16}
-    if t.dtype not in codes:
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        if _lib is None:
+            lib()                # fills the table
+            return _type(t)
         raise TypeError(f"float32, bfloat16 or float16 elements wanted, not {t.dtype}")
-    return codes[t.dtype]
+    return code
 
 
 def _rows(t, rows: int, cols: int, what: str):
     """(address, row stride) of a device matrix whose rows are contiguous; (None, 0) for None."""
     if t is None:
         return None, 0
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+    if t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
         raise ValueError(f"{what}: a [{rows}, {cols}] matrix with contiguous rows wanted, not {tuple(t.shape)} with strides {t.stride()}")
-    return t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+    ld = t.stride(0)
+    return t.data_ptr(), (ld if ld >= cols or rows > 1 else cols)
 
 
 def _like(t, other, what: str):
@@ -549,51 +564,51 @@ def _like(t, other, what: str):
 
 def spd_pages_write(pages: int, plan: "PagePlan", qkv, rope, pool, q_out=None, stream=None) -> None:
     """qkv [tokens, (q_heads + 2 kv_heads) head_dim]; q_out [tokens, q_heads head_dim] in the pool's 16-bit type, or None."""
-    p, ld = _rows(qkv, plan.info.tokens, qkv.shape[-1], "qkv")
-    c = plan.pages.cfg
-    if qkv.shape[-1] < (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim:
+    width = qkv.shape[-1]
+    p, ld = _rows(qkv, plan.tokens, width, "qkv")
+    if width < plan.qkv_cols:
         raise ValueError("qkv: rows too short")
-    qo, ld_q = _rows(q_out, plan.info.tokens, c.n_q_heads * c.head_dim, "q_out")
-    if q_out is not None and _type(q_out) != c.dtype:
+    qo, ld_q = _rows(q_out, plan.tokens, plan.q_cols, "q_out")
+    if qo is not None and _type(q_out) != plan.dtype:
         raise TypeError("q_out: the pool's 16-bit type wanted")
-    _check(lib().spd_pages_write(pages, plan.host.ctypes.data, plan.device.data_ptr(), _type(qkv), p, ld, _ptr(rope), _ptr(pool), qo, ld_q,
-                                 _stream_ptr(stream)), "spd_pages_write")
+    rc = lib().spd_pages_write(pages, plan.host_ptr, plan.device_ptr, _type(qkv), p, ld, _ptr(rope), _ptr(pool), qo, ld_q, _stream_ptr(stream))
+    if rc:
+        raise SpdError(rc, "spd_pages_write")
 
 
 def spd_pages_read(pages: int, plan: "PagePlan", pool, k_out, v_out, stream=None) -> None:
     """k_out, v_out [held, kv_heads, head_dim]: every position of every sequence, one after the other."""
     c = plan.pages.cfg
     want = (plan.info.held, c.n_kv_heads, c.head_dim)
-    if tuple(k_out.shape) != want or tuple(v_out.shape) != want:
+    if k_out.shape != want or v_out.shape != want:
         raise ValueError(f"k_out, v_out: {want} wanted")
     _like(v_out, k_out, "v_out")
-    _check(lib().spd_pages_read(pages, plan.host.ctypes.data, plan.device.data_ptr(), _ptr(pool), _type(k_out), _ptr(k_out), _ptr(v_out),
-                                _stream_ptr(stream)), "spd_pages_read")
+    rc = lib().spd_pages_read(pages, plan.host_ptr, plan.device_ptr, _ptr(pool), _type(k_out), _ptr(k_out), _ptr(v_out), _stream_ptr(stream))
+    if rc:
+        raise SpdError(rc, "spd_pages_read")
 
 
 def spd_pages_attention(pages: int, plan: "PagePlan", q, pool, out, workspace=None, stream=None) -> None:
     """q, out [tokens, q_heads head_dim] in the pool's 16-bit type, rows may be strided."""
-    c = plan.pages.cfg
-    qp, ld_q = _rows(q, plan.info.tokens, c.n_q_heads * c.head_dim, "q")
-    op, ld_o = _rows(out, plan.info.tokens, c.n_q_heads * c.head_dim, "out")
-    if _type(q) != c.dtype or _type(out) != c.dtype:
+    qp, ld_q = _rows(q, plan.tokens, plan.q_cols, "q")
+    op, ld_o = _rows(out, plan.tokens, plan.q_cols, "out")
+    if _type(q) != plan.dtype or _type(out) != plan.dtype:
         raise TypeError("q, out: the pool's 16-bit type wanted")
-    if workspace is not None and workspace.numel() * workspace.element_size() < plan.info.workspace_bytes:
+    if workspace is not None and workspace.nbytes < plan.workspace_bytes:
         raise ValueError("workspace: too small for the plan")
-    _check(lib().spd_pages_attention(pages, plan.host.ctypes.data, plan.device.data_ptr(), qp, ld_q, _ptr(pool), op, ld_o, _ptr(workspace),
-                                     _stream_ptr(stream)), "spd_pages_attention")
+    rc = lib().spd_pages_attention(pages, plan.host_ptr, plan.device_ptr, qp, ld_q, _ptr(pool), op, ld_o, _ptr(workspace), _stream_ptr(stream))
+    if rc:
+        raise SpdError(rc, "spd_pages_attention")
 
 
 def _codes(codes, scales, rows: int, n: int):
-    import torch
-    if codes.dtype != torch.int8 or scales.dtype != torch.float32 or scales.numel() != rows or not scales.is_contiguous():
+    if _type(scales) != SPD_F32 or codes.dtype != _torch.int8 or scales.numel() != rows or not scales.is_contiguous():
         raise TypeError("codes: int8, scales: contiguous float32, one a row")
     return _rows(codes, rows, n, "codes")
 
 
 def spd_q8_norm(x, add, gain, eps: float, sum_out, codes, scales, stream=None) -> None:
     """codes, scales <- RMSNorm(x + add) * gain in 8 bits; sum_out <- x + add.  add and sum_out may be None."""
-    import torch
     rows, n = x.shape
     px, lx = _rows(x, rows, n, "x")
     pa, la = _rows(add, rows, n, "add")
@@ -601,27 +616,34 @@ def spd_q8_norm(x, add, gain, eps: float, sum_out, codes, scales, stream=None) -
     pc, lc = _codes(codes, scales, rows, n)
     _like(add, x, "add")
     _like(sum_out, x, "sum_out")
-    if gain.dtype != torch.float32 or gain.numel() != n:
+    if _type(gain) != SPD_F32 or gain.numel() != n:
         raise TypeError("gain: float32, one a column")
-    _check(lib().spd_q8_norm(_type(x), rows, n, px, lx, pa, la, _ptr(gain), float(eps), ps, ls, pc, lc, _ptr(scales), _stream_ptr(stream)),
-           "spd_q8_norm")
+    rc = lib().spd_q8_norm(_type(x), rows, n, px, lx, pa, la, _ptr(gain), eps, ps, ls, pc, lc, scales.data_ptr(), _stream_ptr(stream))
+    if rc:
+        raise SpdError(rc, "spd_q8_norm")
 
 
 def spd_q8_rows(x, codes, scales, stream=None) -> None:
     rows, n = x.shape
     px, lx = _rows(x, rows, n, "x")
     pc, lc = _codes(codes, scales, rows, n)
-    _check(lib().spd_q8_rows(_type(x), rows, n, px, lx, pc, lc, _ptr(scales), _stream_ptr(stream)), "spd_q8_rows")
+    rc = lib().spd_q8_rows(_type(x), rows, n, px, lx, pc, lc, scales.data_ptr(), _stream_ptr(stream))
+    if rc:
+        raise SpdError(rc, "spd_q8_rows")
 
 
 def spd_q8_swiglu(x, codes, scales, stream=None) -> None:
     """x [rows, 2 n]: gates, then ups."""
-    rows, n = x.shape[0], x.shape[1] // 2
+    rows, n = x.shape
+    n //= 2
     px, lx = _rows(x, rows, 2 * n, "x")
     pc, lc = _codes(codes, scales, rows, n)
-    _check(lib().spd_q8_swiglu(_type(x), rows, n, px, lx, pc, lc, _ptr(scales), _stream_ptr(stream)), "spd_q8_swiglu")
+    rc = lib().spd_q8_swiglu(_type(x), rows, n, px, lx, pc, lc, scales.data_ptr(), _stream_ptr(stream))
+    if rc:
+        raise SpdError(rc, "spd_q8_swiglu")
 
 
+@functools.lru_cache(maxsize=None)
 def spd_q8_weight_bytes(K: int, N: int) -> int:
     return lib().spd_q8_weight_bytes(K, N)
 
@@ -652,23 +674,26 @@ def spd_q8_unpack(K: int, N: int, packed: np.ndarray):
     return w, s
 
 
+@functools.lru_cache(maxsize=4096)
 def spd_q8_matmul_workspace(rows: int, K: int, N: int) -> int:
     return lib().spd_q8_matmul_workspace(rows, K, N)
 
 
 def spd_q8_matmul(codes, scales, packed, N: int, add, out, workspace=None, stream=None) -> None:
     """out [rows, N] <- (codes [rows, K] times the packed K x N weights) * scales (+ add)."""
+    l = lib()
     rows, K = codes.shape
     pc, lc = _codes(codes, scales, rows, K)
     pa, la = _rows(add, rows, N, "add")
     po, lo = _rows(out, rows, N, "out")
     _like(add, out, "add")
-    if packed.numel() * packed.element_size() < spd_q8_weight_bytes(K, N):
+    if packed.nbytes < spd_q8_weight_bytes(K, N):
         raise ValueError("packed: too small for a %d x %d matrix" % (K, N))
-    if workspace is not None and workspace.numel() * workspace.element_size() < spd_q8_matmul_workspace(rows, K, N):
+    if (workspace.nbytes if workspace is not None else 0) < spd_q8_matmul_workspace(rows, K, N):
         raise ValueError("workspace: too small")
-    _check(lib().spd_q8_matmul(rows, K, N, pc, lc, _ptr(scales), _ptr(packed), _type(out), pa, la, po, lo, _ptr(workspace),
-                               _stream_ptr(stream)), "spd_q8_matmul")
+    rc = l.spd_q8_matmul(rows, K, N, pc, lc, scales.data_ptr(), _ptr(packed), _type(out), pa, la, po, lo, _ptr(workspace), _stream_ptr(stream))
+    if rc:
+        raise SpdError(rc, "spd_q8_matmul")
 
 
 # --------------------------------------------------------------------------- device-memory plumbing
@@ -772,5 +797,9 @@ class PagePlan:
         self.host = spd_pages_plan(pages.ctx, positions, q_lens, page_table, window, sinks)
         self.info = spd_pages_plan_get_info(pages.ctx, self.host)
         self.device = torch.from_numpy(self.host).to(pages.device)
-        n = self.info.workspace_bytes
+        c = pages.cfg
+        self.tokens, self.workspace_bytes, self.dtype = self.info.tokens, self.info.workspace_bytes, c.dtype
+        self.q_cols, self.qkv_cols = c.n_q_heads * c.head_dim, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
+        self.host_ptr, self.device_ptr = self.host.ctypes.data, self.device.data_ptr()
+        n = self.workspace_bytes
         self.workspace = torch.empty(n, dtype=torch.uint8, device=pages.device) if n else None

@@ -1,4 +1,5 @@
 // Rows to 8-bit integers, and the product of such rows with packed 8-bit weights, for gfx950.
+#include <mutex>
 #include <type_traits>
 
 #include "spd_q8_internal.h"
@@ -129,47 +130,359 @@ struct Q8Args {
     void *out;
     int64_t ld_codes, ld_add, ld_out;
     int rows, K, N, KT, NT;
+    int quads;               // rows of out and add hold whole, aligned groups of four columns
 };
 
-// (a place past the matrix: nothing)
 template <class T>
-__device__ __forceinline__ void q8_store(const Q8Args &A, int m, int n, i32x4 acc) {
+struct Quad {            // four elements of T
+    T v[4];
+};
+
+template <class T>
+struct Piece {           // 16 bytes of them
+    T v[16 / sizeof(T)];
+};
+
+// four columns of a row, n a multiple of 4; a place past the matrix: nothing.  sm, sn: scales of the row and of the columns
+template <class T>
+__device__ __forceinline__ void q8_store(const Q8Args &A, int m, int n, i32x4 acc, float sm, f32x4 sn) {
     if (m >= A.rows || n >= A.N) return;
-    const float sm = A.scales[m];
-    const float *wsc = (const float *)A.packed;
-    T *out = (T *)A.out + m * A.ld_out;
-    const T *add = A.add ? (const T *)A.add + m * A.ld_add : nullptr;
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)acc[i] * sm * sn[i];
+    T *out = (T *)A.out + m * A.ld_out + n;
+    const T *add = A.add ? (const T *)A.add + m * A.ld_add + n : nullptr;
+    if (A.quads) {       // whole and aligned
+        if (add) {
+            const Quad<T> q = *(const Quad<T> *)__builtin_assume_aligned(add, sizeof(Quad<T>));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += (float)q.v[i];
+        }
+        Quad<T> q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q.v[i] = (T)v[i];
+        *(Quad<T> *)__builtin_assume_aligned(out, sizeof(Quad<T>)) = q;
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (n + i < A.N) {
-            float v = (float)acc[i] * sm * wsc[n + i];
-            if (add) v += (float)add[n + i];
-            out[n + i] = (T)v;
-        }
+        if (n + i < A.N) out[i] = (T)(add ? v[i] + (float)add[i] : v[i]);
+}
+__device__ __forceinline__ float q8_row_scale(const Q8Args &A, int m) { return A.scales[m < A.rows ? m : A.rows - 1]; }
+// (the scales are padded to whole n-tiles)
+__device__ __forceinline__ f32x4 q8_col_scales(const Q8Args &A, int nt, int g) {
+    return *(const f32x4 *)((const float *)A.packed + (nt < A.NT ? nt : A.NT - 1) * 16 + 4 * g);
 }
 
-// one wave: 64 columns x 64 rows, operands straight from memory
-template <class T>
-__global__ void __launch_bounds__(256) k_q8_tile(Q8Args A) {
+// ------------------------------------------------------------------------------------------
+// Few rows: the weights are streamed once.  A workgroup takes NP n-tiles and all of K, its eight waves a share of the k-tiles each; both
+// operands go straight into registers, a batch of k-tiles ahead of the one in use, and the waves' integer sums meet in the LDS.  Bound by what
+// a compute unit draws through its load path: (NP + MT) KiB per k-tile.  K 8192, N 7168, 16 rows: 14.2 us a call (59 MB of
+// weights: 4.1 TB/s); loads and their use in turn: 15.1.
+// ------------------------------------------------------------------------------------------
+template <class T, int MT, int NP>
+__global__ void __launch_bounds__(512) k_q8_skinny(Q8Args A) {
+    constexpr int NB = MT >= 4 ? 2 : 4;                        // k-tiles asked for at a time
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nt0 = (blockIdx.x * 4 + wave) * 4, m0 = blockIdx.y * 64;
+    const int nt0 = blockIdx.x * NP, m0 = blockIdx.y * (MT * 16);
+    const int r = lane & 15, g = lane >> 4;
+    const int per = (A.KT + 7) / 8, kt0 = wave * per, kt1 = kt0 + per < A.KT ? kt0 + per : A.KT;
+    const char *w[NP];
+    const int8_t *x[MT];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int nt = nt0 + i < A.NT ? nt0 + i : A.NT - 1;
+        w[i] = A.packed + spd_q8_weights_at(A.N) + (size_t)nt * A.KT * 1024 + lane * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+        const int m = m0 + 16 * j + r;
+        x[j] = A.codes + (int64_t)(m < A.rows ? m : A.rows - 1) * A.ld_codes;
+    }
+    const int k_last = (A.K - 1) & ~15;                        // past K: anything, the weights are zero there
+    i32x4 acc[NP][MT];
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = (i32x4){0, 0, 0, 0};
+    struct Batch {
+        i32x4 a[NB][NP], b[NB][MT];
+    };
+    auto load = [&](Batch &f, int kt) __attribute__((always_inline)) {      // (k-tiles past the share: its last one, not used)
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            const int t = kt + u < kt1 ? kt + u : kt1 - 1;
+            int k = t * 64 + 16 * g;
+            k = k < k_last ? k : k_last;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) f.a[u][i] = __builtin_nontemporal_load((const i32x4 *)(w[i] + (size_t)t * 1024));
+#pragma unroll
+            for (int j = 0; j < MT; ++j) f.b[u][j] = *(const i32x4 *)(x[j] + k);
+        }
+    };
+    auto use = [&](const Batch &f, int kt) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < NB; ++u)
+            if (kt + u < kt1) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.a[u][i], f.b[u][j], acc[i][j], 0, 0, 0);
+            }
+    };
+    if (kt0 < kt1) {
+        Batch f0, f1;
+        load(f0, kt0);
+        for (int kt = kt0; kt < kt1; kt += 2 * NB) {      // the next batch is on its way while one is used
+            if (kt + NB < kt1) load(f1, kt + NB);
+            use(f0, kt);
+            if (kt + NB < kt1) {
+                if (kt + 2 * NB < kt1) load(f0, kt + 2 * NB);
+                use(f1, kt + NB);
+            }
+        }
+    }
+    __shared__ i32x4 part[8][NP * MT][64];
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) part[wave][i * MT + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int t = wave; t < NP * MT; t += 8) {
+        i32x4 v = part[0][t][lane];
+#pragma unroll
+        for (int u = 1; u < 8; ++u) v += part[u][t][lane];
+        const int i = t / MT, j = t % MT;
+        q8_store<T>(A, m0 + 16 * j + r, (nt0 + i) * 16 + 4 * g, v, q8_row_scale(A, m0 + 16 * j + r), q8_col_scales(A, nt0 + i, g));
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Many rows: tiles of WN TI n-tiles x WM TJ m-tiles through the LDS, NST stages of two k-tiles, copied there directly.  Copies go through
+// buffer descriptors of the tile's panels; rows and inputs past the matrix repeat its last ones.  A step is two sub-steps, one per k-tile:
+// while the MFMAs of one run, the fragments of the next are read between them, and in the second one the copies of the stage
+// NST steps ahead go out; the one barrier of a step lies between them.  The results leave through the LDS in whole cache lines: stored as
+// they lie in the registers (32 bytes a row and store) they took 2.2 times as long as K = 1024 did beside them (8192 rows, N 8192: 146 us a
+// call, now 79).  8192 rows, K 8192, N 7168: 428 us, 2.25 P operations a second; between the ends of a round the matrix cores do 2.6.
+// (A workgroup that goes on with its next tile's copies before it stores needs its descriptors in vector registers: 559.)
+// ------------------------------------------------------------------------------------------
+struct Q8Big {       // 256 x 256
+    static constexpr int WN = 4, WM = 2, TI = 4, TJ = 8, NST = 2;
+};
+struct Q8Half {      // 256 x 128
+    static constexpr int WN = 4, WM = 2, TI = 4, TJ = 4, NST = 3;
+};
+struct Q8Square {    // 128 x 128
+    static constexpr int WN = 4, WM = 2, TI = 2, TJ = 4, NST = 4;
+};
+struct Q8Small {     // 128 x 64, two workgroups per compute unit
+    static constexpr int WN = 4, WM = 2, TI = 2, TJ = 2, NST = 3;
+};
+constexpr int waitcnt_imm(int vm, int lgkm) { return (vm & 15) | ((vm >> 4) << 14) | (7 << 4) | (lgkm << 8); }
+
+template <class T, class G>
+__global__ void __launch_bounds__(G::WN *G::WM * 64, 1) k_q8_gemm(Q8Args A, spd_tile_order ord, int tile0, int n_tiles, int msub) {
+    constexpr int TI = G::TI, TJ = G::TJ, NST = G::NST, NW = G::WN * G::WM, BN = G::WN * TI, BM = G::WM * TJ;
+    constexpr int W_BYTES = BN * 2048, STAGE = W_BYTES + BM * 2048;
+    constexpr int CW = BN * 2 / NW, CX = BM * 2 / NW, NCP = CW + CX;
+    static_assert(BN * 2 % NW == 0 && BM * 2 % NW == 0 && (NST - 1) * NCP < 64, "tile shape");
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wn = wave % G::WN, wm = wave / G::WN;
+    const int KT = A.KT, l16 = lane * 16, r = lane & 15, g = lane >> 4;
+    const unsigned pitch = (unsigned)KT * 1024;
+    const int k16 = (A.K + 15) & ~15;
+    // the last k-tile's lanes past K repeat its last 16 inputs
+    const int tail = (KT - 1) * 64 + 16 * g > k16 - 16 ? k16 - 16 - (KT - 1) * 64 - 16 * g : 0;
+    int nt0, m0;
+    {
+        // n_tiles tiles of the order from tile0 on, each cut into msub along the rows (2: the last round of a launch of tiles twice as high)
+        const int idx = msub == 1 ? spd_tile_deal((int)blockIdx.x, n_tiles) : (int)blockIdx.x / msub;
+        if (idx < 0) return;                 // spare workgroup of a ragged share (whole workgroup, before any barrier)
+        int tn, tm;
+        spd_tile_at(ord, tile0 + idx, tn, tm);
+        nt0 = tn * BN;
+        m0 = (tm * msub + (msub == 1 ? 0 : (int)blockIdx.x % msub)) * BM * 16;
+        if (m0 >= A.rows) return;            // (whole workgroup)
+    }
+    const int n_rows = A.NT - nt0 < BN ? A.NT - nt0 : BN, m_rows = A.rows - m0 < BM * 16 ? A.rows - m0 : BM * 16;
+    const __amdgpu_buffer_rsrc_t
+        wbuf = __builtin_amdgcn_make_buffer_rsrc((void *)(A.packed + spd_q8_weights_at(A.N) + (size_t)nt0 * pitch), 0, (int)(n_rows * pitch), 0x00020000),
+        xbuf = __builtin_amdgcn_make_buffer_rsrc((void *)(A.codes + m0 * A.ld_codes), 0, (int)((m_rows - 1) * (unsigned)A.ld_codes + k16), 0x00020000);
+    unsigned wsrc[CW], xoff[CX];             // (wsrc: wave-uniform)
+#pragma unroll
+    for (int n = 0; n < CW; ++n) {
+        const int t = (wave * CW + n) / 2;
+        wsrc[n] = (unsigned)(t < n_rows ? t : n_rows - 1) * pitch;
+    }
+#pragma unroll
+    for (int n = 0; n < CX; ++n) {
+        const int m = ((wave * CX + n) / 2) * 16 + r;
+        xoff[n] = (unsigned)(m < m_rows ? m : m_rows - 1) * (unsigned)A.ld_codes + 16 * g;
+    }
+    i32x4 acc[TI][TJ];
+    auto copy1 = [&](int st, int slot, int n) __attribute__((always_inline)) {
+        if (n < CW) {
+            int kt = 2 * st + ((wave * CW + n) & 1);
+            kt = kt < KT ? kt : KT - 1;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wbuf, (__attribute__((address_space(3))) void *)(lds + slot * STAGE + (wave * CW + n) * 1024), 16,
+                                                     l16, (int)(wsrc[n] + kt * 1024), 0, 0);
+        } else {
+            const int c = n - CW;
+            int kt = 2 * st + ((wave * CX + c) & 1);
+            kt = kt < KT ? kt : KT - 1;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xbuf, (__attribute__((address_space(3))) void *)(lds + slot * STAGE + W_BYTES + (wave * CX + c) * 1024),
+                                                     16, (int)(xoff[c] + (kt == KT - 1 ? tail : 0)), kt * 64, 0, 0);
+        }
+    };
+    const char *a_base = lds + wn * TI * 2048 + l16, *b_base = lds + W_BYTES + wm * TJ * 2048 + l16;
+    auto read1 = [&](int slot, int p, int f, i32x4(&a)[TI], i32x4(&b)[TJ]) __attribute__((always_inline)) {
+        if (f < TJ) b[f] = *(const i32x4 *)(b_base + slot * STAGE + (2 * f + p) * 1024);
+        else a[f - TJ] = *(const i32x4 *)(a_base + slot * STAGE + ((f - TJ) * 2 + p) * 1024);
+    };
+    const int n_stages = (KT + 1) / 2, n_steps = KT / 2;
+    auto first_copies = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int st = 0; st < NST; ++st)
+            if (st < n_stages) {
+#pragma unroll
+                for (int n = 0; n < NCP; ++n) copy1(st, st, n);
+            }
+    };
+    i32x4 a0[TI], a1[TI], b0[TJ], b1[TJ];
+    auto substep = [&](auto copy_, const i32x4(&a)[TI], const i32x4(&b)[TJ], i32x4(&an)[TI], i32x4(&bn)[TJ], int rslot, int rp, int cst,
+                       int cslot) __attribute__((always_inline)) {
+        constexpr int NR = TI + TJ, NM = TI * TJ;
+        constexpr bool COPY = decltype(copy_)::value;
+        int f = 0, cp = 0;
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                const int n = i * TJ + j;
+                acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[j], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                while (f < NR && n >= (2 * NR <= NM ? 2 * f : f * NM / NR)) read1(rslot, rp, f++, an, bn);
+                while (COPY && cp < NCP && n >= (NM >= NCP ? cp * (NM / NCP) : cp * NM / NCP)) copy1(cst, cslot, cp++);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+    first_copies();
+    __builtin_amdgcn_sched_barrier(0);
+    if (n_stages >= NST) __builtin_amdgcn_s_waitcnt(waitcnt_imm((NST - 1) * NCP, 0));
+    else __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) acc[i][j] = (i32x4){0, 0, 0, 0};
+#pragma unroll
+    for (int f = 0; f < TI + TJ; ++f) read1(0, 0, f, a0, b0);
+    int slot = 0;
+    auto step = [&](auto copy_, int s) __attribute__((always_inline)) {
+        constexpr bool COPY = decltype(copy_)::value;
+        const int next = slot + 1 == NST ? 0 : slot + 1;
+        substep(std::false_type(), a0, b0, a1, b1, slot, 1, 0, 0);
+        // the next stage's copies of this wave have landed, every read of the current stage is done
+        __builtin_amdgcn_s_waitcnt(waitcnt_imm(COPY ? (NST - 2) * NCP : 0, 0));
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        substep(copy_, a1, b1, a0, b0, next, 0, s + NST, slot);      // (in the last step: fragments read and never used)
+        slot = next;
+    };
+    int s = 0;
+    for (; s + NST < n_stages; ++s) step(std::true_type(), s);
+    for (; s < n_steps; ++s) step(std::false_type(), s);
+    if (KT & 1) {                            // the odd k-tile on its own (its fragments are read already)
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a0[i], b0[j], acc[i][j], 0, 0, 0);
+    }
+    f32x4 sn[TI];
+    float sm[TJ];
+#pragma unroll
+    for (int i = 0; i < TI; ++i) sn[i] = q8_col_scales(A, nt0 + wn * TI + i, g);
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) sm[j] = q8_row_scale(A, m0 + (wm * TJ + j) * 16 + r);
+    if (A.quads == 2) {
+        // through the LDS, a wave's own part of it, so that a row of the wave's columns leaves in whole cache lines
+        __builtin_amdgcn_s_waitcnt(waitcnt_imm(63, 0));
+        asm volatile("s_barrier" ::: "memory");
+        const int n0 = (nt0 + wn * TI) * 16;
+        // S: what waits in the LDS, T, or fp32 where a summand joins before the rounding
+        auto rows_out = [&](auto s_) __attribute__((always_inline)) {
+            typedef decltype(s_) S;
+            constexpr bool ADD = !std::is_same<S, T>::value || std::is_same<T, float>::value;
+            constexpr int E = 16 / sizeof(T), PIECES = TI * 16 / E, ROW = TI * 16 + 16 / sizeof(S);      // elements in 16 bytes of output; row pitch
+            static_assert(NW * 16 * ROW * sizeof(S) <= NST * STAGE, "rows fit");
+            S *mine = (S *)lds + wave * 16 * ROW;
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+#pragma unroll
+                for (int i = 0; i < TI; ++i) {
+                    Quad<S> q;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q.v[e] = (S)((float)acc[i][j][e] * sm[j] * sn[i][e]);
+                    *(Quad<S> *)__builtin_assume_aligned(mine + r * ROW + i * 16 + 4 * g, sizeof(Quad<S>)) = q;
+                }
+                const int m1 = m0 + (wm * TJ + j) * 16;
+#pragma unroll
+                for (int p = lane; p < 16 * PIECES; p += 64) {
+                    const int row = p / PIECES, c = (p % PIECES) * E;
+                    if (m1 + row >= A.rows || n0 + c >= A.N) continue;
+                    Piece<T> v;
+                    if constexpr (ADD) {
+                        Piece<T> y;
+                        if (A.add) y = *(const Piece<T> *)__builtin_assume_aligned((const T *)A.add + (m1 + row) * A.ld_add + n0 + c, 16);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const float x = (float)mine[row * ROW + c + e];
+                            v.v[e] = (T)(A.add ? x + (float)y.v[e] : x);
+                        }
+                    } else v = *(const Piece<T> *)__builtin_assume_aligned(mine + row * ROW + c, 16);
+                    *(Piece<T> *)__builtin_assume_aligned((T *)A.out + (m1 + row) * A.ld_out + n0 + c, 16) = v;
+                }
+            }
+        };
+        if (A.add) rows_out(0.f);
+        else rows_out(T());
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+            q8_store<T>(A, m0 + (wm * TJ + j) * 16 + r, (nt0 + wn * TI + i) * 16 + 4 * g, acc[i][j], sm[j], sn[i]);
+}
+
+// Rows too far apart for 32-bit offsets inside a panel: one wave per 64 columns x 64 rows, operands straight from memory
+template <class T>
+__global__ void __launch_bounds__(256) k_q8_far(Q8Args A) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nt0 = (blockIdx.y * 4 + wave) * 4;
+    const int64_t m0 = (int64_t)blockIdx.x * 64;
     if (nt0 >= A.NT) return;
     const int r = lane & 15, g = lane >> 4;
     const char *w[4];
     const int8_t *x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int nt = nt0 + i < A.NT ? nt0 + i : A.NT - 1, m = m0 + 16 * i + r;
+        const int nt = nt0 + i < A.NT ? nt0 + i : A.NT - 1;
+        const int64_t m = m0 + 16 * i + r;
         w[i] = A.packed + spd_q8_weights_at(A.N) + (size_t)nt * A.KT * 1024 + lane * 16;
-        x[i] = A.codes + (int64_t)(m < A.rows ? m : A.rows - 1) * A.ld_codes;
+        x[i] = A.codes + (m < A.rows ? m : A.rows - 1) * A.ld_codes;
     }
+    const int k_last = (A.K - 1) & ~15;
     i32x4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = (i32x4){0, 0, 0, 0};
     for (int kt = 0; kt < A.KT; ++kt) {
-        const int k = kt * 64 + 16 * g < A.K ? kt * 64 + 16 * g : 0;      // past K: anything, the weights are zero there
+        int k = kt * 64 + 16 * g;
+        k = k < k_last ? k : k_last;
         i32x4 a[4], b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -184,13 +497,94 @@ __global__ void __launch_bounds__(256) k_q8_tile(Q8Args A) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q8_store<T>(A, m0 + 16 * j + r, (nt0 + i) * 16 + 4 * g, acc[i][j]);
+        for (int j = 0; j < 4; ++j) {
+            const int64_t m = m0 + 16 * j + r;
+            if (m < A.rows) q8_store<T>(A, (int)m, (nt0 + i) * 16 + 4 * g, acc[i][j], A.scales[m], q8_col_scales(A, nt0 + i, g));
+        }
+}
+
+template <class T, int MT, int NP>
+hipError_t launch_skinny(const Q8Args &A, hipStream_t s) {
+    hipLaunchKernelGGL((k_q8_skinny<T, MT, NP>), dim3((A.NT + NP - 1) / NP, (A.rows + 16 * MT - 1) / (16 * MT)), dim3(512), 0, s, A);
+    return hipGetLastError();
+}
+// tiles tile0 .. of the order of tiles msub times as high as G's
+template <class T, class G>
+hipError_t launch_gemm(const Q8Args &A, hipStream_t s, int tile0 = 0, int n_tiles = -1, int msub = 1) {
+    constexpr int BN = G::WN * G::TI, BM = G::WM * G::TJ, LDS = G::NST * (BN + BM) * 2048;
+    static_assert(LDS <= 160 * 1024, "the stages must fit the LDS of a compute unit");
+    static std::once_flag once;
+    static hipError_t attr = hipSuccess;
+    std::call_once(once, [] { attr = hipFuncSetAttribute((const void *)k_q8_gemm<T, G>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS); });
+    if (attr != hipSuccess) return attr;
+    const int high = BM * 16 * msub;
+    spd_tile_order ord;
+    ord.TN = (A.NT + BN - 1) / BN;
+    ord.TM = (int)(((int64_t)A.rows + high - 1) / high);
+    spd_pick_block(ord.TN, ord.TM, BN * 16, high, ord.bn, ord.bm);
+    if (n_tiles < 0) n_tiles = ord.TN * ord.TM - tile0;
+    hipLaunchKernelGGL((k_q8_gemm<T, G>), dim3(msub == 1 ? spd_tile_launch_size(n_tiles) : n_tiles * msub), dim3(G::WN * G::WM * 64), LDS, s, A, ord,
+                       tile0, n_tiles, msub);
+    return hipGetLastError();
+}
+
+enum Q8Kind { Q8_FAR, Q8_11, Q8_12, Q8_14, Q8_22, Q8_42, Q8_SMALL, Q8_SQUARE, Q8_HALF, Q8_BIG, Q8_BIG_HALF };
+
+// Which kernel: the one that is estimated to end first.  A round of workgroups, one per compute unit, costs what a unit draws through its load
+// path (skinny kernels, small tiles) or multiplies (large ones) over K, and what comes before and after.  The figures, in us for a K of 8192
+// and beside it, are fits to measured calls of 1 to 8192 rows, K 1024 to 8192, N 1280 to 8192.
+Q8Kind q8_pick(int rows, int N, int KT, int64_t ld_codes) {
+    if (ld_codes > (1 << 22)) return Q8_FAR;                  // 256 rows of a panel within 2^31 bytes
+    const double k = KT / 128.0;
+    const int64_t NT = spd_q8_ntiles(N), MT = ((int64_t)rows + 15) / 16;
+    auto rounds = [](int64_t n) { return (double)((n + 255) / 256); };
+    auto tiles = [&](int bn, int bm) { return ((NT + bn - 1) / bn) * ((MT + bm - 1) / bm); };
+    Q8Kind best = Q8_BIG;
+    double least = 1e30;
+    auto offer = [&](Q8Kind kind, double us) {
+        if (us < least) {
+            least = us;
+            best = kind;
+        }
+    };
+    if (rows <= 512) {
+        offer(Q8_11, rounds(tiles(1, 1)) * (k * 3.4 * 2 + 1.6));
+        offer(Q8_12, rounds(tiles(2, 1)) * (k * 3.4 * 3 + 1.7));
+        offer(Q8_14, rounds(tiles(4, 1)) * (k * 3.4 * 5 + 1.9));
+        offer(Q8_22, rounds(tiles(2, 2)) * (k * 3.4 * 4 + 1.9));
+        offer(Q8_42, rounds(tiles(2, 4)) * (k * 3.4 * 6 + 2.3));
+    }
+    offer(Q8_SMALL, (tiles(8, 4) <= 256 ? 1.0 : 0.85) * rounds(tiles(8, 4)) * (k * 28 + 2));
+    offer(Q8_SQUARE, rounds(tiles(8, 8)) * (k * 38 + 2.7));
+    offer(Q8_HALF, rounds(tiles(16, 8)) * (k * 63 + 4));
+    const int64_t big = tiles(16, 16);
+    offer(Q8_BIG, rounds(big) * (k * 104 + 8));
+    if (big > 256 && big % 256) offer(Q8_BIG_HALF, (double)(big / 256) * (k * 104 + 8) + rounds(2 * (big % 256)) * (k * 63 + 4));
+    return best;
 }
 
 template <class T>
 hipError_t launch_product(const Q8Args &A, hipStream_t s) {
-    hipLaunchKernelGGL((k_q8_tile<T>), dim3((A.NT + 15) / 16, (A.rows + 63) / 64), dim3(256), 0, s, A);
-    return hipGetLastError();
+    switch (q8_pick(A.rows, A.N, A.KT, A.ld_codes)) {
+        case Q8_FAR:
+            hipLaunchKernelGGL((k_q8_far<T>), dim3((unsigned)(((int64_t)A.rows + 63) / 64), (A.NT + 15) / 16), dim3(256), 0, s, A);
+            return hipGetLastError();
+        case Q8_11: return launch_skinny<T, 1, 1>(A, s);
+        case Q8_12: return launch_skinny<T, 1, 2>(A, s);
+        case Q8_14: return launch_skinny<T, 1, 4>(A, s);
+        case Q8_22: return launch_skinny<T, 2, 2>(A, s);
+        case Q8_42: return launch_skinny<T, 4, 2>(A, s);
+        case Q8_SMALL: return launch_gemm<T, Q8Small>(A, s);
+        case Q8_SQUARE: return launch_gemm<T, Q8Square>(A, s);
+        case Q8_HALF: return launch_gemm<T, Q8Half>(A, s);
+        case Q8_BIG: return launch_gemm<T, Q8Big>(A, s);
+        case Q8_BIG_HALF: {
+            const int big = ((A.NT + 15) / 16) * (int)(((int64_t)A.rows + 255) / 256), rest = big % 256;
+            const hipError_t e = launch_gemm<T, Q8Big>(A, s, 0, big - rest);
+            return e != hipSuccess ? e : launch_gemm<T, Q8Half>(A, s, big - rest, rest, 2);
+        }
+    }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -222,7 +616,7 @@ size_t spd_q8_matmul_workspace(int32_t rows, int32_t K, int32_t N) {
 
 int spd_q8_matmul(int32_t rows, int32_t K, int32_t N, const int8_t *codes, int64_t ld_codes, const float *scales, const void *packed,
                   int32_t out_dtype, const void *add, int64_t ld_add, void *out, int64_t ld_out, void *workspace, void *stream) {
-    if (rows < 0 || !spd_q8_weight_bytes(K, N)) return SPD_EINVAL;
+    if (rows < 0 || rows > (1 << 30) || !spd_q8_weight_bytes(K, N) || (int64_t)rows * N > (int64_t)1 << 38) return SPD_EINVAL;
     if (out_dtype != SPD_F32 && out_dtype != SPD_BF16 && out_dtype != SPD_F16) return SPD_EINVAL;
     if (!codes || !scales || !packed || !out || ((uintptr_t)codes & 15) || ((uintptr_t)packed & 255) || ((uintptr_t)scales & 3)) return SPD_EINVAL;
     if (ld_codes % 16 || ld_codes < (K + 15) / 16 * 16 || ld_out < N || (add && ld_add < N)) return SPD_EINVAL;
@@ -232,7 +626,10 @@ int spd_q8_matmul(int32_t rows, int32_t K, int32_t N, const int8_t *codes, int64
     if (spd_q8_matmul_workspace(rows, K, N) && (!workspace || ((uintptr_t)workspace & 255))) return SPD_EINVAL;
     if (rows == 0) return SPD_OK;
     (void)hipGetLastError();
-    const Q8Args A{codes, scales, (const char *)packed, add, out, ld_codes, ld_add, ld_out, rows, K, N, spd_q8_ktiles(K), spd_q8_ntiles(N)};
+    const uintptr_t quad = 4 * es;
+    const bool quads = N % 4 == 0 && ld_out % 4 == 0 && (uintptr_t)out % quad == 0 && (!add || (ld_add % 4 == 0 && (uintptr_t)add % quad == 0));
+    const Q8Args A{codes, scales, (const char *)packed, add, out, ld_codes, ld_add, ld_out, rows, K, N, spd_q8_ktiles(K), spd_q8_ntiles(N),
+                   quads ? (N % (16 / es) == 0 && ld_out % (16 / es) == 0 && (uintptr_t)out % 16 == 0 && ld_add % (16 / es) == 0 && (uintptr_t)add % 16 == 0 ? 2 : 1) : 0};
     hipStream_t s = (hipStream_t)stream;
     SPD_HIP(out_dtype == SPD_F32 ? launch_product<float>(A, s) : out_dtype == SPD_BF16 ? launch_product<__bf16>(A, s) : launch_product<_Float16>(A, s));
     return SPD_OK;
