@@ -802,4 +802,4 @@ class PagePlan:
         self.q_cols, self.qkv_cols = c.n_q_heads * c.head_dim, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
         self.host_ptr, self.device_ptr = self.host.ctypes.data, self.device.data_ptr()
         n = self.workspace_bytes
-        self.workspace = torch.empty(n, dtype=torch.uint8, device=pages.device) if n else None
+        self.workspace = torch.zeros(n, dtype=torch.uint8, device=pages.device) if n else None

@@ -34,6 +34,8 @@ SPD_HD int spd_page_value_off(int r, int f, int E) {
 // of the sequence, then those from block0 on.
 // ------------------------------------------------------------------------------------------
 constexpr uint32_t SPD_PLAN_MAGIC = 0x53504731u;
+constexpr int SPD_COUNTERS = 16384;      // 32-bit, at the start of the workspace: items done of rows x head, zero between calls
+constexpr int SPD_SMALL_WAVES = 8;       // of a workgroup of the kernel for few rows
 constexpr int SPD_SMALL_ROWS = 16;       // rows (token x query head of the KV group) of an item of the kernel for few of them
 constexpr int SPD_LARGE_ROWS = 128;      // ... and of the kernel for many
 
@@ -47,10 +49,12 @@ struct spd_plan_item {                   // rows x blocks of one sequence, for e
     int32_t sink_blocks, block0;
     int32_t first, count;                // blocks of the list
     int32_t slot;                        // where its partial result goes, or -1: it is the whole result
-    int32_t pad;
+    int32_t slot0, parts;                // the rows' partial results: slots slot0 .. slot0 + parts - 1
+    int32_t group;                       // number of the rows among those cut into items
+    int32_t pad[2];
 };
 struct spd_plan_merge {                  // rows whose partial results lie in slots slot0 .. slot0 + parts - 1
-    int32_t seq, row0, rows, slot0, parts, large;
+    int32_t seq, row0, rows, slot0, parts, pad;
 };
 struct spd_plan_block {                  // a 16-position block that receives new tokens
     int32_t seq, block;
@@ -63,7 +67,7 @@ struct spd_plan_header {
     spd_pages_config cfg;                // of the handle that made the plan
     int32_t seqs, table, small, large, merge, write;            // byte offsets
     int32_t merge_rows, max_end;         // most rows of a merge, most positions of a sequence
-    size_t bytes, part_small, part_large, workspace;             // of the plan; byte offsets into the workspace; its size
+    size_t bytes, part_small, part_large, workspace;             // of the plan; byte offsets into the workspace (counters at 0); its size
 };
 
 // partial results: per slot and KV head `rows` x (d outputs, then maximum and sum), fp32

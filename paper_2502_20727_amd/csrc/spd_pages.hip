@@ -96,9 +96,14 @@ struct Block {
     char *head;
     int in_page;
 };
-__device__ __forceinline__ Block block_at(const Pages &P, const spd_plan_seq &s, int head, int block) {
-    const int page = ((const int *)(P.plan + P.table))[s.table + (block >> P.shift)];
+__device__ __forceinline__ int page_of(const Pages &P, const spd_plan_seq &s, int block) {
+    return ((const int *)(P.plan + P.table))[s.table + (block >> P.shift)];
+}
+__device__ __forceinline__ Block block_in(const Pages &P, int page, int head, int block) {
     return Block{P.pool + (size_t)page * P.page_bytes + (size_t)head * P.head_bytes, block & ((1 << P.shift) - 1)};
+}
+__device__ __forceinline__ Block block_at(const Pages &P, const spd_plan_seq &s, int head, int block) {
+    return block_in(P, page_of(P, s, block), head, block);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -305,6 +310,7 @@ struct AttendArgs {
     unsigned short *out;
     int64_t ld_q, ld_out;
     float *part;                // partial results of this kernel's items
+    int *counters;
     int window, sinks;
     float scale;                // log2(e) / sqrt(head_dim): softmax in powers of two
 };
@@ -315,31 +321,49 @@ __device__ __forceinline__ bool visible(int key, int at, int window, int sinks) 
 }
 __device__ __forceinline__ int list_block(const spd_plan_item &it, int v) { return v < it.sink_blocks ? v : it.block0 + (v - it.sink_blocks); }
 
+// is the whole block visible to every query between positions `first` and `last`?
+__device__ __forceinline__ bool all_visible(int block, int first, int last, int window, int sinks) {
+    const int k0 = block * 16, k1 = k0 + 15;
+    return k1 <= first && (window == 0 || k0 > last - window || k1 < sinks);
+}
+
 // operands of one 16-position block, as loaded
 template <int D, bool E4M3>
 struct BlockLoad {
     static constexpr int CH = E4M3 ? D / 64 : D / 32;      // 16-byte chunks per lane, keys and values each
     i32x4 k[CH], v[CH];
     f32x4 ks, vs;                                           // scales of keys 4 g .. 4 g + 3
-    __device__ __forceinline__ void load(const Pages &P, const spd_plan_seq &s, int head, int block, int lane) {
+    __device__ __forceinline__ void load(const Pages &P, const Block &B, int lane) {
         constexpr int W = E4M3 ? 1 : 2;
-        const Block B = block_at(P, s, head, block);
         const char *keys = B.head + (size_t)B.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
-        const float *scales = (const float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16 + 4 * (lane >> 4);
+        const float *scales = (const float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16;
+        const int g4 = 4 * (lane >> 4);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) k[c] = *(const i32x4 *)(keys + c * 1024 + lane * 16);
-        ks = *(const f32x4 *)scales;
+        for (int c = 0; c < CH; ++c) k[c] = __builtin_nontemporal_load((const i32x4 *)(keys + c * 1024 + lane * 16));
+        ks = *(const f32x4 *)(scales + g4);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] = *(const i32x4 *)(values + c * 1024 + lane * 16);
-        vs = *(const f32x4 *)(scales + P.page_size);
+        for (int c = 0; c < CH; ++c) v[c] = __builtin_nontemporal_load((const i32x4 *)(values + c * 1024 + lane * 16));
+        vs = *(const f32x4 *)(scales + P.page_size + g4);
     }
 };
 
-// Few rows (a decode step, a short draft): one workgroup per item and KV head, its four waves take pairs of blocks in turn and merge
-// their states in the LDS.  Lane = 16 g + row.
+// A partial result is written by one workgroup and read by another, perhaps on another die with an L2 of its own: both go past that
+// L2, as relaxed atomics of the device's scope do.
+__device__ __forceinline__ void part_put(float *p, float a, float b) {
+    const unsigned long long v = (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32;
+    __hip_atomic_store((unsigned long long *)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 part_get(const float *p) {
+    const unsigned long long v = __hip_atomic_load((const unsigned long long *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+
+// Few rows (a decode step, a short draft): one workgroup per item and KV head, its eight waves take pairs of blocks in turn and merge
+// their states in the LDS.  Rows cut into several items are joined, in the items' order, by the workgroup that ends last.
+// Lane = 16 g + row.
 template <int D, bool E4M3, bool F16>
-__global__ void __launch_bounds__(256) k_attend_small(AttendArgs A) {
-    constexpr int DT = D / 16, NF = D / 32;
+__global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
+    constexpr int DT = D / 16, NF = D / 32, NW = SPD_SMALL_WAVES;
     typedef Half<F16> QK;                        // queries and keys
     typedef Half<F16 && !E4M3> PV;               // probabilities (times a scale that may be tiny: bf16 beside e4m3) and values
     const Pages &P = A.P;
@@ -350,7 +374,14 @@ __global__ void __launch_bounds__(256) k_attend_small(AttendArgs A) {
     const int row = lane & 15, g = lane >> 4;
     const int rows = s.q_len * P.group;          // at most 16
     const int token = row / P.group;
-    const int at = s.pos + token;
+    const int at = s.pos + token, last = s.end - 1;
+    // the wave's pairs are number wave, wave + NW, ... of the item's; lane i keeps the page of the i-th of the next 64 blocks
+    const int n_pairs = (it.count + 1) / 2, mine = (n_pairs - wave + NW - 1) / NW;
+    auto my_block = [&](int i) {                 // i-th block of the wave (the missing half of the last pair: its first)
+        const int v = 2 * (wave + NW * (i >> 1)) + (i & 1);
+        return list_block(it, it.first + (v < it.count ? v : it.count - 1));
+    };
+    int pages = mine > 0 ? page_of(P, s, my_block(lane < 2 * mine ? lane : 0)) : 0;
     i32x4 qf[NF];
     {
         const unsigned short *qp = A.q + (int64_t)(s.tok0 + token) * A.ld_q + (int64_t)(head * P.group + row % P.group) * D;
@@ -364,12 +395,21 @@ __global__ void __launch_bounds__(256) k_attend_small(AttendArgs A) {
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = -__builtin_inff(), l = 0.f;
-    for (int p = wave; 2 * p < it.count; p += 4) {
-        const bool two = 2 * p + 1 < it.count;
-        const int b0 = list_block(it, it.first + 2 * p), b1 = two ? list_block(it, it.first + 2 * p + 1) : b0;
-        BlockLoad<D, E4M3> x0, x1;
-        x0.load(P, s, head, b0, lane);
-        x1.load(P, s, head, b1, lane);
+    struct Pair {
+        BlockLoad<D, E4M3> x[2];
+    };
+    auto load = [&](Pair &f, int j) __attribute__((always_inline)) {      // pair j of the wave
+        if (j > 0 && (j & 31) == 0) pages = page_of(P, s, my_block(2 * j + lane < 2 * mine ? 2 * j + lane : 2 * j));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int page = __builtin_amdgcn_readlane(pages, (2 * j + h) & 63);
+            f.x[h].load(P, block_in(P, page, head, my_block(2 * j + h)), lane);
+        }
+    };
+    auto use = [&](const Pair &f, int j) __attribute__((always_inline)) {
+        const bool two = 2 * (wave + NW * j) + 1 < it.count;
+        const int b0 = my_block(2 * j), b1 = my_block(2 * j + 1);
+        const BlockLoad<D, E4M3> &x0 = f.x[0], &x1 = f.x[1];
         f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
@@ -384,26 +424,38 @@ __global__ void __launch_bounds__(256) k_attend_small(AttendArgs A) {
             s0 = QK::mfma16(k0, qf[i], s0);
             s1 = QK::mfma16(k1, qf[i], s1);
         }
-        float mx = -__builtin_inff();
+        f32x4 v0 = x0.vs, v1 = x1.vs;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s0[i] = visible(b0 * 16 + 4 * g + i, at, A.window, A.sinks) ? s0[i] * (x0.ks[i] * A.scale) : -__builtin_inff();
-            s1[i] = two && visible(b1 * 16 + 4 * g + i, at, A.window, A.sinks) ? s1[i] * (x1.ks[i] * A.scale) : -__builtin_inff();
-            mx = fmaxf(mx, fmaxf(s0[i], s1[i]));
+            s0[i] *= x0.ks[i] * A.scale;
+            s1[i] *= x1.ks[i] * A.scale;
         }
+        // (the scale of a hidden key's value may be NaN)
+        if (!(two && all_visible(b0, s.pos, last, A.window, A.sinks) && all_visible(b1, s.pos, last, A.window, A.sinks))) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!visible(b0 * 16 + 4 * g + i, at, A.window, A.sinks)) {
+                    s0[i] = -__builtin_inff();
+                    v0[i] = 0.f;
+                }
+                if (!two || !visible(b1 * 16 + 4 * g + i, at, A.window, A.sinks)) {
+                    s1[i] = -__builtin_inff();
+                    v1[i] = 0.f;
+                }
+            }
+        }
+        float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
         const float m_new = fmaxf(m, quad_max(mx)), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(m - m_use);
-        float ps = 0.f;
-        float w0[4], w1[4];
+        float ps = 0.f, w0[4], w1[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float p0 = __builtin_amdgcn_exp2f(s0[i] - m_use), p1 = __builtin_amdgcn_exp2f(s1[i] - m_use);
             ps += p0 + p1;
-            // (the scale of a hidden key's value may be NaN)
-            w0[i] = s0[i] == -__builtin_inff() ? 0.f : p0 * x0.vs[i];
-            w1[i] = s1[i] == -__builtin_inff() ? 0.f : p1 * x1.vs[i];
+            w0[i] = p0 * v0[i];
+            w1[i] = p1 * v1[i];
         }
-        l = l * alpha + quad_sum(ps);
+        l = l * alpha + ps;                      // (of the lane's keys; the four lanes of a row meet at the end)
         m = m_new;
         const i32x4 pf = {PV::pack(w0[0], w0[1]), PV::pack(w0[2], w0[3]), PV::pack(w1[0], w1[1]), PV::pack(w1[2], w1[3])};
 #pragma unroll
@@ -413,9 +465,23 @@ __global__ void __launch_bounds__(256) k_attend_small(AttendArgs A) {
             else vf = (i32x4){x0.v[t >> 1][2 * (t & 1)], x0.v[t >> 1][2 * (t & 1) + 1], x1.v[t >> 1][2 * (t & 1)], x1.v[t >> 1][2 * (t & 1) + 1]};
             o[t] = PV::mfma16(vf, pf, o[t] * alpha);
         }
+    };
+    if (mine > 0) {
+        Pair f0, f1;
+        load(f0, 0);
+        for (int j = 0; j < mine; j += 2) {      // the next pair is on its way while one is used
+            if (j + 1 < mine) load(f1, j + 1);
+            use(f0, j);
+            if (j + 1 < mine) {
+                if (j + 2 < mine) load(f0, j + 2);
+                use(f1, j + 1);
+            }
+        }
     }
+    l = quad_sum(l);
     // merge the waves
-    __shared__ float so[4][16][D + 4], sm[4][16], sl[4][16];
+    __shared__ float so[NW][16][D + 4], sm[NW][16], sl[NW][16];
+    __shared__ int ended;
 #pragma unroll
     for (int t = 0; t < DT; ++t) *(f32x4 *)&so[wave][row][t * 16 + 4 * g] = o[t];
     if (g == 0) {
@@ -423,41 +489,107 @@ __global__ void __launch_bounds__(256) k_attend_small(AttendArgs A) {
         sl[wave][row] = l;
     }
     __syncthreads();
-    constexpr int N = D / 16;
-    const int mr = threadIdx.x >> 4, f0 = (threadIdx.x & 15) * N;
+    constexpr int N = D / 32;                    // of a row by each of 32 threads
+    const int mr = threadIdx.x >> 5, f0 = (threadIdx.x & 31) * N;
     float mm = -__builtin_inff();
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm[w][mr]);
-    const float m_use = mm == -__builtin_inff() ? 0.f : mm;
+    for (int w = 0; w < NW; ++w) mm = fmaxf(mm, sm[w][mr]);
+    float m_use = mm == -__builtin_inff() ? 0.f : mm;
     float ll = 0.f, acc[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
         const float f = __builtin_amdgcn_exp2f(sm[w][mr] - m_use);
         ll += f * sl[w][mr];
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[i] += f * so[w][mr][f0 + i];
     }
-    if (mr >= rows) return;
-    if (it.slot < 0) {
-        int *to = (int *)(A.out + (int64_t)(s.tok0 + mr / P.group) * A.ld_out + (int64_t)(head * P.group + mr % P.group) * D + f0);
-        const float inv = 1.f / ll;
+    if (it.slot >= 0) {
+        constexpr int PART = SPD_SMALL_ROWS * (D + 2), ML = SPD_SMALL_ROWS * D;
+        float *to = A.part + ((size_t)it.slot * P.kv + head) * PART;
+        if (mr < rows) {
 #pragma unroll
-        for (int i = 0; i < N; i += 2) to[i / 2] = QK::pack(acc[i] * inv, acc[i + 1] * inv);
-    } else {
-        float *to = A.part + ((size_t)it.slot * P.kv + head) * (SPD_SMALL_ROWS * (D + 2));
+            for (int i = 0; i < N; i += 2) part_put(to + mr * D + f0 + i, acc[i], acc[i + 1]);
+            if (f0 == 0) part_put(to + ML + 2 * mr, mm, ll);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the wave's part has left
+        __syncthreads();
+        int *counter = A.counters + it.group * P.kv + head;
+        if (threadIdx.x == 0) ended = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (ended != it.parts - 1) return;
+        if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // 32 threads per row and set of parts: with fewer than sixteen rows several sets side by side, joined in the LDS
+        const int rshift = rows > 8 ? 4 : rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0, sets = 16 >> rshift;
+        const int jr = mr & ((1 << rshift) - 1), set = mr >> rshift;
+        const float *p = A.part + ((size_t)it.slot0 * P.kv + head) * PART;
+        const size_t step = (size_t)P.kv * PART;
+        mm = -__builtin_inff();
+        ll = 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) to[mr * D + f0 + i] = acc[i];
-        if (f0 == 0) {
-            to[SPD_SMALL_ROWS * D + mr] = mm;
-            to[SPD_SMALL_ROWS * D + SPD_SMALL_ROWS + mr] = ll;
+        for (int i = 0; i < N; ++i) acc[i] = 0.f;
+        constexpr int NB = 8;                    // parts asked for at a time
+        if (jr < rows)
+            for (int i0 = set; i0 < it.parts; i0 += NB * sets) {
+                float2 ml[NB], x[NB][N / 2];
+#pragma unroll
+                for (int u = 0; u < NB; ++u) {
+                    const float *q = p + (size_t)(i0 + u * sets < it.parts ? i0 + u * sets : i0) * step;
+                    ml[u] = part_get(q + ML + 2 * jr);
+#pragma unroll
+                    for (int i = 0; i < N / 2; ++i) x[u][i] = part_get(q + jr * D + f0 + 2 * i);
+                }
+#pragma unroll
+                for (int u = 0; u < NB; ++u) {
+                    if (i0 + u * sets >= it.parts) break;
+                    const float m_new = fmaxf(mm, ml[u].x);
+                    m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+                    const float fa = __builtin_amdgcn_exp2f(mm - m_use), fb = __builtin_amdgcn_exp2f(ml[u].x - m_use);
+                    mm = m_new;
+                    ll = ll * fa + ml[u].y * fb;
+#pragma unroll
+                    for (int i = 0; i < N / 2; ++i) {
+                        acc[2 * i] = acc[2 * i] * fa + x[u][i].x * fb;
+                        acc[2 * i + 1] = acc[2 * i + 1] * fa + x[u][i].y * fb;
+                    }
+                }
+            }
+        if (sets > 1) {
+            float *lo = &so[0][0][0], *lm = &sm[0][0], *ls = &sl[0][0];      // (sixteen rows of the waves' places)
+#pragma unroll
+            for (int i = 0; i < N; ++i) lo[mr * (D + 4) + f0 + i] = acc[i];
+            if (f0 == 0) {
+                lm[mr] = mm;
+                ls[mr] = ll;
+            }
+            __syncthreads();
+            if (mr >= rows) return;
+            mm = -__builtin_inff();
+            for (int u = 0; u < sets; ++u) mm = fmaxf(mm, lm[(u << rshift) + mr]);
+            m_use = mm == -__builtin_inff() ? 0.f : mm;
+            ll = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc[i] = 0.f;
+            for (int u = 0; u < sets; ++u) {
+                const int from = (u << rshift) + mr;
+                const float f = __builtin_amdgcn_exp2f(lm[from] - m_use);
+                ll += f * ls[from];
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc[i] += f * lo[from * (D + 4) + f0 + i];
+            }
         }
     }
+    if (mr >= rows) return;
+    int *to = (int *)(A.out + (int64_t)(s.tok0 + mr / P.group) * A.ld_out + (int64_t)(head * P.group + mr % P.group) * D + f0);
+    const float inv = 1.f / ll;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) to[i / 2] = QK::pack(acc[i] * inv, acc[i + 1] * inv);
 }
 
 // Many rows (a prompt's chunk): one workgroup per 128 rows and KV head; each wave has 32 of them, tiles of 64 keys go through the LDS in 16
-// bits, dequantised once for the workgroup.  Lane = 32 half + row.
+// bits, dequantised once for the workgroup, two stages: while one is used the next is loaded into registers, and put away ahead of
+// the second contraction.  Lane = 32 half + row.
 template <int D, bool E4M3, bool F16>
 __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     constexpr int W = E4M3 ? 1 : 2, KS = D / 16, DT = D / 32, CH = E4M3 ? D / 64 : D / 32;
@@ -474,9 +606,13 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     const bool live = row < n_rows;
     const int token = (live ? row : n_rows - 1) / P.group, qh = head * P.group + (live ? row : n_rows - 1) % P.group;
     const int at = s.pos + token;
+    const int first_at = __builtin_amdgcn_readfirstlane(at), last_at = __builtin_amdgcn_readlane(at, 31);
     // keys: [block][feature / 8][position][8]; values: [block][feature / 16][half][feature % 16][8 positions of the half]
-    __shared__ __attribute__((aligned(16))) short lk[64 * D], lv[64 * D];
-    __shared__ __attribute__((aligned(16))) float lks[64], lvs[64];
+    struct Stage {
+        short k[64 * D], v[64 * D];
+        float ks[64], vs[64];      // (of the keys: times the softmax's scale)
+    };
+    __shared__ __attribute__((aligned(16))) Stage stage[2];
     i32x4 qf[KS];
     {
         const unsigned short *qp = A.q + (int64_t)(s.tok0 + token) * A.ld_q + (int64_t)qh * D;
@@ -489,40 +625,73 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = -__builtin_inff(), l = 0.f;
-    for (int v0 = 0; v0 < it.count; v0 += 4) {
-        __syncthreads();
-        {       // wave w brings the tile's block w
-            const int v = v0 + wave < it.count ? v0 + wave : it.count - 1;
-            const int r = lane & 15, g = lane >> 4;
-            const Block B = block_at(P, s, head, list_block(it, it.first + v));
-            const char *keys = B.head + (size_t)B.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
-            const float *scales = (const float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16;
-            i32x4 k[CH], x[CH];
+    // wave w brings block w of a tile
+    const int r16 = lane & 15, g = lane >> 4;
+    auto my_block = [&](int v0) { return list_block(it, it.first + (v0 + wave < it.count ? v0 + wave : it.count - 1)); };
+    i32x4 kx[CH], vx[CH];
+    float sx = 0.f;
+    auto fetch = [&](int v0, int page) __attribute__((always_inline)) {
+        const Block B = block_in(P, page, head, my_block(v0));
+        const char *keys = B.head + (size_t)B.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
+        const float *scales = (const float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                k[c] = *(const i32x4 *)(keys + c * 1024 + lane * 16);
-                x[c] = *(const i32x4 *)(values + c * 1024 + lane * 16);
-            }
-            if (lane < 32) (lane < 16 ? lks : lvs)[wave * 16 + r] = scales[lane < 16 ? r : P.page_size + r];
-            short *kd = lk + wave * 16 * D, *vd = lv + wave * 16 * D;
+        for (int c = 0; c < CH; ++c) kx[c] = *(const i32x4 *)(keys + c * 1024 + lane * 16);
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                if constexpr (E4M3) {
-                    *(i32x4 *)(kd + ((8 * c + 2 * g) * 16 + r) * 8) = QK::widen(k[c][0], k[c][1]);
-                    *(i32x4 *)(kd + ((8 * c + 2 * g + 1) * 16 + r) * 8) = QK::widen(k[c][2], k[c][3]);
+        for (int c = 0; c < CH; ++c) vx[c] = *(const i32x4 *)(values + c * 1024 + lane * 16);
+        if (lane < 32) sx = scales[lane < 16 ? r16 : P.page_size + r16];
+    };
+    auto put_away = [&](Stage &to) __attribute__((always_inline)) {
+        short *kd = to.k + wave * 16 * D, *vd = to.v + wave * 16 * D;
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        *(i32x2 *)(vd + (((4 * c + t) * 2 + (g & 1)) * 16 + r) * 8 + (g >> 1) * 4) =
-                            (i32x2){PV::template from_e4m3<false>(x[c][t]), PV::template from_e4m3<true>(x[c][t])};
-                } else {
-                    *(i32x4 *)(kd + ((4 * c + g) * 16 + r) * 8) = k[c];
+        for (int c = 0; c < CH; ++c) {
+            if constexpr (E4M3) {
+                *(i32x4 *)(kd + ((8 * c + 2 * g) * 16 + r16) * 8) = QK::widen(kx[c][0], kx[c][1]);
+                *(i32x4 *)(kd + ((8 * c + 2 * g + 1) * 16 + r16) * 8) = QK::widen(kx[c][2], kx[c][3]);
+            } else *(i32x4 *)(kd + ((4 * c + g) * 16 + r16) * 8) = kx[c];
+        }
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        *(i32x2 *)(vd + (((2 * c + t) * 2 + (g & 1)) * 16 + r) * 8 + (g >> 1) * 4) = (i32x2){x[c][2 * t], x[c][2 * t + 1]};
-                }
+        for (int c = 0; c < CH; ++c) {
+            if constexpr (E4M3) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    *(i32x2 *)(vd + (((4 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) =
+                        (i32x2){PV::template from_e4m3<false>(vx[c][t]), PV::template from_e4m3<true>(vx[c][t])};
+            } else {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    *(i32x2 *)(vd + (((2 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) = (i32x2){vx[c][2 * t], vx[c][2 * t + 1]};
             }
         }
-        __syncthreads();
+        if (lane < 16) to.ks[wave * 16 + r16] = sx * A.scale;
+        else if (lane < 32) to.vs[wave * 16 + r16] = sx;
+    };
+    int page = page_of(P, s, my_block(0));
+    fetch(0, page);
+    page = page_of(P, s, my_block(4));
+    put_away(stage[0]);
+    __syncthreads();
+    for (int v0 = 0, turn = 0; v0 < it.count; v0 += 4, turn ^= 1) {
+        const Stage &now = stage[turn];
+        const bool more = v0 + 4 < it.count;
+        if (more) {
+            fetch(v0 + 4, page);
+            page = page_of(P, s, my_block(v0 + 8));
+        }
+        // which of the tile's blocks the wave's queries see: all of a block, some, or none
+        bool all = v0 + 4 <= it.count, any = false;
+        int key0[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int block = v0 + b < it.count ? list_block(it, it.first + v0 + b) : 0x7fffff;
+            key0[b] = block * 16;
+            all = all && all_visible(block, first_at, last_at, A.window, A.sinks);
+            any = any || (key0[b] <= last_at && (A.window == 0 || key0[b] + 15 > first_at - A.window || key0[b] < A.sinks));
+        }
+        if (!any) {                              // (the wave's rows lie before the tile, or past its window)
+            if (more) put_away(stage[turn ^ 1]);
+            __syncthreads();
+            continue;
+        }
         f32x16 sc[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -530,62 +699,91 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
             for (int i = 0; i < 16; ++i) sc[h][i] = 0.f;
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
-                const i32x4 kf = *(const i32x4 *)(lk + (2 * h + (col >> 4)) * 16 * D + ((2 * i + half) * 16 + (col & 15)) * 8);
+                const i32x4 kf = *(const i32x4 *)(now.k + (2 * h + (col >> 4)) * 16 * D + ((2 * i + half) * 16 + (col & 15)) * 8);
                 sc[h] = QK::mfma32(kf, qf[i], sc[h]);
             }
         }
         // score i of half h: block 2 h + i / 8 of the tile, position 8 ((i / 4) % 2) + 4 half + i % 4 in it
-        float mx = -__builtin_inff();
+        f32x4 ks[8], vs[8];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const bool there = v0 + b < it.count;
-            const int key0 = there ? list_block(it, it.first + v0 + b) * 16 : 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = 8 * (i >> 2) + 4 * half + (i & 3);
-                const float x = sc[b >> 1][(b & 1) * 8 + i] * (lks[b * 16 + r] * A.scale);
-                const float y = there && visible(key0 + r, at, A.window, A.sinks) ? x : -__builtin_inff();
-                sc[b >> 1][(b & 1) * 8 + i] = y;
-                mx = fmaxf(mx, y);
-            }
+        for (int q = 0; q < 8; ++q) {
+            ks[q] = *(const f32x4 *)(now.ks + q * 8 + 4 * half);
+            vs[q] = *(const f32x4 *)(now.vs + q * 8 + 4 * half);
         }
-        const float m_new = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32, 64))), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[q >> 2][(q & 3) * 4 + i] *= ks[q][i];
+        if (!all) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!visible(key0[q >> 1] + 8 * (q & 1) + 4 * half + i, at, A.window, A.sinks)) {
+                        sc[q >> 2][(q & 3) * 4 + i] = -__builtin_inff();
+                        vs[q][i] = 0.f;          // (it may be NaN)
+                    }
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = fmaxf(m, mx), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+        m = m_new;
+        i32x4 pf[4];
         float ps = 0.f;
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             float w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float x = sc[b >> 1][(b & 1) * 8 + i], p = __builtin_amdgcn_exp2f(x - m_use);
+                const float p = __builtin_amdgcn_exp2f(sc[b >> 1][(b & 1) * 8 + i] - m_use);
                 ps += p;
-                w[i] = x == -__builtin_inff() ? 0.f : p * lvs[b * 16 + 8 * (i >> 2) + 4 * half + (i & 3)];
+                w[i] = p * vs[2 * b + (i >> 2)][i & 3];
             }
-            const i32x4 pf = {PV::pack(w[0], w[1]), PV::pack(w[2], w[3]), PV::pack(w[4], w[5]), PV::pack(w[6], w[7])};
+            pf[b] = (i32x4){PV::pack(w[0], w[1]), PV::pack(w[2], w[3]), PV::pack(w[4], w[5]), PV::pack(w[6], w[7])};
+        }
+        l = l * alpha + ps;                      // (of the lane's half of the keys)
+        if (more) put_away(stage[turn ^ 1]);
+        // (a factor of exactly 1 changes nothing; maxima settle after the first tiles)
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
-                const i32x4 vf = *(const i32x4 *)(lv + b * 16 * D + (((2 * t + (col >> 4)) * 2 + half) * 16 + (col & 15)) * 8);
-                o[t] = PV::mfma32(vf, pf, o[t]);
+                const i32x4 vf = *(const i32x4 *)(now.v + b * 16 * D + (((2 * t + (col >> 4)) * 2 + half) * 16 + (col & 15)) * 8);
+                o[t] = PV::mfma32(vf, pf[b], o[t]);
             }
-        }
-        l = l * alpha + ps + __shfl_xor(ps, 32, 64);
-        m = m_new;
+        __syncthreads();
     }
-    if (!live) return;
+    l += __shfl_xor(l, 32, 64);
     if (it.slot < 0) {
+        // through the LDS, so that rows leave in whole cache lines
+        constexpr int ROW = D + 8, PIECES = D / 8;
+        static_assert(4 * 32 * ROW * 2 <= (int)sizeof(stage), "rows fit");
+        short *mine = (short *)stage + wave * 32 * ROW;
         const float inv = 1.f / l;
-        int *to = (int *)(A.out + (int64_t)(s.tok0 + token) * A.ld_out + (int64_t)qh * D);
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                *(i32x2 *)(to + (32 * t + 2 * i + 4 * half) / 2) =
+                *(i32x2 *)(mine + col * ROW + 32 * t + 2 * i + 4 * half) =
                     (i32x2){QK::pack(o[t][i] * inv, o[t][i + 1] * inv), QK::pack(o[t][i + 2] * inv, o[t][i + 3] * inv)};
-    } else {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int p = lane; p < 32 * PIECES; p += 64) {
+            const int pr = it.row0 + wave * 32 + p / PIECES, c = (p % PIECES) * 8;
+            if (pr < n_rows)
+                *(i32x4 *)(A.out + (int64_t)(s.tok0 + pr / P.group) * A.ld_out + (int64_t)(head * P.group + pr % P.group) * D + c) =
+                    *(const i32x4 *)(mine + (p / PIECES) * ROW + c);
+        }
+    } else if (live) {
         float *to = A.part + ((size_t)it.slot * P.kv + head) * (SPD_LARGE_ROWS * (D + 2));
         const int pr = wave * 32 + col;
 #pragma unroll
@@ -600,32 +798,42 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     }
 }
 
-// Joins the partial results of rows whose blocks were cut into several items: a wave per row, in the order of the items.
+// Joins the partial results of a chunk's rows whose blocks were cut into several items: a wave per row, in the order of the items.
 template <int D, bool F16>
-__global__ void __launch_bounds__(256) k_attend_merge(Pages P, const float *part_small, const float *part_large, unsigned short *out,
-                                                      int64_t ld_out) {
+__global__ void __launch_bounds__(256) k_attend_merge(Pages P, const float *part, unsigned short *out, int64_t ld_out) {
+    constexpr int N = D / 64, CAP = SPD_LARGE_ROWS, NB = 8;      // NB: parts asked for at a time
     const int head = blockIdx.x % P.kv;
-    const spd_plan_merge g = ((const spd_plan_merge *)(P.plan + P.list))[blockIdx.x / P.kv];
+    const spd_plan_merge j = ((const spd_plan_merge *)(P.plan + P.list))[blockIdx.x / P.kv];
     const int r = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (r >= g.rows) return;
-    const spd_plan_seq s = ((const spd_plan_seq *)(P.plan + P.seqs))[g.seq];
-    const int cap = g.large ? SPD_LARGE_ROWS : SPD_SMALL_ROWS;
-    const size_t step = (size_t)P.kv * cap * (D + 2);
-    const float *p = (g.large ? part_large : part_small) + ((size_t)g.slot0 * P.kv + head) * (cap * (D + 2));
-    float m = -__builtin_inff();
-    for (int i = 0; i < g.parts; ++i) m = fmaxf(m, p[i * step + cap * D + r]);
-    const float m_use = m == -__builtin_inff() ? 0.f : m;
-    constexpr int N = D / 64;
-    float l = 0.f, acc[N];
+    if (r >= j.rows) return;
+    const spd_plan_seq s = ((const spd_plan_seq *)(P.plan + P.seqs))[j.seq];
+    const size_t step = (size_t)P.kv * CAP * (D + 2);
+    const float *p = part + ((size_t)j.slot0 * P.kv + head) * (CAP * (D + 2));
+    float mm = -__builtin_inff(), l = 0.f, acc[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) acc[j] = 0.f;
-    for (int i = 0; i < g.parts; ++i) {
-        const float f = __builtin_amdgcn_exp2f(p[i * step + cap * D + r] - m_use);
-        l += f * p[i * step + cap * D + cap + r];
+    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+    for (int i0 = 0; i0 < j.parts; i0 += NB) {
+        float m[NB], sum[NB], x[NB][N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) acc[j] += f * p[i * step + (size_t)r * D + lane * N + j];
+        for (int u = 0; u < NB; ++u) {
+            const float *q = p + (size_t)(i0 + u < j.parts ? i0 + u : j.parts - 1) * step;
+            m[u] = q[CAP * D + r];
+            sum[u] = q[CAP * D + CAP + r];
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[u][e] = q[(size_t)r * D + lane * N + e];
+        }
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            if (i0 + u >= j.parts) break;
+            const float m_new = fmaxf(mm, m[u]), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+            const float fa = __builtin_amdgcn_exp2f(mm - m_use), fb = __builtin_amdgcn_exp2f(m[u] - m_use);
+            mm = m_new;
+            l = l * fa + sum[u] * fb;
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] = acc[e] * fa + x[u][e] * fb;
+        }
     }
-    const int row = g.row0 + r;
+    const int row = j.row0 + r;
     unsigned short *to = out + (int64_t)(s.tok0 + row / P.group) * ld_out + (int64_t)(head * P.group + row % P.group) * D + lane * N;
     const float inv = 1.f / l;
     if constexpr (N == 2) *(int *)to = Half<F16>::pack(acc[0] * inv, acc[1] * inv);
@@ -755,6 +963,7 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
     A.ld_out = ld_out;
     A.window = h.window;
     A.sinks = h.sinks;
+    A.counters = nullptr;
     A.scale = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
     float *small = workspace ? (float *)((char *)workspace + h.part_small) : nullptr,
           *large = workspace ? (float *)((char *)workspace + h.part_large) : nullptr;
@@ -771,13 +980,14 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
         if (h.n_small) {
             A.P = pages_args(pages, h, plan_dev, pool, h.small);
             A.part = small;
-            hipLaunchKernelGGL((k_attend_small<D, E, F>), dim3(h.n_small * c.n_kv_heads), dim3(256), 0, s, A);
+            A.counters = (int *)workspace;
+            hipLaunchKernelGGL((k_attend_small<D, E, F>), dim3(h.n_small * c.n_kv_heads), dim3(64 * SPD_SMALL_WAVES), 0, s, A);
             SPD_TRY(hipGetLastError());
         }
         if (h.n_merge) {
             const Pages P = pages_args(pages, h, plan_dev, pool, h.merge);
             hipLaunchKernelGGL((k_attend_merge<D, F>), dim3(h.n_merge * c.n_kv_heads, (h.merge_rows + 3) / 4), dim3(256), 0, s, P,
-                               (const float *)small, (const float *)large, (unsigned short *)out, ld_out);
+                               (const float *)large, (unsigned short *)out, ld_out);
             SPD_TRY(hipGetLastError());
         }
         return hipSuccess;

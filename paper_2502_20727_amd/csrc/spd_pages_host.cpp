@@ -9,9 +9,9 @@
 
 namespace {
 
-// The chip holds SMALL_TARGET workgroups of the kernel for few rows at once, LARGE_TARGET of the one for many.
-constexpr int SMALL_TARGET = 768, LARGE_TARGET = 512;
-constexpr int SMALL_MIN_BLOCKS = 8;      // of an item: a pair of blocks for each of the workgroup's four waves
+// The chip holds SMALL_TARGET workgroups of the kernel for few rows at once (one of eight waves per compute unit: 48 sequences of up to 16000
+// 31.0 us, two of four waves 33 to 38), LARGE_TARGET of the one for many.
+constexpr int SMALL_TARGET = 256, LARGE_TARGET = 512;
 constexpr int LARGE_MIN_BLOCKS = 16;
 
 struct Piece {
@@ -33,16 +33,25 @@ Piece piece_of(const spd_pages *P, int seq, int pos, int row0, int rows, int win
     return w;
 }
 
-// Cuts pieces into items of about equal numbers of blocks, enough of them for `target` workgroups; `unit` blocks go together.
-void cut(const std::vector<Piece> &pieces, int kv, int target, int least, int unit, int large, std::vector<spd_plan_item> &items,
+// Cuts pieces into items of at most `chunk` blocks, the fewest that gives no more than `target` workgroups (0: not at all); `unit` blocks go
+// together.  most(blocks): the most items a piece is cut into.
+template <class Most>
+void cut(const std::vector<Piece> &pieces, int kv, int target, int unit, Most most, std::vector<spd_plan_item> &items,
          std::vector<spd_plan_merge> &merges, int &slots) {
     int64_t total = 0;
     for (const Piece &w : pieces) total += w.total;
-    const int64_t share = (total * kv + target - 1) / target;
-    const int64_t chunk = std::max<int64_t>(least, (share + unit - 1) / unit * unit);
+    int64_t chunk = target ? std::max<int64_t>(unit, ((total * kv + target - 1) / target + unit - 1) / unit * unit) : 0;
+    auto parts_of = [&](const Piece &w) { return chunk ? (int)std::min<int64_t>(most(w.total), (w.total + chunk - 1) / chunk) : 1; };
+    // (what lengths leave over after whole chunks makes more items than the target: longer chunks, while cutting is what makes them)
+    for (int i = 0; i < 16 && chunk; ++i) {
+        int64_t n = 0;
+        for (const Piece &w : pieces) n += parts_of(w);
+        if (n * kv <= target || n == (int64_t)pieces.size()) break;
+        chunk = (chunk + chunk / 16 + unit) / unit * unit;
+    }
     for (const Piece &w : pieces) {
         const int units = (w.total + unit - 1) / unit;
-        const int parts = (int)std::min<int64_t>(units, (w.total + chunk - 1) / chunk);
+        const int parts = std::min(units, parts_of(w));
         for (int i = 0; i < parts; ++i) {
             spd_plan_item it;
             it.seq = w.seq;
@@ -52,11 +61,14 @@ void cut(const std::vector<Piece> &pieces, int kv, int target, int least, int un
             it.first = (int)((int64_t)i * units / parts) * unit;
             it.count = std::min((int)((int64_t)(i + 1) * units / parts) * unit, w.total) - it.first;
             it.slot = parts > 1 ? slots + i : -1;
-            it.pad = 0;
+            it.slot0 = slots;
+            it.parts = parts;
+            it.group = (int)merges.size();
+            it.pad[0] = it.pad[1] = 0;
             items.push_back(it);
         }
         if (parts > 1) {
-            merges.push_back(spd_plan_merge{w.seq, w.row0, w.rows, slots, parts, large});
+            merges.push_back(spd_plan_merge{w.seq, w.row0, w.rows, slots, parts, 0});
             slots += parts;
         }
     }
@@ -140,10 +152,17 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
             many.push_back(piece_of(P, b, seqs[b].pos, (int)r, (int)std::min<int64_t>(SPD_LARGE_ROWS, rows - r), window, sinks));
     }
     std::vector<spd_plan_item> small, large;
-    std::vector<spd_plan_merge> merges;
+    std::vector<spd_plan_merge> joined, merges;      // (the rows of the kernel for few are joined by the last of their items)
     int small_slots = 0, large_slots = 0;
-    cut(few, c.n_kv_heads, SMALL_TARGET, SMALL_MIN_BLOCKS, 2, 0, small, merges, small_slots);
-    cut(many, c.n_kv_heads, LARGE_TARGET, LARGE_MIN_BLOCKS, 4, 1, large, merges, large_slots);
+    const bool counted = (int64_t)few.size() * c.n_kv_heads <= SPD_COUNTERS;
+    // Rows whose blocks go round a workgroup's waves three times or less are not cut.  Beyond that a turn of a wave (a pair of blocks) takes
+    // about as long as 0.15 of the join of a part by one of `sets` sets of threads, which gives the number of parts that ends first when
+    // there is room for all of them.  (us a call, 0.05 / 0.1 / 0.3: 16 sequences of 4096 11.5 / 11.0 / 11.5, one of 32000 17.9 / 15.8 / 14.6; 64
+    // of 500: 6.8 uncut, 8.4 in two parts)
+    const int sets = P->group > 8 ? 1 : P->group > 4 ? 2 : P->group > 2 ? 4 : P->group > 1 ? 8 : 16;
+    auto most_small = [&](int blocks) { return blocks <= 3 * 2 * SPD_SMALL_WAVES ? 1 : (int)std::min(std::sqrt(0.15 * blocks * sets), blocks / 8.0); };
+    cut(few, c.n_kv_heads, counted ? SMALL_TARGET : 0, 2, most_small, small, joined, small_slots);
+    cut(many, c.n_kv_heads, LARGE_TARGET, 4, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, large, merges, large_slots);
     for (const spd_plan_merge &m : merges) h.merge_rows = std::max(h.merge_rows, m.rows);
 
     h.magic = SPD_PLAN_MAGIC;
@@ -167,8 +186,8 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
     at = (at + 15) & ~(size_t)15;
     if (at > 0x7fffffffull) return SPD_EINVAL;
     h.bytes = at;
-    h.part_small = 0;
-    h.part_large = spd_align256((size_t)small_slots * c.n_kv_heads * spd_part_floats(SPD_SMALL_ROWS, c.head_dim) * 4);
+    h.part_small = small_slots ? SPD_COUNTERS * 4 : 0;
+    h.part_large = h.part_small + spd_align256((size_t)small_slots * c.n_kv_heads * spd_part_floats(SPD_SMALL_ROWS, c.head_dim) * 4);
     h.workspace = h.part_large + spd_align256((size_t)large_slots * c.n_kv_heads * spd_part_floats(SPD_LARGE_ROWS, c.head_dim) * 4);
     *bytes = h.bytes;
     if (!plan_host) return SPD_OK;
