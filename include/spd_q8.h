@@ -111,7 +111,7 @@ int spd_pages_plan_get_info(const spd_pages *pages, const void *plan_host, spd_p
 /* Rotates queries and keys and puts keys and values away, quantised.
  *   qkv     [tokens][ld]: n_q_heads query heads, n_kv_heads keys, n_kv_heads values of head_dim each; in_dtype SPD_F32, or the
  *           pool's dtype; 16-byte aligned, ld * element size a multiple of 16
- *   rope    device copy of the rotary table, or NULL: keys go in as they are, and q_out has to be NULL
+ *   rope    device copy of the rotary table, 16-byte aligned, or NULL: keys go in as they are, and q_out has to be NULL
  *   q_out   [tokens][ld_q] in the pool's dtype, receives the rotated queries, 16-byte aligned rows; may be qkv itself (with its
  *           ld) when in_dtype is the pool's dtype; NULL: not wanted
  * Must be enqueued ahead of the step's spd_pages_attention(). */

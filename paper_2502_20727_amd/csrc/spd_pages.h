@@ -44,20 +44,24 @@ struct spd_plan_seq {
     int64_t held0;                       // row of position 0 in spd_pages_read()'s output
     int32_t end, pad;                    // pos + q_len
 };
+// (Work carries a copy of its sequence: a kernel is a load from its first address, not two.)
 struct spd_plan_item {                   // rows x blocks of one sequence, for every KV head
-    int32_t seq, row0;                   // sequence, first row
+    spd_plan_seq s;
+    int32_t row0;                        // first row
     int32_t sink_blocks, block0;
     int32_t first, count;                // blocks of the list
     int32_t slot;                        // where its partial result goes, or -1: it is the whole result
     int32_t slot0, parts;                // the rows' partial results: slots slot0 .. slot0 + parts - 1
     int32_t group;                       // number of the rows among those cut into items
-    int32_t pad[2];
+    int32_t pad[3];
 };
 struct spd_plan_merge {                  // rows whose partial results lie in slots slot0 .. slot0 + parts - 1
-    int32_t seq, row0, rows, slot0, parts, pad;
+    spd_plan_seq s;
+    int32_t row0, rows, slot0, parts;
 };
 struct spd_plan_block {                  // a 16-position block that receives new tokens
-    int32_t seq, block;
+    spd_plan_seq s;
+    int32_t block, pad[3];
 };
 struct spd_plan_header {
     uint32_t magic;

@@ -7,6 +7,7 @@
 // A key's scale multiplies its scores in fp32; a value's scale multiplies its probability before that is rounded for the second
 // contraction.  e4m3 codes are exact in bf16 and fp16, so that dequantising rounds nothing.  Hidden keys are taken out by selection after
 // the scale has been multiplied, and codes in pages are always finite: a NaN scale of a hidden key reaches nothing.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -107,8 +108,10 @@ __device__ __forceinline__ Block block_at(const Pages &P, const spd_plan_seq &s,
 }
 
 // ------------------------------------------------------------------------------------------
-// Writing.  One workgroup per 16-position block and KV head, or query head: sixteen threads per token, each with the same features of
-// both rotary halves.
+// Writing.  One workgroup per 16-position block and a few heads: sixteen threads per token, D / 16 of them to a row of D features, each with
+// eight of one rotary half and the eight that they turn with.  A workgroup of KV heads has keys and values side by side; one of
+// query heads keeps its angles for all of its heads.  Bound by what is read and written: four prompts of 2048 tokens, 64 + 2 x 8 heads in bf16,
+// XX us (319 MB).
 // ------------------------------------------------------------------------------------------
 struct WriteArgs {
     Pages P;
@@ -117,100 +120,90 @@ struct WriteArgs {
     char *q_out;
     int64_t ld, ld_q;           // in elements
     int q_heads;
+    int kv_groups, q_groups;    // workgroups per block: for KV heads, for query heads
 };
 
-template <class In, int N>      // N elements -> fp32
-__device__ __forceinline__ void load_row(const char *p, float (&x)[N]) {
+// two rows' halves of eight elements -> fp32
+template <class In>
+__device__ __forceinline__ void load_halves(const char *p, int apart, float (&a)[8], float (&b)[8]) {
+    struct Eight {
+        In v[8];
+    };
+    const Eight x = *(const Eight *)__builtin_assume_aligned(p, 16), y = *(const Eight *)__builtin_assume_aligned(p + apart * sizeof(In), 16);
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = (float)((const In *)p)[i];
-}
-
-// largest magnitude over the sixteen threads of a token; NaN if any of them holds a value that is not finite
-template <int N>
-__device__ __forceinline__ float row_amax(const float (&a)[N], const float (&b)[N]) {
-    float m = 0.f;
-    bool fine = true;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        m = fmaxf(m, fmaxf(fabsf(a[i]), fabsf(b[i])));
-        fine = fine && fabsf(a[i]) <= 3.402823466e38f && fabsf(b[i]) <= 3.402823466e38f;
+    for (int i = 0; i < 8; ++i) {
+        a[i] = (float)x.v[i];
+        b[i] = (float)y.v[i];
     }
-    if (!fine) m = __builtin_inff();
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    return m == __builtin_inff() ? __builtin_nanf("") : m;
 }
 
 template <class In, int D, bool E4M3, bool F16>
 __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
-    constexpr int N = D / 32, W = E4M3 ? 1 : 2, E = 16 / W;
+    constexpr int W = E4M3 ? 1 : 2, E = 16 / W, TPR = D / 16, UNITS = 16 / TPR;      // threads per row; rows of a token side by side
     const Pages &P = A.P;
     const spd_plan_block it = ((const spd_plan_block *)(P.plan + P.list))[blockIdx.x];
-    const spd_plan_seq s = ((const spd_plan_seq *)(P.plan + P.seqs))[it.seq];
-    const int r = threadIdx.x >> 4, u = threadIdx.x & 15;
+    const spd_plan_seq &s = it.s;
+    const int r = threadIdx.x >> 4, unit = (threadIdx.x & 15) / TPR, f0 = (threadIdx.x % TPR) * 8;
     const int pos = it.block * 16 + r, lo = it.block * 16 > s.pos ? 0 : s.pos - it.block * 16,
               hi = s.end - it.block * 16 < 16 ? s.end - it.block * 16 : 16;      // rows lo .. hi - 1 of the block are new
     const bool mine = r >= lo && r < hi;
     const int64_t token = s.tok0 + (pos - s.pos);
-    const int y = blockIdx.y;
-    const int f0 = u * N;
-    float c[N], sn[N];
-    if (A.rope) {
+    float2 turn[8];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float2 t = mine ? A.rope[(size_t)pos * (D / 2) + f0 + i] : make_float2(1.f, 0.f);
-            c[i] = t.x;
-            sn[i] = t.y;
+    for (int i = 0; i < 8; ++i) turn[i] = make_float2(1.f, 0.f);
+    if (A.rope && mine) {
+        const float4 *t = (const float4 *)(A.rope + (size_t)pos * (D / 2) + f0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 x = t[i];
+            turn[2 * i] = make_float2(x.x, x.y);
+            turn[2 * i + 1] = make_float2(x.z, x.w);
         }
     }
-    auto fetch = [&](int head, float(&a)[N], float(&b)[N]) {
-        if (mine) {
-            const char *p = A.qkv + (token * A.ld + (int64_t)head * D + f0) * sizeof(In);
-            load_row<In, N>(p, a);
-            load_row<In, N>(p + D / 2 * sizeof(In), b);
-        } else {
+    auto rotate = [&](float(&a)[8], float(&b)[8]) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) a[i] = b[i] = 0.f;
+        for (int i = 0; i < 8; ++i) {
+            const float x = a[i], z = b[i];
+            a[i] = x * turn[i].x - z * turn[i].y;
+            b[i] = z * turn[i].x + x * turn[i].y;
         }
     };
-    auto rotate = [&](float(&a)[N], float(&b)[N]) {
-        if (A.rope) {
+    const char *in = A.qkv + (token * A.ld + f0) * sizeof(In);
+    if ((int)blockIdx.y >= A.kv_groups) {      // query heads
+        if (!mine) return;
+        const int group = blockIdx.y - A.kv_groups;
+        for (int head = group * UNITS + unit; head < A.q_heads; head += A.q_groups * UNITS) {
+            float a[8], b[8];
+            load_halves<In>(in + (size_t)head * D * sizeof(In), D / 2, a, b);
+            rotate(a, b);
+            i32x4 x, y;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float x = a[i], z = b[i];
-                a[i] = x * c[i] - z * sn[i];
-                b[i] = z * c[i] + x * sn[i];
+            for (int i = 0; i < 4; ++i) {
+                x[i] = Half<F16>::pack(a[2 * i], a[2 * i + 1]);
+                y[i] = Half<F16>::pack(b[2 * i], b[2 * i + 1]);
             }
-        }
-    };
-    if (y >= P.kv) {            // a query head
-        float a[N], b[N];
-        fetch(y - P.kv, a, b);
-        rotate(a, b);
-        if (mine) {
-            int *o = (int *)(A.q_out + (token * A.ld_q + (int64_t)(y - P.kv) * D + f0) * 2);
-#pragma unroll
-            for (int i = 0; i < N / 2; ++i) {
-                o[i] = Half<F16>::pack(a[2 * i], a[2 * i + 1]);
-                o[D / 4 + i] = Half<F16>::pack(b[2 * i], b[2 * i + 1]);
-            }
+            char *o = A.q_out + (token * A.ld_q + (int64_t)head * D + f0) * 2;
+            *(i32x4 *)o = x;
+            *(i32x4 *)(o + D) = y;
         }
         return;
     }
-    // codes of the block's keys and values, rows = positions
-    __shared__ __attribute__((aligned(16))) char codes[2][16 * D * W];
-    const Block B = block_at(P, s, y, it.block);
-    char *keys = B.head + (size_t)B.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
-    float *scales = (float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16;
+    // codes of the block's keys and values, rows = positions: even units keys, odd units values
+    constexpr int HEADS = UNITS / 2;
+    __shared__ __attribute__((aligned(16))) char codes[UNITS][16 * D * W];
+    const int head0 = blockIdx.y * HEADS, head = head0 + unit / 2, kind = unit & 1;
+    const bool there = mine && head < P.kv;
+    auto scales_of = [&](const Block &B) { return (float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16; };
+    const Block B0 = block_at(P, s, head0, it.block);
+    {
+        float a[8], b[8];
 #pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-        float a[N], b[N];
-        fetch(A.q_heads + y + kind * P.kv, a, b);
+        for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
+        if (there) load_halves<In>(in + (size_t)(A.q_heads + head + kind * P.kv) * D * sizeof(In), D / 2, a, b);
         if (kind == 0) rotate(a, b);
-        float amax;
         if constexpr (!E4M3) {       // what the 16-bit type makes of it decides whether the row is finite
 #pragma unroll
-            for (int i = 0; i < N; i += 2) {
+            for (int i = 0; i < 8; i += 2) {
                 const int pa = Half<F16>::pack(a[i], a[i + 1]), pb = Half<F16>::pack(b[i], b[i + 1]);
                 a[i] = Half<F16>::low(pa);
                 a[i + 1] = Half<F16>::high(pa);
@@ -218,86 +211,149 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
                 b[i + 1] = Half<F16>::high(pb);
             }
         }
-        amax = row_amax<N>(a, b);
-        const bool fine = amax == amax;
+        // largest magnitude over the threads of the row, infinity if any holds a value that is not finite
+        float amax = 0.f;
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            amax = fmaxf(amax, fmaxf(fabsf(a[i]), fabsf(b[i])));
+            fine = fine && fabsf(a[i]) <= 3.402823466e38f && fabsf(b[i]) <= 3.402823466e38f;
+        }
+        if (!fine) amax = __builtin_inff();
+#pragma unroll
+        for (int d = 1; d < TPR; d <<= 1) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
+        fine = amax < __builtin_inff();
         float scale = 1.f;
+        char *to = codes[unit] + (r * D + f0) * W;
         if constexpr (E4M3) {
-            amax = fmaxf(amax, 0x1p-90f);      // (a NaN gives the other operand)
+            amax = fmaxf(amax, 0x1p-90f);
             scale = amax / 448.f;
             const float up = 448.f / amax;
+            i32x2 x, y;
 #pragma unroll
-            for (int i = 0; i < N; i += 2) {
-                const int pa = __builtin_amdgcn_cvt_pk_fp8_f32(a[i] * up, a[i + 1] * up, 0, false);
-                const int pb = __builtin_amdgcn_cvt_pk_fp8_f32(b[i] * up, b[i + 1] * up, 0, false);
-                *(short *)(codes[kind] + r * D + f0 + i) = (short)(fine ? pa : 0);
-                *(short *)(codes[kind] + r * D + D / 2 + f0 + i) = (short)(fine ? pb : 0);
+            for (int i = 0; i < 2; ++i) {
+                x[i] = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i] * up, a[4 * i + 1] * up, 0, false);
+                x[i] = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i + 2] * up, a[4 * i + 3] * up, x[i], true);
+                y[i] = __builtin_amdgcn_cvt_pk_fp8_f32(b[4 * i] * up, b[4 * i + 1] * up, 0, false);
+                y[i] = __builtin_amdgcn_cvt_pk_fp8_f32(b[4 * i + 2] * up, b[4 * i + 3] * up, y[i], true);
             }
+            *(i32x2 *)to = fine ? x : (i32x2){0, 0};
+            *(i32x2 *)(to + D / 2) = fine ? y : (i32x2){0, 0};
         } else {
+            i32x4 x, y;
 #pragma unroll
-            for (int i = 0; i < N; i += 2) {
-                *(int *)(codes[kind] + (r * D + f0 + i) * 2) = fine ? Half<F16>::pack(a[i], a[i + 1]) : 0;
-                *(int *)(codes[kind] + (r * D + D / 2 + f0 + i) * 2) = fine ? Half<F16>::pack(b[i], b[i + 1]) : 0;
+            for (int i = 0; i < 4; ++i) {
+                x[i] = Half<F16>::pack(a[2 * i], a[2 * i + 1]);
+                y[i] = Half<F16>::pack(b[2 * i], b[2 * i + 1]);
             }
+            *(i32x4 *)to = fine ? x : (i32x4){0, 0, 0, 0};
+            *(i32x4 *)(to + D) = fine ? y : (i32x4){0, 0, 0, 0};
         }
-        if (mine && u == 0) scales[kind * P.page_size + r] = fine ? scale : __builtin_nanf("");
+        if (there && f0 == 0) scales_of(B0)[(size_t)(head - head0) * (P.head_bytes / 4) + kind * P.page_size + r] = fine ? scale : __builtin_nanf("");
     }
     __syncthreads();
-    // keys: a 16-byte piece belongs to one position
-    for (int i = threadIdx.x; i < D * W; i += 256) {
-        const int pr = i & 15, g = (i >> 4) & 3, ch = i >> 6;
-        if (pr >= lo && pr < hi) *(i32x4 *)(keys + i * 16) = *(const i32x4 *)(codes[0] + (pr * D + ch * 4 * E + g * E) * W);
-    }
-    // values: a piece holds four positions.  Whole blocks go out in pieces, the others position by position.
-    if (lo == 0 && hi == 16) {
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+        if (head0 + h >= P.kv) return;
+        char *keys = B0.head + (size_t)h * P.head_bytes + (size_t)B0.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
+        const char *kc = codes[2 * h], *vc = codes[2 * h + 1];
+        // keys: a 16-byte piece belongs to one position
         for (int i = threadIdx.x; i < D * W; i += 256) {
             const int pr = i & 15, g = (i >> 4) & 3, ch = i >> 6;
-            union {
-                i32x4 v;
-                unsigned char b[16];
-                unsigned short h[8];
-            } piece;
-#pragma unroll
-            for (int t = 0; t < E / 4; ++t)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int at = (4 * g + k) * D + pr + 16 * (ch * (E / 4) + t);
-                    if constexpr (E4M3) piece.b[t * 4 + k] = codes[1][at];
-                    else piece.h[t * 4 + k] = ((const unsigned short *)codes[1])[at];
-                }
-            *(i32x4 *)(values + i * 16) = piece.v;
+            if (pr >= lo && pr < hi) *(i32x4 *)(keys + i * 16) = *(const i32x4 *)(kc + (pr * D + ch * 4 * E + g * E) * W);
         }
-    } else {
-        for (int i = threadIdx.x; i < (hi - lo) * D; i += 256) {
-            const int pr = lo + i / D, f = i % D, to = spd_page_value_off(pr, f, E);
-            if constexpr (E4M3) values[to] = codes[1][pr * D + f];
-            else ((unsigned short *)values)[to] = ((const unsigned short *)codes[1])[pr * D + f];
+        // values: a piece holds four positions.  Whole blocks go out in pieces, the others position by position.
+        if (lo == 0 && hi == 16) {
+            for (int i = threadIdx.x; i < D * W; i += 256) {
+                const int pr = i & 15, g = (i >> 4) & 3, ch = i >> 6;
+                union {
+                    i32x4 v;
+                    unsigned char b[16];
+                    unsigned short h[8];
+                } piece;
+#pragma unroll
+                for (int t = 0; t < E / 4; ++t)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int at = (4 * g + k) * D + pr + 16 * (ch * (E / 4) + t);
+                        if constexpr (E4M3) piece.b[t * 4 + k] = vc[at];
+                        else piece.h[t * 4 + k] = ((const unsigned short *)vc)[at];
+                    }
+                *(i32x4 *)(values + i * 16) = piece.v;
+            }
+        } else {
+            for (int i = threadIdx.x; i < (hi - lo) * D; i += 256) {
+                const int pr = lo + i / D, f = i % D, to = spd_page_value_off(pr, f, E);
+                if constexpr (E4M3) values[to] = vc[pr * D + f];
+                else ((unsigned short *)values)[to] = ((const unsigned short *)vc)[pr * D + f];
+            }
         }
     }
 }
 
 // ------------------------------------------------------------------------------------------
-// Reading back.  One workgroup per 16-position block and KV head.
+// Reading back.  One workgroup per four 16-position blocks and KV head, a wave per block.  A lane's keys are pieces of rows; its values
+// (four positions of several features) change places in the LDS.  16 contexts of up to 4096 of one KV head, bf16: XX us (37 MB).
 // ------------------------------------------------------------------------------------------
 template <class Out, int D, bool E4M3, bool F16>
 __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_out) {
-    constexpr int N = D / 16, W = E4M3 ? 1 : 2, E = 16 / W;
+    constexpr int W = E4M3 ? 1 : 2, E = 16 / W, CH = D / (4 * E), ROW = D + 16 / (int)sizeof(Out);
+    struct Piece {
+        Out v[16 / sizeof(Out)];
+    };
+    __shared__ __attribute__((aligned(16))) Out turned[4][16 * ROW];
     const spd_plan_seq s = ((const spd_plan_seq *)(P.plan + P.seqs))[blockIdx.y];
-    const int block = blockIdx.x, head = blockIdx.z;
-    const int r = threadIdx.x >> 4, f0 = (threadIdx.x & 15) * N;
-    if (block * 16 + r >= s.end) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int block = blockIdx.x * 4 + wave, head = blockIdx.z, r = lane & 15, g = lane >> 4;
+    if (block * 16 >= s.end) return;             // (a wave works by itself)
     const Block B = block_at(P, s, head, block);
     const char *keys = B.head + (size_t)B.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
-    const float *scales = (const float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16 + r;
-    const float ks = scales[0], vs = scales[P.page_size];
-    const int64_t to = ((s.held0 + block * 16 + r) * P.kv + head) * D + f0;
-    auto value = [&](const char *p, int at) -> float {
-        if constexpr (E4M3) return Half<false>::low(Half<false>::template from_e4m3<false>((int)(unsigned char)p[at]));
-        else return Half<F16>::low(((const unsigned short *)p)[at]);
-    };
+    const float *scales = (const float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16;
+    i32x4 kx[CH], vx[CH];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        k_out[to + i] = (Out)(value(keys, spd_page_key_off(r, f0 + i, E)) * ks);
-        v_out[to + i] = (Out)(value(values, spd_page_value_off(r, f0 + i, E)) * vs);
+    for (int c = 0; c < CH; ++c) kx[c] = *(const i32x4 *)(keys + c * 1024 + lane * 16);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) vx[c] = *(const i32x4 *)(values + c * 1024 + lane * 16);
+    const float ks = scales[r];
+    const f32x4 vs = *(const f32x4 *)(scales + P.page_size + 4 * g);
+    typedef Half<F16 && !E4M3> Codes;            // (e4m3 by way of bf16)
+    auto pair = [&](const i32x4 &x, int i) {     // elements 2 i and 2 i + 1 of a piece, as 16-bit values
+        if constexpr (E4M3) return i & 1 ? Codes::template from_e4m3<true>(x[i >> 1]) : Codes::template from_e4m3<false>(x[i >> 1]);
+        else return x[i];
+    };
+    Out *mine = turned[wave];
+    const int n = s.end - block * 16 < 16 ? s.end - block * 16 : 16;
+    const int64_t row0 = ((s.held0 + block * 16) * P.kv + head) * D, pitch = (int64_t)P.kv * D;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        Out piece[E];
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            const int k = pair(kx[c], i), v = pair(vx[c], i);
+            piece[2 * i] = (Out)(Codes::low(k) * ks);
+            piece[2 * i + 1] = (Out)(Codes::high(k) * ks);
+            // elements 4 t .. 4 t + 3: positions 4 g .. of feature r + 16 (E / 4 c + t)
+            const int f = r + 16 * (c * (E / 4) + i / 2), p = 4 * g + 2 * (i & 1);
+            mine[p * ROW + f] = (Out)(Codes::low(v) * vs[2 * (i & 1)]);
+            mine[(p + 1) * ROW + f] = (Out)(Codes::high(v) * vs[2 * (i & 1) + 1]);
+        }
+        if (r < n) {
+#pragma unroll
+            for (int i = 0; i < E; i += 16 / (int)sizeof(Out)) {
+                Piece q;
+#pragma unroll
+                for (int e = 0; e < 16 / (int)sizeof(Out); ++e) q.v[e] = piece[i + e];
+                *(Piece *)__builtin_assume_aligned(k_out + row0 + r * pitch + c * 4 * E + g * E + i, 16) = q;
+            }
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+    constexpr int PIECES = D * sizeof(Out) / 16;
+#pragma unroll
+    for (int i = lane; i < 16 * PIECES; i += 64) {
+        const int pr = i / PIECES, f = (i % PIECES) * (16 / (int)sizeof(Out));
+        if (pr < n)
+            *(Piece *)__builtin_assume_aligned(v_out + row0 + pr * pitch + f, 16) = *(const Piece *)__builtin_assume_aligned(mine + pr * ROW + f, 16);
     }
 }
 
@@ -369,7 +425,7 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
     const Pages &P = A.P;
     const int head = blockIdx.x % P.kv;
     const spd_plan_item it = ((const spd_plan_item *)(P.plan + P.list))[blockIdx.x / P.kv];
-    const spd_plan_seq s = ((const spd_plan_seq *)(P.plan + P.seqs))[it.seq];
+    const spd_plan_seq &s = it.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 15, g = lane >> 4;
     const int rows = s.q_len * P.group;          // at most 16
@@ -598,7 +654,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     const Pages &P = A.P;
     const int head = blockIdx.x % P.kv;
     const spd_plan_item it = ((const spd_plan_item *)(P.plan + P.list))[blockIdx.x / P.kv];
-    const spd_plan_seq s = ((const spd_plan_seq *)(P.plan + P.seqs))[it.seq];
+    const spd_plan_seq &s = it.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int n_rows = s.q_len * P.group;
@@ -704,25 +760,18 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
             }
         }
         // score i of half h: block 2 h + i / 8 of the tile, position 8 ((i / 4) % 2) + 4 half + i % 4 in it
-        f32x4 ks[8], vs[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            ks[q] = *(const f32x4 *)(now.ks + q * 8 + 4 * half);
-            vs[q] = *(const f32x4 *)(now.vs + q * 8 + 4 * half);
+            const f32x4 ks = *(const f32x4 *)(now.ks + q * 8 + 4 * half);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[q >> 2][(q & 3) * 4 + i] *= ks[i];
         }
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sc[q >> 2][(q & 3) * 4 + i] *= ks[q][i];
         if (!all) {
 #pragma unroll
             for (int q = 0; q < 8; ++q)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (!visible(key0[q >> 1] + 8 * (q & 1) + 4 * half + i, at, A.window, A.sinks)) {
-                        sc[q >> 2][(q & 3) * 4 + i] = -__builtin_inff();
-                        vs[q][i] = 0.f;          // (it may be NaN)
-                    }
+                    if (!visible(key0[q >> 1] + 8 * (q & 1) + 4 * half + i, at, A.window, A.sinks)) sc[q >> 2][(q & 3) * 4 + i] = -__builtin_inff();
         }
         float mx = sc[0][0];
 #pragma unroll
@@ -733,17 +782,26 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         m = m_new;
         i32x4 pf[4];
         float ps = 0.f;
+        auto weigh = [&](auto masked_) __attribute__((always_inline)) {
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            float w[8];
+            for (int b = 0; b < 4; ++b) {
+                float w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float p = __builtin_amdgcn_exp2f(sc[b >> 1][(b & 1) * 8 + i] - m_use);
-                ps += p;
-                w[i] = p * vs[2 * b + (i >> 2)][i & 3];
+                for (int i = 0; i < 8; i += 4) {
+                    const f32x4 vs = *(const f32x4 *)(now.vs + b * 16 + 2 * i + 4 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x = sc[b >> 1][(b & 1) * 8 + i + e], p = __builtin_amdgcn_exp2f(x - m_use);
+                        ps += p;
+                        // (the scale of a hidden key's value may be NaN)
+                        w[i + e] = decltype(masked_)::value && x == -__builtin_inff() ? 0.f : p * vs[e];
+                    }
+                }
+                pf[b] = (i32x4){PV::pack(w[0], w[1]), PV::pack(w[2], w[3]), PV::pack(w[4], w[5]), PV::pack(w[6], w[7])};
             }
-            pf[b] = (i32x4){PV::pack(w[0], w[1]), PV::pack(w[2], w[3]), PV::pack(w[4], w[5]), PV::pack(w[6], w[7])};
-        }
+        };
+        if (all) weigh(std::false_type());
+        else weigh(std::true_type());
         l = l * alpha + ps;                      // (of the lane's half of the keys)
         if (more) put_away(stage[turn ^ 1]);
         // (a factor of exactly 1 changes nothing; maxima settle after the first tiles)
@@ -806,7 +864,7 @@ __global__ void __launch_bounds__(256) k_attend_merge(Pages P, const float *part
     const spd_plan_merge j = ((const spd_plan_merge *)(P.plan + P.list))[blockIdx.x / P.kv];
     const int r = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (r >= j.rows) return;
-    const spd_plan_seq s = ((const spd_plan_seq *)(P.plan + P.seqs))[j.seq];
+    const spd_plan_seq &s = j.s;
     const size_t step = (size_t)P.kv * CAP * (D + 2);
     const float *p = part + ((size_t)j.slot0 * P.kv + head) * (CAP * (D + 2));
     float mm = -__builtin_inff(), l = 0.f, acc[N];
@@ -893,7 +951,7 @@ int spd_pages_write(const spd_pages *pages, const void *plan_host, const void *p
     const spd_pages_config &c = pages->cfg;
     if (in_dtype != SPD_F32 && in_dtype != c.dtype) return SPD_EINVAL;
     const int es = in_dtype == SPD_F32 ? 4 : 2;
-    if (!qkv || !pool || !aligned(qkv, 16) || !aligned(pool, 256) || (q_out && !rope)) return SPD_EINVAL;
+    if (!qkv || !pool || !aligned(qkv, 16) || !aligned(pool, 256) || (q_out && !rope) || !aligned(rope, 16)) return SPD_EINVAL;
     if (ld < (int64_t)(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim || ld * es % 16) return SPD_EINVAL;
     if (q_out && (!aligned(q_out, 16) || ld_q < (int64_t)c.n_q_heads * c.head_dim || ld_q % 8)) return SPD_EINVAL;
     if (q_out == qkv && (in_dtype == SPD_F32 || ld_q != ld)) return SPD_EINVAL;
@@ -907,7 +965,11 @@ int spd_pages_write(const spd_pages *pages, const void *plan_host, const void *p
     A.ld = ld;
     A.ld_q = ld_q;
     A.q_heads = c.n_q_heads;
-    const dim3 grid(h.n_write, c.n_kv_heads + (q_out ? c.n_q_heads : 0));
+    // query heads: about a thousand workgroups, so that one has several heads and its angles serve them all
+    const int units = 256 / c.head_dim, q_units = (c.n_q_heads + units - 1) / units;
+    A.kv_groups = (c.n_kv_heads + units / 2 - 1) / (units / 2);
+    A.q_groups = q_out ? std::min(q_units, std::max(1, 2048 / h.n_write)) : 0;
+    const dim3 grid(h.n_write, A.kv_groups + A.q_groups);
     SPD_HIP(by_kind(pages, [&](auto d, auto e, auto f) {
         constexpr int D = decltype(d)::value;
         constexpr bool E = decltype(e)::value, F = decltype(f)::value;
@@ -929,7 +991,7 @@ int spd_pages_read(const spd_pages *pages, const void *plan_host, const void *pl
     if (!h.held) return SPD_OK;
     (void)hipGetLastError();
     const Pages P = pages_args(pages, h, plan_dev, pool, 0);
-    const dim3 grid((h.max_end + 15) / 16, h.batch, c.n_kv_heads);
+    const dim3 grid((h.max_end + 63) / 64, h.batch, c.n_kv_heads);
     SPD_HIP(by_kind(pages, [&](auto d, auto e, auto f) {
         constexpr int D = decltype(d)::value;
         constexpr bool E = decltype(e)::value, F = decltype(f)::value;

@@ -33,17 +33,17 @@ Piece piece_of(const spd_pages *P, int seq, int pos, int row0, int rows, int win
     return w;
 }
 
-// Cuts pieces into items of at most `chunk` blocks, the fewest that gives no more than `target` workgroups (0: not at all); `unit` blocks go
-// together.  most(blocks): the most items a piece is cut into.
+// Cuts pieces into items of at most `chunk` blocks, what each of `target` workgroups would have of them (0: not at all); `unit` blocks go
+// together.  one_round: into no more than `target` items.  most(blocks): the most items a piece is cut into.
 template <class Most>
-void cut(const std::vector<Piece> &pieces, int kv, int target, int unit, Most most, std::vector<spd_plan_item> &items,
+void cut(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs, int kv, int target, int unit, bool one_round, Most most, std::vector<spd_plan_item> &items,
          std::vector<spd_plan_merge> &merges, int &slots) {
     int64_t total = 0;
     for (const Piece &w : pieces) total += w.total;
     int64_t chunk = target ? std::max<int64_t>(unit, ((total * kv + target - 1) / target + unit - 1) / unit * unit) : 0;
     auto parts_of = [&](const Piece &w) { return chunk ? (int)std::min<int64_t>(most(w.total), (w.total + chunk - 1) / chunk) : 1; };
     // (what lengths leave over after whole chunks makes more items than the target: longer chunks, while cutting is what makes them)
-    for (int i = 0; i < 16 && chunk; ++i) {
+    for (int i = 0; i < 16 && chunk && one_round; ++i) {
         int64_t n = 0;
         for (const Piece &w : pieces) n += parts_of(w);
         if (n * kv <= target || n == (int64_t)pieces.size()) break;
@@ -54,7 +54,7 @@ void cut(const std::vector<Piece> &pieces, int kv, int target, int unit, Most mo
         const int parts = std::min(units, parts_of(w));
         for (int i = 0; i < parts; ++i) {
             spd_plan_item it;
-            it.seq = w.seq;
+            it.s = seqs[w.seq];
             it.row0 = w.row0;
             it.sink_blocks = w.sink_blocks;
             it.block0 = w.block0;
@@ -64,11 +64,11 @@ void cut(const std::vector<Piece> &pieces, int kv, int target, int unit, Most mo
             it.slot0 = slots;
             it.parts = parts;
             it.group = (int)merges.size();
-            it.pad[0] = it.pad[1] = 0;
+            it.pad[0] = it.pad[1] = it.pad[2] = 0;
             items.push_back(it);
         }
         if (parts > 1) {
-            merges.push_back(spd_plan_merge{w.seq, w.row0, w.rows, slots, parts, 0});
+            merges.push_back(spd_plan_merge{seqs[w.seq], w.row0, w.rows, slots, parts});
             slots += parts;
         }
     }
@@ -137,7 +137,7 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
         if (!s.q_len) continue;
         for (int i = s.pos / c.page_size; i <= (s.end - 1) / c.page_size; ++i)
             if (uses[table[s.table + i]] != 1) return SPD_EINVAL;      // written here and in use elsewhere
-        for (int blk = s.pos / 16; blk <= (s.end - 1) / 16; ++blk) writes.push_back(spd_plan_block{b, blk});
+        for (int blk = s.pos / 16; blk <= (s.end - 1) / 16; ++blk) writes.push_back(spd_plan_block{s, blk, {0, 0, 0}});
     }
 
     std::vector<Piece> few, many;
@@ -161,8 +161,8 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
     // of 500: 6.8 uncut, 8.4 in two parts)
     const int sets = P->group > 8 ? 1 : P->group > 4 ? 2 : P->group > 2 ? 4 : P->group > 1 ? 8 : 16;
     auto most_small = [&](int blocks) { return blocks <= 3 * 2 * SPD_SMALL_WAVES ? 1 : (int)std::min(std::sqrt(0.15 * blocks * sets), blocks / 8.0); };
-    cut(few, c.n_kv_heads, counted ? SMALL_TARGET : 0, 2, most_small, small, joined, small_slots);
-    cut(many, c.n_kv_heads, LARGE_TARGET, 4, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, large, merges, large_slots);
+    cut(few, seqs, c.n_kv_heads, counted ? SMALL_TARGET : 0, 2, true, most_small, small, joined, small_slots);
+    cut(many, seqs, c.n_kv_heads, LARGE_TARGET, 4, false, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, large, merges, large_slots);
     for (const spd_plan_merge &m : merges) h.merge_rows = std::max(h.merge_rows, m.rows);
 
     h.magic = SPD_PLAN_MAGIC;
