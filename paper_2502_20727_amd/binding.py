@@ -551,9 +551,10 @@ def _rows(t, rows: int, cols: int, what: str):
     """(address, row stride) of a device matrix whose rows are contiguous; (None, 0) for None."""
     if t is None:
         return None, 0
-    if t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a [{rows}, {cols}] matrix with contiguous rows wanted, not {tuple(t.shape)} with strides {t.stride()}")
-    ld = t.stride(0)
+    strides = t.stride()
+    if t.shape != (rows, cols) or (cols > 1 and strides[1] != 1):
+        raise ValueError(f"{what}: a [{rows}, {cols}] matrix with contiguous rows wanted, not {tuple(t.shape)} with strides {strides}")
+    ld = strides[0]
     return t.data_ptr(), (ld if ld >= cols or rows > 1 else cols)
 
 

@@ -733,16 +733,11 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
             fetch(v0 + 4, page);
             page = page_of(P, s, my_block(v0 + 8));
         }
-        // which of the tile's blocks the wave's queries see: all of a block, some, or none
-        bool all = v0 + 4 <= it.count, any = false;
-        int key0[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int block = v0 + b < it.count ? list_block(it, it.first + v0 + b) : 0x7fffff;
-            key0[b] = block * 16;
-            all = all && all_visible(block, first_at, last_at, A.window, A.sinks);
-            any = any || (key0[b] <= last_at && (A.window == 0 || key0[b] + 15 > first_at - A.window || key0[b] < A.sinks));
-        }
+        // does every query of the wave see all of the tile?  Does any see some of it?  (first and last block; a tile of sinks and window blocks is mixed)
+        const int n_here = it.count - v0 < 4 ? it.count - v0 : 4;
+        const int b_first = list_block(it, it.first + v0), b_last = list_block(it, it.first + v0 + n_here - 1);
+        const bool all = n_here == 4 && b_last * 16 + 15 <= first_at && (A.window == 0 || b_first * 16 > last_at - A.window || b_last * 16 + 15 < A.sinks);
+        const bool any = b_first * 16 <= last_at && (A.window == 0 || b_last * 16 + 15 > first_at - A.window || b_first * 16 < A.sinks);
         if (!any) {                              // (the wave's rows lie before the tile, or past its window)
             if (more) put_away(stage[turn ^ 1]);
             __syncthreads();
@@ -768,16 +763,20 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         }
         if (!all) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
+            for (int q = 0; q < 8; ++q) {
+                const int key0 = (q >> 1) < n_here ? list_block(it, it.first + v0 + (q >> 1)) * 16 : 0x7fffff0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (!visible(key0[q >> 1] + 8 * (q & 1) + 4 * half + i, at, A.window, A.sinks)) sc[q >> 2][(q & 3) * 4 + i] = -__builtin_inff();
+                    if (!visible(key0 + 8 * (q & 1) + 4 * half + i, at, A.window, A.sinks)) sc[q >> 2][(q & 3) * 4 + i] = -__builtin_inff();
+            }
         }
         float mx = sc[0][0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(m, mx), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+        // The maximum only keeps the powers of two in range: one that has grown by less than 2^8 stays, and the outputs with it.
+        const bool grown = __builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0;
+        const float m_new = grown ? fmaxf(m, mx) : m, m_use = m_new == -__builtin_inff() ? 0.f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(m - m_use);
         m = m_new;
         i32x4 pf[4];
@@ -804,8 +803,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         else weigh(std::true_type());
         l = l * alpha + ps;                      // (of the lane's half of the keys)
         if (more) put_away(stage[turn ^ 1]);
-        // (a factor of exactly 1 changes nothing; maxima settle after the first tiles)
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+        if (grown) {
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -841,44 +839,49 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
                 *(i32x4 *)(A.out + (int64_t)(s.tok0 + pr / P.group) * A.ld_out + (int64_t)(head * P.group + pr % P.group) * D + c) =
                     *(const i32x4 *)(mine + (p / PIECES) * ROW + c);
         }
-    } else if (live) {
+    } else {
+        // as it lies in the registers: [wave][32 features][4][lane][4], then the rows' maxima and sums
         float *to = A.part + ((size_t)it.slot * P.kv + head) * (SPD_LARGE_ROWS * (D + 2));
-        const int pr = wave * 32 + col;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *(f32x4 *)(to + pr * D + 32 * t + 2 * i + 4 * half) = (f32x4){o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+            for (int q = 0; q < 4; ++q)
+                *(f32x4 *)(to + ((wave * DT + t) * 4 + q) * 256 + lane * 4) = (f32x4){o[t][4 * q], o[t][4 * q + 1], o[t][4 * q + 2], o[t][4 * q + 3]};
         if (half == 0) {
-            to[SPD_LARGE_ROWS * D + pr] = m;
-            to[SPD_LARGE_ROWS * D + SPD_LARGE_ROWS + pr] = l;
+            to[SPD_LARGE_ROWS * D + wave * 32 + col] = m;
+            to[SPD_LARGE_ROWS * D + SPD_LARGE_ROWS + wave * 32 + col] = l;
         }
     }
 }
 
-// Joins the partial results of a chunk's rows whose blocks were cut into several items: a wave per row, in the order of the items.
+// Joins the partial results of a chunk's rows whose blocks were cut into several items, in the order of the items: a workgroup per 32 rows and KV
+// head (a wave's rows in the kernel that wrote them), a wave per 32 features.  Lane = 32 half + row, as they were written.
 template <int D, bool F16>
-__global__ void __launch_bounds__(256) k_attend_merge(Pages P, const float *part, unsigned short *out, int64_t ld_out) {
-    constexpr int N = D / 64, CAP = SPD_LARGE_ROWS, NB = 8;      // NB: parts asked for at a time
+__global__ void __launch_bounds__(2 * D) k_attend_merge(Pages P, const float *part, unsigned short *out, int64_t ld_out) {
+    constexpr int DT = D / 32, CAP = SPD_LARGE_ROWS, NB = 8, ROW = D + 8;      // NB: parts asked for at a time
     const int head = blockIdx.x % P.kv;
     const spd_plan_merge j = ((const spd_plan_merge *)(P.plan + P.list))[blockIdx.x / P.kv];
-    const int r = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (r >= j.rows) return;
+    const int lane = threadIdx.x & 63, t = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int r0 = blockIdx.y * 32;
+    if (r0 >= j.rows) return;                    // (whole workgroup)
     const spd_plan_seq &s = j.s;
     const size_t step = (size_t)P.kv * CAP * (D + 2);
     const float *p = part + ((size_t)j.slot0 * P.kv + head) * (CAP * (D + 2));
-    float mm = -__builtin_inff(), l = 0.f, acc[N];
+    const float *po = p + (size_t)(blockIdx.y * DT + t) * 1024 + lane * 4, *pm = p + CAP * D + r0 + col;
+    float mm = -__builtin_inff(), l = 0.f;
+    f32x4 acc[4];
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+    for (int q = 0; q < 4; ++q) acc[q] = (f32x4){0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 < j.parts; i0 += NB) {
-        float m[NB], sum[NB], x[NB][N];
+        float m[NB], sum[NB];
+        f32x4 x[NB][4];
 #pragma unroll
         for (int u = 0; u < NB; ++u) {
-            const float *q = p + (size_t)(i0 + u < j.parts ? i0 + u : j.parts - 1) * step;
-            m[u] = q[CAP * D + r];
-            sum[u] = q[CAP * D + CAP + r];
+            const size_t at = (size_t)(i0 + u < j.parts ? i0 + u : j.parts - 1) * step;
+            m[u] = pm[at];
+            sum[u] = pm[at + CAP];
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[u][e] = q[(size_t)r * D + lane * N + e];
+            for (int q = 0; q < 4; ++q) x[u][q] = *(const f32x4 *)(po + at + q * 256);
         }
 #pragma unroll
         for (int u = 0; u < NB; ++u) {
@@ -888,14 +891,24 @@ __global__ void __launch_bounds__(256) k_attend_merge(Pages P, const float *part
             mm = m_new;
             l = l * fa + sum[u] * fb;
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] = acc[e] * fa + x[u][e] * fb;
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[q][e] = acc[q][e] * fa + x[u][q][e] * fb;
         }
     }
-    const int row = j.row0 + r;
-    unsigned short *to = out + (int64_t)(s.tok0 + row / P.group) * ld_out + (int64_t)(head * P.group + row % P.group) * D + lane * N;
+    __shared__ __attribute__((aligned(16))) short rows[32 * ROW];
     const float inv = 1.f / l;
-    if constexpr (N == 2) *(int *)to = Half<F16>::pack(acc[0] * inv, acc[1] * inv);
-    else *to = (unsigned short)Half<F16>::pack(acc[0] * inv, 0.f);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *(i32x2 *)(rows + col * ROW + 32 * t + 8 * q + 4 * half) =
+            (i32x2){Half<F16>::pack(acc[q][0] * inv, acc[q][1] * inv), Half<F16>::pack(acc[q][2] * inv, acc[q][3] * inv)};
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * D / 8; i += 2 * D) {
+        const int r = r0 + i / (D / 8), c = (i % (D / 8)) * 8, row = j.row0 + r;
+        if (r < j.rows)
+            *(i32x4 *)(out + (int64_t)(s.tok0 + row / P.group) * ld_out + (int64_t)(head * P.group + row % P.group) * D + c) =
+                *(const i32x4 *)(rows + (i / (D / 8)) * ROW + c);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1048,7 +1061,7 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
         }
         if (h.n_merge) {
             const Pages P = pages_args(pages, h, plan_dev, pool, h.merge);
-            hipLaunchKernelGGL((k_attend_merge<D, F>), dim3(h.n_merge * c.n_kv_heads, (h.merge_rows + 3) / 4), dim3(256), 0, s, P,
+            hipLaunchKernelGGL((k_attend_merge<D, F>), dim3(h.n_merge * c.n_kv_heads, (h.merge_rows + 31) / 32), dim3(2 * D), 0, s, P,
                                (const float *)large, (unsigned short *)out, ld_out);
             SPD_TRY(hipGetLastError());
         }

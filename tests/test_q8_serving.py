@@ -735,3 +735,79 @@ def test_product_adds_in_place_and_keeps_its_bits(gpu):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, third)
+
+
+# ------------------------------------------------------------------------------------------ GPU: all of them together
+
+def _example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_q8_block.py")
+    spec = importlib.util.spec_from_file_location("paged_q8_block", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+@gpu_test
+@pytest.mark.parametrize("cache", [B.SPD_E4M3, B.SPD_BF16], ids=["e4m3", "bf16"])
+def test_block_in_8_bits_over_pages(gpu, cache):
+    """An SPD block of one rank: chunks of a prompt beside decode steps, against the same block in 64 bits with nothing rounded.
+
+    Per projection: an operand whose largest value is 4 to 5 times its rms is rounded in steps of that over 127, an error of 4.5 / 127 / sqrt(12) = 1 % of its
+    rms, for rows and weights 1.5 % of the product; e4m3 rounds keys and values by 2^-4 / sqrt(3) = 3.6 % at most.  Scores of about unit size
+    turn the error of queries and keys into as much of the probabilities.  QKV, cache, attention, O: sqrt(1.5^2 (3 times) + 3.6^2 (twice) +
+    1 + ...) below 7 %; the MLP on it below 8 %."""
+    from paper_2502_20727_amd import inputs, workloads
+    ex = _example()
+    w = workloads.Workload(name="q8-block", hidden=512, n_q_heads=16, n_kv_heads=4, head_dim=64, ffn=1376, n_layers=1, tp=2, dtype=workloads.BF16,
+                           seed=11, batch=3, q_len=1, ctx=64, mask=(1,))
+    rank = 1
+    shard = inputs.layer_shard(w, 0, rank)
+    block = ex.Q8Block(w, shard, rank, max_tokens=200, n_pages=40, page_size=16, max_ctx=512, cache=cache)
+    pool = ex.PagedPool(40, 16)
+    W = {n: torch.from_numpy(a).double() for n, a in shard.items()}
+    q, kv, d = w.q_per_rank, w.kv_per_rank, w.head_dim
+    past = [[torch.zeros(0, kv, d, dtype=torch.float64) for _ in range(2)] for _ in range(3)]
+    g = torch.Generator().manual_seed(0)
+    done = [0, 0, 0]
+
+    def norm(t, gain):
+        return t / (t.square().mean(-1, keepdim=True) + w.rms_eps).sqrt() * gain
+
+    for lens in ([40, 0, 3], [1, 90, 1], [1, 60, 1], [1, 1, 1], [1, 1, 0]):
+        for s, n in enumerate(lens):
+            pool.grow(s, done[s] + n)
+        plan = B.PagePlan(block.pages, done, lens, [pool.table.get(s, []) for s in range(3)], window=100, sinks=4)
+        x = torch.randn(sum(lens), w.hidden, generator=g)
+        slots = 0.05 * torch.randn(w.tp, sum(lens), w.hidden, generator=g)
+        xd, sd = x.to(gpu), slots.to(gpu)
+        out = torch.empty_like(xd)
+        block.forward(plan, xd, sd, out)
+        X = x.double()
+        qkv = norm(X, W["g1"])
+        Q, K, V = ((qkv @ W[n]).unflatten(-1, (-1, d)) for n in ("wq", "wk", "wv"))
+        att, first = [], 0
+        for s, n in enumerate(lens):
+            at = torch.arange(done[s], done[s] + n)
+            rows = slice(first, first + n)
+            first += n
+            past[s][0] = torch.cat([past[s][0], rotate(K[rows], at, w.rope_base)])
+            past[s][1] = torch.cat([past[s][1], V[rows]])
+            key = torch.arange(done[s] + n)
+            seen = (key <= at[:, None]) & ((key > at[:, None] - 100) | (key < 4))
+            qs, o = rotate(Q[rows], at, w.rope_base), torch.zeros(n, q, d, dtype=torch.float64)
+            for j in range(q):
+                sc = qs[:, j] @ past[s][0][:, j // (q // kv)].t() / math.sqrt(d)
+                o[:, j] = sc.masked_fill(~seen, -math.inf).softmax(-1) @ past[s][1][:, j // (q // kv)]
+            att.append(o.flatten(1))
+            done[s] += n
+        y = torch.cat(att) @ W["wo"]
+        m = norm(X + y, W["g2"])
+        gate = m @ W["wg"]
+        z = (gate * torch.sigmoid(gate) * (m @ W["wu"])) @ W["wd"]
+        got = sd[rank].cpu().double()
+        assert float((got - (y + z)).norm() / (y + z).norm()) < 0.08
+        total = X + slots[0].double() + got
+        assert float((out.cpu().double() - total).abs().max()) < 1e-5
+    block.close()
