@@ -73,7 +73,7 @@ class spd_pages_plan_info(C.Structure):
     _fields_ = [("batch", C.c_int32), ("tokens", C.c_int32), ("held", C.c_int64), ("workspace_bytes", C.c_size_t)]
 
 
-_lib = _torch = None
+_lib = _torch = _int8 = _float32 = _raw_stream = _device = None
 _TYPES: Dict[object, int] = {}       # SPD_* codes of torch's element types
 
 _PROTOS = {
@@ -155,7 +155,7 @@ SPD_STAGE_EMPTY = len(STAGES)
 
 def lib():
     """The loaded HIP library.  Raises if it is missing and cannot be built."""
-    global _lib, _torch
+    global _lib, _torch, _int8, _float32, _raw_stream, _device
     if _lib is None:
         path = build.ensure_hip()
         # PyTorch ships its own HIP runtime.  The library must bind to the same one as the tensors it
@@ -163,7 +163,8 @@ def lib():
         # other way round, the process holds two runtimes and this library's calls see no device.
         try:
             import torch
-            _torch = torch
+            _torch, _int8, _float32 = torch, torch.int8, torch.float32
+            _raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
             _TYPES.update({torch.float32: SPD_F32, torch.bfloat16: SPD_BF16, torch.float16: SPD_F16})
         except ImportError:
             pass
@@ -340,12 +341,11 @@ def spd_kv_unpack(ctx: int, cache_host: np.ndarray, batch: int, n_pos: int, kv_h
 # --------------------------------------------------------------------------- device calls
 
 def _current_stream() -> int:
-    """torch's current stream on its current device, without the object around it (which takes longer than a small launch)."""
-    import torch
-    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
-    if raw is None or device is None:
+    """torch's current stream on its current device, without the object around it (which takes as long as a small launch)."""
+    if _raw_stream is None or _device is None:
+        import torch
         return torch.cuda.current_stream().cuda_stream
-    return raw(device())
+    return _raw_stream(_device())
 
 
 def _stream_ptr(stream) -> Optional[int]:
@@ -547,99 +547,115 @@ def _type(t) -> int:
     return code
 
 
-def _rows(t, rows: int, cols: int, what: str):
+def _rows(t, shape, what: str):
     """(address, row stride) of a device matrix whose rows are contiguous; (None, 0) for None."""
     if t is None:
         return None, 0
-    strides = t.stride()
-    if t.shape != (rows, cols) or (cols > 1 and strides[1] != 1):
-        raise ValueError(f"{what}: a [{rows}, {cols}] matrix with contiguous rows wanted, not {tuple(t.shape)} with strides {strides}")
-    ld = strides[0]
-    return t.data_ptr(), (ld if ld >= cols or rows > 1 else cols)
+    if t.shape != shape:
+        raise ValueError(f"{what}: {shape} wanted, not {tuple(t.shape)}")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"{what}: rows have to be contiguous, strides {t.stride()}")
+    if ld < shape[1] and shape[0] == 1:
+        ld = shape[1]
+    return t.data_ptr(), ld
+
+
+def _buffer(t):
+    """Address of a contiguous device tensor, None for None."""
+    if t is None:
+        return None
+    assert t.is_contiguous()
+    return t.data_ptr()
 
 
 def _like(t, other, what: str):
-    if t is not None and t.dtype != other.dtype:
+    if t is not None and t.dtype is not other.dtype:
         raise TypeError(f"{what}: {other.dtype} wanted, not {t.dtype}")
 
 
 def spd_pages_write(pages: int, plan: "PagePlan", qkv, rope, pool, q_out=None, stream=None) -> None:
     """qkv [tokens, (q_heads + 2 kv_heads) head_dim]; q_out [tokens, q_heads head_dim] in the pool's 16-bit type, or None."""
     width = qkv.shape[-1]
-    p, ld = _rows(qkv, plan.tokens, width, "qkv")
+    p, ld = _rows(qkv, (plan.tokens, width), "qkv")
     if width < plan.qkv_cols:
         raise ValueError("qkv: rows too short")
-    qo, ld_q = _rows(q_out, plan.tokens, plan.q_cols, "q_out")
+    qo, ld_q = _rows(q_out, plan.q_shape, "q_out")
     if qo is not None and _type(q_out) != plan.dtype:
         raise TypeError("q_out: the pool's 16-bit type wanted")
-    rc = lib().spd_pages_write(pages, plan.host_ptr, plan.device_ptr, _type(qkv), p, ld, _ptr(rope), _ptr(pool), qo, ld_q, _stream_ptr(stream))
+    rc = _lib.spd_pages_write(pages, plan.host_ptr, plan.device_ptr, _type(qkv), p, ld, _buffer(rope), _buffer(pool), qo, ld_q,
+                              _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_pages_write")
 
 
 def spd_pages_read(pages: int, plan: "PagePlan", pool, k_out, v_out, stream=None) -> None:
     """k_out, v_out [held, kv_heads, head_dim]: every position of every sequence, one after the other."""
-    c = plan.pages.cfg
-    want = (plan.info.held, c.n_kv_heads, c.head_dim)
-    if k_out.shape != want or v_out.shape != want:
-        raise ValueError(f"k_out, v_out: {want} wanted")
+    if k_out.shape != plan.held_shape or v_out.shape != plan.held_shape:
+        raise ValueError(f"k_out, v_out: {plan.held_shape} wanted")
     _like(v_out, k_out, "v_out")
-    rc = lib().spd_pages_read(pages, plan.host_ptr, plan.device_ptr, _ptr(pool), _type(k_out), _ptr(k_out), _ptr(v_out), _stream_ptr(stream))
+    rc = _lib.spd_pages_read(pages, plan.host_ptr, plan.device_ptr, _buffer(pool), _type(k_out), _buffer(k_out), _buffer(v_out),
+                             _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_pages_read")
 
 
 def spd_pages_attention(pages: int, plan: "PagePlan", q, pool, out, workspace=None, stream=None) -> None:
     """q, out [tokens, q_heads head_dim] in the pool's 16-bit type, rows may be strided."""
-    qp, ld_q = _rows(q, plan.tokens, plan.q_cols, "q")
-    op, ld_o = _rows(out, plan.tokens, plan.q_cols, "out")
+    qp, ld_q = _rows(q, plan.q_shape, "q")
+    op, ld_o = _rows(out, plan.q_shape, "out")
     if _type(q) != plan.dtype or _type(out) != plan.dtype:
         raise TypeError("q, out: the pool's 16-bit type wanted")
     if workspace is not None and workspace.nbytes < plan.workspace_bytes:
         raise ValueError("workspace: too small for the plan")
-    rc = lib().spd_pages_attention(pages, plan.host_ptr, plan.device_ptr, qp, ld_q, _ptr(pool), op, ld_o, _ptr(workspace), _stream_ptr(stream))
+    rc = _lib.spd_pages_attention(pages, plan.host_ptr, plan.device_ptr, qp, ld_q, _buffer(pool), op, ld_o, _buffer(workspace),
+                                  _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_pages_attention")
 
 
-def _codes(codes, scales, rows: int, n: int):
-    if _type(scales) != SPD_F32 or codes.dtype != _torch.int8 or scales.numel() != rows or not scales.is_contiguous():
+def _codes(codes, scales, shape):
+    if codes.dtype is not _int8 or scales.dtype is not _float32 or scales.numel() != shape[0] or not scales.is_contiguous():
         raise TypeError("codes: int8, scales: contiguous float32, one a row")
-    return _rows(codes, rows, n, "codes")
+    return _rows(codes, shape, "codes")
 
 
 def spd_q8_norm(x, add, gain, eps: float, sum_out, codes, scales, stream=None) -> None:
     """codes, scales <- RMSNorm(x + add) * gain in 8 bits; sum_out <- x + add.  add and sum_out may be None."""
-    rows, n = x.shape
-    px, lx = _rows(x, rows, n, "x")
-    pa, la = _rows(add, rows, n, "add")
-    ps, ls = _rows(sum_out, rows, n, "sum_out")
-    pc, lc = _codes(codes, scales, rows, n)
+    l = _lib or lib()
+    rows, n = shape = x.shape
+    px, lx = _rows(x, shape, "x")
+    pa, la = _rows(add, shape, "add")
+    ps, ls = _rows(sum_out, shape, "sum_out")
+    pc, lc = _codes(codes, scales, shape)
     _like(add, x, "add")
     _like(sum_out, x, "sum_out")
-    if _type(gain) != SPD_F32 or gain.numel() != n:
+    if gain.dtype is not _float32 or gain.numel() != n:
         raise TypeError("gain: float32, one a column")
-    rc = lib().spd_q8_norm(_type(x), rows, n, px, lx, pa, la, _ptr(gain), eps, ps, ls, pc, lc, scales.data_ptr(), _stream_ptr(stream))
+    rc = l.spd_q8_norm(_type(x), rows, n, px, lx, pa, la, _buffer(gain), eps, ps, ls, pc, lc, scales.data_ptr(),
+                       _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_q8_norm")
 
 
 def spd_q8_rows(x, codes, scales, stream=None) -> None:
-    rows, n = x.shape
-    px, lx = _rows(x, rows, n, "x")
-    pc, lc = _codes(codes, scales, rows, n)
-    rc = lib().spd_q8_rows(_type(x), rows, n, px, lx, pc, lc, scales.data_ptr(), _stream_ptr(stream))
+    l = _lib or lib()
+    rows, n = shape = x.shape
+    px, lx = _rows(x, shape, "x")
+    pc, lc = _codes(codes, scales, shape)
+    rc = l.spd_q8_rows(_type(x), rows, n, px, lx, pc, lc, scales.data_ptr(), _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_q8_rows")
 
 
 def spd_q8_swiglu(x, codes, scales, stream=None) -> None:
     """x [rows, 2 n]: gates, then ups."""
+    l = _lib or lib()
     rows, n = x.shape
     n //= 2
-    px, lx = _rows(x, rows, 2 * n, "x")
-    pc, lc = _codes(codes, scales, rows, n)
-    rc = lib().spd_q8_swiglu(_type(x), rows, n, px, lx, pc, lc, scales.data_ptr(), _stream_ptr(stream))
+    px, lx = _rows(x, (rows, 2 * n), "x")
+    pc, lc = _codes(codes, scales, (rows, n))
+    rc = l.spd_q8_swiglu(_type(x), rows, n, px, lx, pc, lc, scales.data_ptr(), _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_q8_swiglu")
 
@@ -682,17 +698,19 @@ def spd_q8_matmul_workspace(rows: int, K: int, N: int) -> int:
 
 def spd_q8_matmul(codes, scales, packed, N: int, add, out, workspace=None, stream=None) -> None:
     """out [rows, N] <- (codes [rows, K] times the packed K x N weights) * scales (+ add)."""
-    l = lib()
+    l = _lib or lib()
     rows, K = codes.shape
-    pc, lc = _codes(codes, scales, rows, K)
-    pa, la = _rows(add, rows, N, "add")
-    po, lo = _rows(out, rows, N, "out")
+    shape = (rows, N)
+    pc, lc = _codes(codes, scales, (rows, K))
+    pa, la = _rows(add, shape, "add")
+    po, lo = _rows(out, shape, "out")
     _like(add, out, "add")
     if packed.nbytes < spd_q8_weight_bytes(K, N):
         raise ValueError("packed: too small for a %d x %d matrix" % (K, N))
     if (workspace.nbytes if workspace is not None else 0) < spd_q8_matmul_workspace(rows, K, N):
         raise ValueError("workspace: too small")
-    rc = l.spd_q8_matmul(rows, K, N, pc, lc, scales.data_ptr(), _ptr(packed), _type(out), pa, la, po, lo, _ptr(workspace), _stream_ptr(stream))
+    rc = l.spd_q8_matmul(rows, K, N, pc, lc, scales.data_ptr(), _buffer(packed), _type(out), pa, la, po, lo, _buffer(workspace),
+                         _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_q8_matmul")
 
@@ -800,7 +818,8 @@ class PagePlan:
         self.device = torch.from_numpy(self.host).to(pages.device)
         c = pages.cfg
         self.tokens, self.workspace_bytes, self.dtype = self.info.tokens, self.info.workspace_bytes, c.dtype
-        self.q_cols, self.qkv_cols = c.n_q_heads * c.head_dim, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
+        self.qkv_cols = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
+        self.q_shape, self.held_shape = (self.tokens, c.n_q_heads * c.head_dim), (self.info.held, c.n_kv_heads, c.head_dim)
         self.host_ptr, self.device_ptr = self.host.ctypes.data, self.device.data_ptr()
         n = self.workspace_bytes
         self.workspace = torch.zeros(n, dtype=torch.uint8, device=pages.device) if n else None
