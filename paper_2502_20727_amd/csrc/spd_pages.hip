@@ -84,6 +84,12 @@ __device__ __forceinline__ float quad_max(float x) {
     return fmaxf(x, __shfl_xor(x, 32, 64));
 }
 
+// over lanes l, l^32
+__device__ __forceinline__ float half_max(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
 // what every kernel over pages is told
 struct Pages {
     const char *plan;
@@ -696,127 +702,161 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         for (int c = 0; c < CH; ++c) vx[c] = *(const i32x4 *)(values + c * 1024 + lane * 16);
         if (lane < 32) sx = scales[lane < 16 ? r16 : P.page_size + r16];
     };
-    auto put_away = [&](Stage &to) __attribute__((always_inline)) {
+    // (after the last tile what is put away is not read)
+    auto put_away = [&](int c, Stage &to) __attribute__((always_inline)) {
         short *kd = to.k + wave * 16 * D, *vd = to.v + wave * 16 * D;
+        if constexpr (E4M3) {
+            *(i32x4 *)(kd + ((8 * c + 2 * g) * 16 + r16) * 8) = QK::widen(kx[c][0], kx[c][1]);
+            *(i32x4 *)(kd + ((8 * c + 2 * g + 1) * 16 + r16) * 8) = QK::widen(kx[c][2], kx[c][3]);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if constexpr (E4M3) {
-                *(i32x4 *)(kd + ((8 * c + 2 * g) * 16 + r16) * 8) = QK::widen(kx[c][0], kx[c][1]);
-                *(i32x4 *)(kd + ((8 * c + 2 * g + 1) * 16 + r16) * 8) = QK::widen(kx[c][2], kx[c][3]);
-            } else *(i32x4 *)(kd + ((4 * c + g) * 16 + r16) * 8) = kx[c];
+            for (int t = 0; t < 4; ++t)
+                *(i32x2 *)(vd + (((4 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) =
+                    (i32x2){PV::template from_e4m3<false>(vx[c][t]), PV::template from_e4m3<true>(vx[c][t])};
+        } else {
+            *(i32x4 *)(kd + ((4 * c + g) * 16 + r16) * 8) = kx[c];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                *(i32x2 *)(vd + (((2 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) = (i32x2){vx[c][2 * t], vx[c][2 * t + 1]};
         }
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if constexpr (E4M3) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    *(i32x2 *)(vd + (((4 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) =
-                        (i32x2){PV::template from_e4m3<false>(vx[c][t]), PV::template from_e4m3<true>(vx[c][t])};
-            } else {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    *(i32x2 *)(vd + (((2 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) = (i32x2){vx[c][2 * t], vx[c][2 * t + 1]};
-            }
-        }
-        if (lane < 16) to.ks[wave * 16 + r16] = sx * A.scale;
-        else if (lane < 32) to.vs[wave * 16 + r16] = sx;
+    };
+    auto put_scales = [&](Stage &to) __attribute__((always_inline)) {
+        // a value that is NaN makes its key's score NaN, and nothing else: whoever sees it gets NaN, others multiply by 0
+        const float vs = __shfl(sx, r16 + 16, 64);
+        if (lane < 16) to.ks[wave * 16 + r16] = vs == vs ? sx * A.scale : vs;
+        else if (lane < 32) to.vs[wave * 16 + r16] = vs == vs ? vs : 0.f;
     };
     int page = page_of(P, s, my_block(0));
     fetch(0, page);
     page = page_of(P, s, my_block(4));
-    put_away(stage[0]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) put_away(c, stage[0]);
+    put_scales(stage[0]);
     __syncthreads();
-    for (int v0 = 0, turn = 0; v0 < it.count; v0 += 4, turn ^= 1) {
+    // Operands and scales are read from the LDS some instructions ahead of their use, fenced so that the compiler leaves them there (read
+    // where they are used, a wave waits for the LDS 24 times a tile).
+    constexpr int AHEAD = 4;
+    const int k_lane = (col >> 4) * 16 * D + (half * 16 + (col & 15)) * 8, v_lane = (((col >> 4) * 2 + half) * 16 + (col & 15)) * 8;
+    i32x4 ring[AHEAD];
+    f32x4 ks[4], vs[4];
+    f32x16 sc[2];
+    int v0 = 0, turn = 0;
+    // Scores of tile v0, which lies in stage `turn`, and their maximum over the row: score i of half h is of block 2 h + i / 8, position
+    // 8 ((i / 4) % 2) + 4 half + i % 4 in it.
+    auto scores = [&]() __attribute__((always_inline)) {
         const Stage &now = stage[turn];
-        const bool more = v0 + 4 < it.count;
-        if (more) {
-            fetch(v0 + 4, page);
-            page = page_of(P, s, my_block(v0 + 8));
+        const short *kp = now.k + k_lane;
+        auto frag = [&](int n) __attribute__((always_inline)) { return *(const i32x4 *)(kp + (n / KS) * 32 * D + (n % KS) * 256); };
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) ring[n] = frag(n);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[0][i] = sc[1][i] = 0.f;
+        float mx = -__builtin_inff();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < 2 * KS; ++n) {
+            sc[n / KS] = QK::mfma32(ring[n % AHEAD], qf[n % KS], sc[n / KS]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (n + AHEAD < 2 * KS) ring[n % AHEAD] = frag(n + AHEAD);
+            if (n < 4) ks[n] = *(const f32x4 *)(now.ks + n * 8 + 4 * half);
+            if (n >= KS) {                       // beside the second half's: the first half scaled, and its maximum
+                constexpr int PER = 16 / KS;
+#pragma unroll
+                for (int i = (n - KS) * PER; i < (n - KS + 1) * PER; ++i) {
+                    sc[0][i] *= ks[i >> 2][i & 3];
+                    mx = fmaxf(mx, sc[0][i]);
+                    if ((i & 3) == 3) ks[i >> 2] = *(const f32x4 *)(now.ks + 32 + (i >> 2) * 8 + 4 * half);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        // does every query of the wave see all of the tile?  Does any see some of it?  (first and last block; a tile of sinks and window blocks is mixed)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) vs[q] = *(const f32x4 *)(now.vs + q * 8 + 4 * half);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            sc[1][i] *= ks[i >> 2][i & 3];
+            mx = fmaxf(mx, sc[1][i]);
+        }
+        // is something of the tile hidden from some query of the wave?  (first and last block; a tile of sinks and window blocks is mixed)
         const int n_here = it.count - v0 < 4 ? it.count - v0 : 4;
         const int b_first = list_block(it, it.first + v0), b_last = list_block(it, it.first + v0 + n_here - 1);
-        const bool all = n_here == 4 && b_last * 16 + 15 <= first_at && (A.window == 0 || b_first * 16 > last_at - A.window || b_last * 16 + 15 < A.sinks);
-        const bool any = b_first * 16 <= last_at && (A.window == 0 || b_last * 16 + 15 > first_at - A.window || b_first * 16 < A.sinks);
-        if (!any) {                              // (the wave's rows lie before the tile, or past its window)
-            if (more) put_away(stage[turn ^ 1]);
-            __syncthreads();
-            continue;
-        }
-        f32x16 sc[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[h][i] = 0.f;
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                const i32x4 kf = *(const i32x4 *)(now.k + (2 * h + (col >> 4)) * 16 * D + ((2 * i + half) * 16 + (col & 15)) * 8);
-                sc[h] = QK::mfma32(kf, qf[i], sc[h]);
-            }
-        }
-        // score i of half h: block 2 h + i / 8 of the tile, position 8 ((i / 4) % 2) + 4 half + i % 4 in it
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const f32x4 ks = *(const f32x4 *)(now.ks + q * 8 + 4 * half);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sc[q >> 2][(q & 3) * 4 + i] *= ks[i];
-        }
-        if (!all) {
+        if (!(n_here == 4 && b_last * 16 + 15 <= first_at && (A.window == 0 || b_first * 16 > last_at - A.window || b_last * 16 + 15 < A.sinks))) {
+            mx = -__builtin_inff();
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 const int key0 = (q >> 1) < n_here ? list_block(it, it.first + v0 + (q >> 1)) * 16 : 0x7fffff0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!visible(key0 + 8 * (q & 1) + 4 * half + i, at, A.window, A.sinks)) sc[q >> 2][(q & 3) * 4 + i] = -__builtin_inff();
+                for (int i = 0; i < 4; ++i) {
+                    const bool seen = visible(key0 + 8 * (q & 1) + 4 * half + i, at, A.window, A.sinks);
+                    const float x = seen ? sc[q >> 2][(q & 3) * 4 + i] : -__builtin_inff();
+                    sc[q >> 2][(q & 3) * 4 + i] = x;
+                    mx = fmaxf(mx, x);
+                }
             }
         }
-        float mx = sc[0][0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        // The maximum only keeps the powers of two in range: one that has grown by less than 2^8 stays, and the outputs with it.
-        const bool grown = __builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0;
-        const float m_new = grown ? fmaxf(m, mx) : m, m_use = m_new == -__builtin_inff() ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m - m_use);
-        m = m_new;
-        i32x4 pf[4];
-        float ps = 0.f;
-        auto weigh = [&](auto masked_) __attribute__((always_inline)) {
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                float w[8];
-#pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    const f32x4 vs = *(const f32x4 *)(now.vs + b * 16 + 2 * i + 4 * half);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float x = sc[b >> 1][(b & 1) * 8 + i + e], p = __builtin_amdgcn_exp2f(x - m_use);
-                        ps += p;
-                        // (the scale of a hidden key's value may be NaN)
-                        w[i + e] = decltype(masked_)::value && x == -__builtin_inff() ? 0.f : p * vs[e];
-                    }
-                }
-                pf[b] = (i32x4){PV::pack(w[0], w[1]), PV::pack(w[2], w[3]), PV::pack(w[4], w[5]), PV::pack(w[6], w[7])};
-            }
-        };
-        if (all) weigh(std::false_type());
-        else weigh(std::true_type());
-        l = l * alpha + ps;                      // (of the lane's half of the keys)
-        if (more) put_away(stage[turn ^ 1]);
-        if (grown) {
+        return half_max(mx);
+    };
+    float mx = scores();
+    while (true) {
+        // The maximum only keeps the powers of two in range: while it grows by less than 2^8 it stays, and the outputs with it, in the inner loop.
+        {
+            const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - (m_new == -__builtin_inff() ? 0.f : m_new));
+            m = m_new;
+            l *= alpha;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
         }
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                const i32x4 vf = *(const i32x4 *)(now.v + b * 16 * D + (((2 * t + (col >> 4)) * 2 + half) * 16 + (col & 15)) * 8);
-                o[t] = PV::mfma32(vf, pf[b], o[t]);
+        const float m_use = m == -__builtin_inff() ? 0.f : m;
+        bool grown = false;
+        do {
+            const Stage &now = stage[turn];
+            const bool more = v0 + 4 < it.count;
+            if (more) {
+                fetch(v0 + 4, page);
+                page = page_of(P, s, my_block(v0 + 8));
             }
-        __syncthreads();
+            i32x4 pf[4];
+            float ps = 0.f, w[2];
+            // element i (of 32) of the scores: its power of two, with the value's scale, a pair at a time into the operand
+            auto weigh = [&](int i) __attribute__((always_inline)) {
+                const float p = __builtin_amdgcn_exp2f(sc[i >> 4][i & 15] - m_use);
+                ps += p;
+                w[i & 1] = p * vs[(i >> 2) & 3][i & 3];
+                if (i & 1) pf[i >> 3][(i & 7) >> 1] = PV::pack(w[0], w[1]);
+                if ((i & 3) == 3 && i < 16) vs[i >> 2] = *(const f32x4 *)(now.vs + 32 + (i >> 2) * 8 + 4 * half);
+            };
+            const short *vp = now.v + v_lane;
+            auto frag = [&](int n) __attribute__((always_inline)) { return *(const i32x4 *)(vp + (n / DT) * 16 * D + (n % DT) * 512); };
+#pragma unroll
+            for (int i = 0; i < 16; ++i) weigh(i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) ring[n] = frag(n);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < 4 * DT; ++n) {
+                o[n % DT] = PV::mfma32(ring[n % AHEAD], pf[n / DT], o[n % DT]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (n + AHEAD < 4 * DT) ring[n % AHEAD] = frag(n + AHEAD);
+                if (n < 2 * DT) {                // beside the first half's outputs: the second half's weights
+                    constexpr int PER = 8 / DT;
+#pragma unroll
+                    for (int i = 16 + n * PER; i < 16 + (n + 1) * PER; ++i) weigh(i);
+                } else if ((n - 2 * DT) % (2 * DT / CH) == 0) put_away((n - 2 * DT) / (2 * DT / CH), stage[turn ^ 1]);      // beside the second's: the next tile
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            l += ps;                             // (of the lane's half of the keys)
+            put_scales(stage[turn ^ 1]);
+            __syncthreads();
+            v0 += 4;
+            turn ^= 1;
+            if (v0 >= it.count) break;
+            mx = scores();
+            grown = __builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0;
+        } while (!grown);
+        if (!grown) break;
     }
     l += __shfl_xor(l, 32, 64);
     if (it.slot < 0) {
