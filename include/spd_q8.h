@@ -141,7 +141,7 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
  *   ld*      row strides in elements; rows need no alignment beyond their elements'
  *   codes    int8 [rows][ld_codes]
  *   scales   fp32 [rows]
- * rows = 0 or n = 0: nothing is done. */
+ * rows (at most 2^23) = 0 or n = 0: nothing is done. */
 
 /* v = s / sqrt(mean(s^2) + eps) * gain with s = x + add.
  *   add   [rows][ld_add] or NULL (s = x);   sum   receives s in `dtype` or NULL, may alias x or add (same stride) */
@@ -172,7 +172,7 @@ int spd_q8_unpack(int32_t K, int32_t N, const void *packed_host, int8_t *w, int6
 /* scratch of a product of at most `rows` rows on one stream, may be 0 */
 size_t spd_q8_matmul_workspace(int32_t rows, int32_t K, int32_t N);
 /* Device call.
- *   rows       at most 2^30, rows * N at most 2^38
+ *   rows       at most 2^28, rows * N at most 2^38
  *   codes      int8 [rows][ld_codes], 16-byte aligned, ld_codes a multiple of 16 and at least K rounded up to that (bytes past K
  *              may hold anything)
  *   packed     device copy of the packed weights, 256-byte aligned

@@ -553,6 +553,8 @@ def _rows(t, shape, what: str):
         return None, 0
     if t.shape != shape:
         raise ValueError(f"{what}: {shape} wanted, not {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: a tensor on the device wanted")
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
         raise ValueError(f"{what}: rows have to be contiguous, strides {t.stride()}")
@@ -561,11 +563,14 @@ def _rows(t, shape, what: str):
     return t.data_ptr(), ld
 
 
-def _buffer(t):
-    """Address of a contiguous device tensor, None for None."""
+def _buffer(t, what: str = "buffer", nbytes: int = 0):
+    """Address of a contiguous device tensor of at least `nbytes`, None for None."""
     if t is None:
         return None
-    assert t.is_contiguous()
+    if not (t.is_cuda and t.is_contiguous()):
+        raise ValueError(f"{what}: a contiguous tensor on the device wanted")
+    if t.nbytes < nbytes:
+        raise ValueError(f"{what}: too small")
     return t.data_ptr()
 
 
@@ -583,7 +588,8 @@ def spd_pages_write(pages: int, plan: "PagePlan", qkv, rope, pool, q_out=None, s
     qo, ld_q = _rows(q_out, plan.q_shape, "q_out")
     if qo is not None and _type(q_out) != plan.dtype:
         raise TypeError("q_out: the pool's 16-bit type wanted")
-    rc = _lib.spd_pages_write(pages, plan.host_ptr, plan.device_ptr, _type(qkv), p, ld, _buffer(rope), _buffer(pool), qo, ld_q,
+    rc = _lib.spd_pages_write(pages, plan.host_ptr, plan.device_ptr, _type(qkv), p, ld, _buffer(rope, "rope", plan.rope_bytes),
+                              _buffer(pool, "pool", plan.pool_bytes), qo, ld_q,
                               _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_pages_write")
@@ -594,7 +600,8 @@ def spd_pages_read(pages: int, plan: "PagePlan", pool, k_out, v_out, stream=None
     if k_out.shape != plan.held_shape or v_out.shape != plan.held_shape:
         raise ValueError(f"k_out, v_out: {plan.held_shape} wanted")
     _like(v_out, k_out, "v_out")
-    rc = _lib.spd_pages_read(pages, plan.host_ptr, plan.device_ptr, _buffer(pool), _type(k_out), _buffer(k_out), _buffer(v_out),
+    rc = _lib.spd_pages_read(pages, plan.host_ptr, plan.device_ptr, _buffer(pool, "pool", plan.pool_bytes), _type(k_out),
+                             _buffer(k_out, "k_out"), _buffer(v_out, "v_out"),
                              _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_pages_read")
@@ -606,17 +613,16 @@ def spd_pages_attention(pages: int, plan: "PagePlan", q, pool, out, workspace=No
     op, ld_o = _rows(out, plan.q_shape, "out")
     if _type(q) != plan.dtype or _type(out) != plan.dtype:
         raise TypeError("q, out: the pool's 16-bit type wanted")
-    if workspace is not None and workspace.nbytes < plan.workspace_bytes:
-        raise ValueError("workspace: too small for the plan")
-    rc = _lib.spd_pages_attention(pages, plan.host_ptr, plan.device_ptr, qp, ld_q, _buffer(pool), op, ld_o, _buffer(workspace),
+    rc = _lib.spd_pages_attention(pages, plan.host_ptr, plan.device_ptr, qp, ld_q, _buffer(pool, "pool", plan.pool_bytes), op, ld_o,
+                                  _buffer(workspace, "workspace", plan.workspace_bytes),
                                   _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_pages_attention")
 
 
 def _codes(codes, scales, shape):
-    if codes.dtype is not _int8 or scales.dtype is not _float32 or scales.numel() != shape[0] or not scales.is_contiguous():
-        raise TypeError("codes: int8, scales: contiguous float32, one a row")
+    if codes.dtype is not _int8 or scales.dtype is not _float32 or scales.numel() != shape[0] or not (scales.is_cuda and scales.is_contiguous()):
+        raise TypeError("codes: int8, scales: contiguous float32 on the device, one a row")
     return _rows(codes, shape, "codes")
 
 
@@ -632,7 +638,7 @@ def spd_q8_norm(x, add, gain, eps: float, sum_out, codes, scales, stream=None) -
     _like(sum_out, x, "sum_out")
     if gain.dtype is not _float32 or gain.numel() != n:
         raise TypeError("gain: float32, one a column")
-    rc = l.spd_q8_norm(_type(x), rows, n, px, lx, pa, la, _buffer(gain), eps, ps, ls, pc, lc, scales.data_ptr(),
+    rc = l.spd_q8_norm(_type(x), rows, n, px, lx, pa, la, _buffer(gain, "gain"), eps, ps, ls, pc, lc, scales.data_ptr(),
                        _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_q8_norm")
@@ -705,11 +711,10 @@ def spd_q8_matmul(codes, scales, packed, N: int, add, out, workspace=None, strea
     pa, la = _rows(add, shape, "add")
     po, lo = _rows(out, shape, "out")
     _like(add, out, "add")
-    if packed.nbytes < spd_q8_weight_bytes(K, N):
-        raise ValueError("packed: too small for a %d x %d matrix" % (K, N))
     if (workspace.nbytes if workspace is not None else 0) < spd_q8_matmul_workspace(rows, K, N):
         raise ValueError("workspace: too small")
-    rc = l.spd_q8_matmul(rows, K, N, pc, lc, scales.data_ptr(), _buffer(packed), _type(out), pa, la, po, lo, _buffer(workspace),
+    rc = l.spd_q8_matmul(rows, K, N, pc, lc, scales.data_ptr(), _buffer(packed, "packed", spd_q8_weight_bytes(K, N)), _type(out), pa, la, po, lo,
+                         _buffer(workspace, "workspace"),
                          _current_stream() if stream is None else _stream_ptr(stream))
     if rc:
         raise SpdError(rc, "spd_q8_matmul")
@@ -781,7 +786,8 @@ class DeviceShard:
 
 
 class DevicePages:
-    """A pool of pages on the device with its handle and rotary table.  Holds memory only."""
+    """A pool of pages on the device with its handle and rotary table.  Holds memory only; a pool made here is cleared on torch's current
+    stream, which other streams wait for."""
 
     def __init__(self, cfg: spd_pages_config, device, pool=None, rope: bool = True):
         import torch
@@ -808,7 +814,8 @@ class DevicePages:
 
 
 class PagePlan:
-    """The plan of a step, on the host and on the device, and its scratch."""
+    """The plan of a step, on the host and on the device, and its scratch, cleared on torch's current stream.  Calls of one plan that may
+    overlap (on several streams) need a scratch each."""
 
     def __init__(self, pages: DevicePages, positions: Sequence[int], q_lens: Sequence[int], page_table, window: int = 0, sinks: int = 0):
         import torch
@@ -820,6 +827,7 @@ class PagePlan:
         self.tokens, self.workspace_bytes, self.dtype = self.info.tokens, self.info.workspace_bytes, c.dtype
         self.qkv_cols = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
         self.q_shape, self.held_shape = (self.tokens, c.n_q_heads * c.head_dim), (self.info.held, c.n_kv_heads, c.head_dim)
+        self.pool_bytes, self.rope_bytes = pages.sizes.pool_bytes, pages.sizes.rope_bytes
         self.host_ptr, self.device_ptr = self.host.ctypes.data, self.device.data_ptr()
         n = self.workspace_bytes
         self.workspace = torch.zeros(n, dtype=torch.uint8, device=pages.device) if n else None

@@ -186,7 +186,8 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
     at = (at + 15) & ~(size_t)15;
     if (at > 0x7fffffffull) return SPD_EINVAL;
     h.bytes = at;
-    h.part_small = small_slots ? SPD_COUNTERS * 4 : 0;
+    // (the counters' place is kept wherever there is a workspace: another plan may use it next, and finds them at zero)
+    h.part_small = small_slots || large_slots ? SPD_COUNTERS * 4 : 0;
     h.part_large = h.part_small + spd_align256((size_t)small_slots * c.n_kv_heads * spd_part_floats(SPD_SMALL_ROWS, c.head_dim) * 4);
     h.workspace = h.part_large + spd_align256((size_t)large_slots * c.n_kv_heads * spd_part_floats(SPD_LARGE_ROWS, c.head_dim) * 4);
     *bytes = h.bytes;

@@ -79,7 +79,8 @@ __global__ void __launch_bounds__(256) k_rows_q8(RowArgs A) {
     ss = (sh[0][0] + sh[0][1]) + (sh[0][2] + sh[0][3]);
     most = fmaxf(fmaxf(sh[1][0], sh[1][1]), fmaxf(sh[1][2], sh[1][3]));
     const float factor = KIND == ROW_NORM ? 1.f / sqrtf(ss / (float)A.n + A.eps) : 1.f;
-    const bool ok = most < __builtin_inff() && (KIND != ROW_NORM || (ss < __builtin_inff()));
+    // (a row of zeros without an eps has a factor of infinity, and 0 times it is NaN)
+    const bool ok = most < __builtin_inff() && (KIND != ROW_NORM || (ss < __builtin_inff() && most * factor < __builtin_inff()));
     const float a = fmaxf(most * factor, 0x1p-90f), up = 127.f / a;
     if (threadIdx.x == 0) A.scales[row] = ok ? a / 127.f : __builtin_nanf("");
     int8_t *codes = A.codes + row * A.ld_codes;
@@ -165,7 +166,8 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
         most = fmaxf(most, sh[1][w]);
     }
     const float factor = KIND == ROW_NORM ? 1.f / sqrtf(ss / (float)A.n + A.eps) : 1.f;
-    const bool ok = most < __builtin_inff() && (KIND != ROW_NORM || ss < __builtin_inff());
+    // (a row of zeros without an eps has a factor of infinity, and 0 times it is NaN)
+    const bool ok = most < __builtin_inff() && (KIND != ROW_NORM || (ss < __builtin_inff() && most * factor < __builtin_inff()));
     const float a = fmaxf(most * factor, 0x1p-90f), up = 127.f / a;
     if (threadIdx.x == 0) A.scales[row] = ok ? a / 127.f : __builtin_nanf("");
     int8_t *codes = A.codes + row * A.ld_codes;
@@ -211,7 +213,7 @@ hipError_t launch_rows(int kind, int rows, const RowArgs &A, hipStream_t s) {
 int rows_impl(int kind, int32_t dtype, int32_t rows, const RowArgs &A, void *stream) {
     const int64_t width = kind == ROW_SWIGLU ? 2 * (int64_t)A.n : A.n;
     if (dtype != SPD_F32 && dtype != SPD_BF16 && dtype != SPD_F16) return SPD_EINVAL;
-    if (rows < 0 || A.n < 0 || A.n > (1 << 30)) return SPD_EINVAL;
+    if (rows < 0 || rows > (1 << 23) || A.n < 0 || A.n > (1 << 30)) return SPD_EINVAL;
     if (!A.x || !A.codes || !A.scales || A.ld_x < width || A.ld_codes < A.n) return SPD_EINVAL;
     if ((kind == ROW_NORM && !A.gain) || (A.add && A.ld_add < A.n) || (A.sum && A.ld_sum < A.n)) return SPD_EINVAL;
     const uintptr_t es = dtype == SPD_F32 ? 4 : 2;
@@ -722,7 +724,7 @@ size_t spd_q8_matmul_workspace(int32_t rows, int32_t K, int32_t N) {
 
 int spd_q8_matmul(int32_t rows, int32_t K, int32_t N, const int8_t *codes, int64_t ld_codes, const float *scales, const void *packed,
                   int32_t out_dtype, const void *add, int64_t ld_add, void *out, int64_t ld_out, void *workspace, void *stream) {
-    if (rows < 0 || rows > (1 << 30) || !spd_q8_weight_bytes(K, N) || (int64_t)rows * N > (int64_t)1 << 38) return SPD_EINVAL;
+    if (rows < 0 || rows > (1 << 28) || !spd_q8_weight_bytes(K, N) || (int64_t)rows * N > (int64_t)1 << 38) return SPD_EINVAL;
     if (out_dtype != SPD_F32 && out_dtype != SPD_BF16 && out_dtype != SPD_F16) return SPD_EINVAL;
     if (!codes || !scales || !packed || !out || ((uintptr_t)codes & 15) || ((uintptr_t)packed & 255) || ((uintptr_t)scales & 3)) return SPD_EINVAL;
     if (ld_codes % 16 || ld_codes < (K + 15) / 16 * 16 || ld_out < N || (add && ld_add < N)) return SPD_EINVAL;

@@ -242,6 +242,25 @@ def test_q8_pack_rejects():
     assert B.spd_q8_weight_bytes(0, 4) == 0 and B.spd_q8_weight_bytes(B.SPD_Q8_MAX_K + 1, 4) == 0
 
 
+def test_tensors_that_are_not_on_the_device_are_refused(pages):
+    cfg, ctx = pages()
+    x, codes, scales = torch.zeros(2, 16), torch.zeros(2, 16, dtype=torch.int8), torch.zeros(2)
+    B.lib()
+    for call in (lambda: B.spd_q8_rows(x, codes, scales), lambda: B.spd_q8_norm(x, None, torch.ones(16), 1e-5, None, codes, scales),
+                 lambda: B.spd_q8_swiglu(x, codes[:, :8], scales),
+                 lambda: B.spd_q8_matmul(codes, scales, torch.zeros(B.spd_q8_weight_bytes(16, 16), dtype=torch.uint8), 16, None, x)):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+
+
+def test_every_workspace_keeps_the_counters_place(pages):
+    """Chunks alone, cut into items: the partial results begin behind the counters, which a plan of single tokens shares."""
+    cfg, ctx = pages()
+    chunk = B.spd_pages_plan_get_info(ctx, B.spd_pages_plan(ctx, [900], [60], [list(range(30))])).workspace_bytes
+    rows, heads, d = 128, cfg.n_kv_heads, cfg.head_dim
+    assert chunk > 0 and (chunk - 16384 * 4) % (rows * heads * (d + 2) * 4) == 0
+
+
 # ------------------------------------------------------------------------------------------ GPU: pages
 
 KINDS = [(B.SPD_BF16, B.SPD_E4M3), (B.SPD_F16, B.SPD_E4M3), (B.SPD_BF16, B.SPD_BF16), (B.SPD_F16, B.SPD_F16)]
@@ -558,6 +577,47 @@ def test_step_on_another_stream_in_a_graph_and_twice(gpu):
 
 
 @gpu_test
+def test_one_workspace_for_several_plans(gpu):
+    cfg = config(page=16, n_pages=200)
+    steps = [Step(gpu, cfg, p, n, seed=9) for p, n in (([900], [60]), ([1000], [1]), ([640, 900], [33, 1]))]
+    wants = []
+    for step in steps:
+        step.write()
+        wants.append(step.attend())
+    shared = torch.zeros(max(s.plan.workspace_bytes for s in steps), dtype=torch.uint8, device=gpu)
+    for i in (0, 1, 2, 1, 0, 2, 1):
+        step, out = steps[i], torch.full_like(wants[i], float("nan"))
+        B.spd_pages_attention(step.dp.ctx, step.plan, step.q, step.dp.pool, out, shared)
+        assert torch.equal(out, wants[i])
+
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("up", [True, False])
+def test_scores_that_rise_and_fall_along_the_keys(gpu, dtype, cache, up):
+    """Maxima that grow by far more than a tile's room, or not at all after the first tile."""
+    cfg = config(q=4, kv=2, page=16, n_pages=60, dtype=dtype, cache=cache)
+
+    def spoil(step, past):
+        n = past.shape[0]
+        k = past[:, 4 * 128:6 * 128]
+        k *= torch.linspace(0.1, 8.0, n).flip(0 if not up else []).to(past.dtype)[:, None]
+    step = Step(gpu, cfg, [400, 390], [90, 1], seed=3, spoil=spoil)
+    step.write()
+    q = (step.q.float() * 4).to(step.q.dtype)
+    got = step.attend(q).cpu().double()
+    want, mag = reference(step, q.cpu(), step.dp.pool.cpu())
+    # scores of up to s in units of e: sums of 128 products in fp32 (at most 16 of them one after the other) and three factors move them by
+    # 20 u s, and a probability by as much
+    k = torch.cat([held(cfg, step.dp.pool.cpu(), step.table, b, step.ends[b])[0].flatten(0, 1) for b in range(2)])
+    s = float(q.float().cpu().view(-1, 128).norm(dim=-1).max() * k.norm(dim=-1).max()) / math.sqrt(128)
+    t = T16[dtype]
+    rounded = U[torch.bfloat16] if cache == B.SPD_E4M3 else U[t]
+    bound = (rounded * 1.01 + 2 * 20 * U32 * s + 2e-5) * mag + U[t] * want.abs() * 1.01 + 2.0 ** -24
+    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).max())
+
+
+@gpu_test
 def test_empty_steps(gpu):
     cfg = config()
     dp = B.DevicePages(cfg, gpu)
@@ -654,6 +714,8 @@ def test_rows_strides_aliases_and_edges(gpu):
     B.spd_q8_norm(x.to(gpu), None, torch.ones(64, device=gpu), 1e-5, None, codes, scales)
     assert torch.equal(torch.isnan(scales.cpu()), bad)
     assert not codes[0].any()
+    B.spd_q8_norm(x.to(gpu), None, torch.ones(64, device=gpu), 0.0, None, codes, scales)      # 0 / 0
+    assert bool(torch.isnan(scales[0])) and not codes[0].any()
     B.spd_q8_swiglu(torch.cat([x, x], 1).to(gpu), codes, scales)
     assert torch.isnan(scales.cpu())[3:5].all() and not torch.isnan(scales.cpu())[:2].any()
 
