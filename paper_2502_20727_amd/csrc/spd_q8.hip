@@ -366,34 +366,43 @@ __global__ void __launch_bounds__(512) k_q8_skinny(Q8Args A) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Many rows: tiles of WN TI n-tiles x WM TJ m-tiles through the LDS, NST stages of two k-tiles, copied there directly.  Copies go through
-// buffer descriptors of the tile's panels; rows and inputs past the matrix repeat its last ones.  A step is two sub-steps, one per k-tile:
-// while the MFMAs of one run, the fragments of the next are read between them, and in the second one the copies of the stage
-// NST steps ahead go out; the one barrier of a step lies between them.  The results leave through the LDS in whole cache lines: stored as
+// Many rows: tiles of WN TI n-tiles x WM TJ m-tiles through the LDS, NST stages of KPS k-tiles, copied there directly.  Copies go through
+// buffer descriptors of the tile's panels; rows and inputs past the matrix repeat its last ones.  While the MFMAs of a k-tile run, the fragments of
+// the next are read between them.  KPS 2: a step is two k-tiles with a barrier between them, and in the second one the copies of the stage NST
+// steps ahead go out.  KPS 1: a barrier per k-tile, the copies go out five k-tiles ahead.  Two k-tiles of a row of codes are a cache line, which
+// KPS 2 copies at once and KPS 1 twice: it pays from K 7168 on, where far rows (K a multiple of 4096 above all) answer late.  2000 rows, N 7168, us
+// with KPS 2 / 1: K 2048 33.1 / 33.9, 5120 69.0 / 69.6, 7168 100 / 94, 8192 120 / 107, 8256 111 / 109, 16384 244 / 209; K 1728 25.5 / 29.1.
+// The results leave through the LDS in whole cache lines: stored as
 // they lie in the registers (32 bytes a row and store) they took 2.2 times as long as K = 1024 did beside them (8192 rows, N 8192: 146 us a
-// call, now 79).  8192 rows, K 8192, N 7168: 428 us, 2.25 P operations a second; between the ends of a round the matrix cores do 2.6.
-// (A workgroup that goes on with its next tile's copies before it stores needs its descriptors in vector registers: 559.)
+// call, now 79).  8192 rows, K 8192, N 7168: 414 us, 2.32 P operations a second (torch's library product of 8-bit integers: 400).  Bound by
+// the copies beside the MFMAs: 8192 cubed takes 472 us, without the copies 348, and all workgroups at one tile, out of the L2, 456; MFMAs
+// alone run at 3.55 P a second.  (A workgroup that goes on with its next tile's copies before it stores needs its descriptors in vector
+// registers: 559 us; four waves of 128 x 128 each, a third less read from the LDS: 445 beside 431; copies of the waves at different MFMAs: 426 to 496.)
 // ------------------------------------------------------------------------------------------
 struct Q8Big {       // 256 x 256
-    static constexpr int WN = 4, WM = 2, TI = 4, TJ = 8, NST = 2;
+    static constexpr int WN = 4, WM = 2, TI = 4, TJ = 8, KPS = 2, NST = 2;
 };
+struct Q8Deep {      // the same for a long K: copies four k-tiles ahead instead of two
+    static constexpr int WN = 4, WM = 2, TI = 4, TJ = 8, KPS = 1, NST = 5;
+};
+constexpr int Q8_DEEP_KT = 112;
 struct Q8Half {      // 256 x 128
-    static constexpr int WN = 4, WM = 2, TI = 4, TJ = 4, NST = 3;
+    static constexpr int WN = 4, WM = 2, TI = 4, TJ = 4, KPS = 2, NST = 3;
 };
 struct Q8Square {    // 128 x 128
-    static constexpr int WN = 4, WM = 2, TI = 2, TJ = 4, NST = 4;
+    static constexpr int WN = 4, WM = 2, TI = 2, TJ = 4, KPS = 2, NST = 4;
 };
 struct Q8Small {     // 128 x 64, two workgroups per compute unit
-    static constexpr int WN = 4, WM = 2, TI = 2, TJ = 2, NST = 3;
+    static constexpr int WN = 4, WM = 2, TI = 2, TJ = 2, KPS = 2, NST = 3;
 };
 constexpr int waitcnt_imm(int vm, int lgkm) { return (vm & 15) | ((vm >> 4) << 14) | (7 << 4) | (lgkm << 8); }
 
 template <class T, class G>
 __global__ void __launch_bounds__(G::WN *G::WM * 64, 1) k_q8_gemm(Q8Args A, spd_tile_order ord, int tile0, int n_tiles, int msub) {
-    constexpr int TI = G::TI, TJ = G::TJ, NST = G::NST, NW = G::WN * G::WM, BN = G::WN * TI, BM = G::WM * TJ;
-    constexpr int W_BYTES = BN * 2048, STAGE = W_BYTES + BM * 2048;
-    constexpr int CW = BN * 2 / NW, CX = BM * 2 / NW, NCP = CW + CX;
-    static_assert(BN * 2 % NW == 0 && BM * 2 % NW == 0 && (NST - 1) * NCP < 64, "tile shape");
+    constexpr int TI = G::TI, TJ = G::TJ, NST = G::NST, KPS = G::KPS, NW = G::WN * G::WM, BN = G::WN * TI, BM = G::WM * TJ;
+    constexpr int W_BYTES = BN * KPS * 1024, STAGE = W_BYTES + BM * KPS * 1024;
+    constexpr int CW = BN * KPS / NW, CX = BM * KPS / NW, NCP = CW + CX;
+    static_assert(BN * KPS % NW == 0 && BM * KPS % NW == 0 && (NST - 1) * NCP < 64, "tile shape");
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % G::WN, wm = wave / G::WN;
@@ -420,35 +429,35 @@ __global__ void __launch_bounds__(G::WN *G::WM * 64, 1) k_q8_gemm(Q8Args A, spd_
     unsigned wsrc[CW], xoff[CX];             // (wsrc: wave-uniform)
 #pragma unroll
     for (int n = 0; n < CW; ++n) {
-        const int t = (wave * CW + n) / 2;
+        const int t = (wave * CW + n) / KPS;
         wsrc[n] = (unsigned)(t < n_rows ? t : n_rows - 1) * pitch;
     }
 #pragma unroll
     for (int n = 0; n < CX; ++n) {
-        const int m = ((wave * CX + n) / 2) * 16 + r;
+        const int m = ((wave * CX + n) / KPS) * 16 + r;
         xoff[n] = (unsigned)(m < m_rows ? m : m_rows - 1) * (unsigned)A.ld_codes + 16 * g;
     }
     i32x4 acc[TI][TJ];
     auto copy1 = [&](int st, int slot, int n) __attribute__((always_inline)) {
         if (n < CW) {
-            int kt = 2 * st + ((wave * CW + n) & 1);
-            kt = kt < KT ? kt : KT - 1;
+            int kt = KPS * st + (wave * CW + n) % KPS;
+            if constexpr (KPS > 1) kt = kt < KT ? kt : KT - 1;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(wbuf, (__attribute__((address_space(3))) void *)(lds + slot * STAGE + (wave * CW + n) * 1024), 16,
-                                                     l16, (int)(wsrc[n] + kt * 1024), 0, 0);
+                                                     l16, __builtin_amdgcn_readfirstlane((int)(wsrc[n] + kt * 1024)), 0, 0);
         } else {
             const int c = n - CW;
-            int kt = 2 * st + ((wave * CX + c) & 1);
-            kt = kt < KT ? kt : KT - 1;
+            int kt = KPS * st + (wave * CX + c) % KPS;
+            if constexpr (KPS > 1) kt = kt < KT ? kt : KT - 1;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(xbuf, (__attribute__((address_space(3))) void *)(lds + slot * STAGE + W_BYTES + (wave * CX + c) * 1024),
                                                      16, (int)(xoff[c] + (kt == KT - 1 ? tail : 0)), kt * 64, 0, 0);
         }
     };
-    const char *a_base = lds + wn * TI * 2048 + l16, *b_base = lds + W_BYTES + wm * TJ * 2048 + l16;
+    const char *a_base = lds + wn * TI * KPS * 1024 + l16, *b_base = lds + W_BYTES + wm * TJ * KPS * 1024 + l16;
     auto read1 = [&](int slot, int p, int f, i32x4(&a)[TI], i32x4(&b)[TJ]) __attribute__((always_inline)) {
-        if (f < TJ) b[f] = *(const i32x4 *)(b_base + slot * STAGE + (2 * f + p) * 1024);
-        else a[f - TJ] = *(const i32x4 *)(a_base + slot * STAGE + ((f - TJ) * 2 + p) * 1024);
+        if (f < TJ) b[f] = *(const i32x4 *)(b_base + slot * STAGE + (KPS * f + p) * 1024);
+        else a[f - TJ] = *(const i32x4 *)(a_base + slot * STAGE + ((f - TJ) * KPS + p) * 1024);
     };
-    const int n_stages = (KT + 1) / 2, n_steps = KT / 2;
+    const int n_stages = (KT + KPS - 1) / KPS, n_steps = KT / 2;
     auto first_copies = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int st = 0; st < NST; ++st)
@@ -461,7 +470,7 @@ __global__ void __launch_bounds__(G::WN *G::WM * 64, 1) k_q8_gemm(Q8Args A, spd_
     auto substep = [&](auto copy_, const i32x4(&a)[TI], const i32x4(&b)[TJ], i32x4(&an)[TI], i32x4(&bn)[TJ], int rslot, int rp, int cst,
                        int cslot) __attribute__((always_inline)) {
         constexpr int NR = TI + TJ, NM = TI * TJ;
-        constexpr bool COPY = decltype(copy_)::value;
+        const bool copy = copy_;                 // (a constant, or uniform)
         int f = 0, cp = 0;
 #pragma unroll
         for (int i = 0; i < TI; ++i)
@@ -471,7 +480,10 @@ __global__ void __launch_bounds__(G::WN *G::WM * 64, 1) k_q8_gemm(Q8Args A, spd_
                 acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[j], acc[i][j], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 while (f < NR && n >= (2 * NR <= NM ? 2 * f : f * NM / NR)) read1(rslot, rp, f++, an, bn);
-                while (COPY && cp < NCP && n >= (NM >= NCP ? cp * (NM / NCP) : cp * NM / NCP)) copy1(cst, cslot, cp++);
+                while (cp < NCP && n >= (NM >= NCP ? cp * (NM / NCP) : cp * NM / NCP)) {
+                    if (copy) copy1(cst, cslot, cp);
+                    ++cp;
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
     };
@@ -488,21 +500,42 @@ __global__ void __launch_bounds__(G::WN *G::WM * 64, 1) k_q8_gemm(Q8Args A, spd_
 #pragma unroll
     for (int f = 0; f < TI + TJ; ++f) read1(0, 0, f, a0, b0);
     int slot = 0;
-    auto step = [&](auto copy_, int s) __attribute__((always_inline)) {
-        constexpr bool COPY = decltype(copy_)::value;
-        const int next = slot + 1 == NST ? 0 : slot + 1;
-        substep(std::false_type(), a0, b0, a1, b1, slot, 1, 0, 0);
-        // the next stage's copies of this wave have landed, every read of the current stage is done
-        __builtin_amdgcn_s_waitcnt(waitcnt_imm(COPY ? (NST - 2) * NCP : 0, 0));
-        asm volatile("s_barrier" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        substep(copy_, a1, b1, a0, b0, next, 0, s + NST, slot);      // (in the last step: fragments read and never used)
-        slot = next;
-    };
-    int s = 0;
-    for (; s + NST < n_stages; ++s) step(std::true_type(), s);
-    for (; s < n_steps; ++s) step(std::false_type(), s);
-    if (KT & 1) {                            // the odd k-tile on its own (its fragments are read already)
+    if constexpr (KPS == 1) {
+        // One k-tile: the copies of the next one have landed in every wave, and every wave holds the fragments of this one.  (Copies are left out by
+        // branches: steps of their own without them double the code, and the accumulators do not survive it in registers.)
+        auto step = [&](const i32x4(&a)[TI], const i32x4(&b)[TJ], i32x4(&an)[TI], i32x4(&bn)[TJ], int s) __attribute__((always_inline)) {
+            const int next = slot + 1 == NST ? 0 : slot + 1;
+            const bool more = s + NST < KT;
+            if (more) __builtin_amdgcn_s_waitcnt(waitcnt_imm((NST - 2) * NCP, 0));
+            else __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
+            asm volatile("s_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            substep(more, a, b, an, bn, next, 0, s + NST, slot);      // (in the last step: fragments read and never used)
+            slot = next;
+        };
+        for (int s = 0;;) {
+            step(a0, b0, a1, b1, s);
+            if (++s == KT) break;
+            step(a1, b1, a0, b0, s);
+            if (++s == KT) break;
+        }
+    } else {
+        auto step = [&](auto copy_, int s) __attribute__((always_inline)) {
+            constexpr bool COPY = decltype(copy_)::value;
+            const int next = slot + 1 == NST ? 0 : slot + 1;
+            substep(std::false_type(), a0, b0, a1, b1, slot, 1, 0, 0);
+            // the next stage's copies of this wave have landed, every read of the current stage is done
+            __builtin_amdgcn_s_waitcnt(waitcnt_imm(COPY ? (NST - 2) * NCP : 0, 0));
+            asm volatile("s_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            substep(copy_, a1, b1, a0, b0, next, 0, s + NST, slot);      // (in the last step: fragments read and never used)
+            slot = next;
+        };
+        int s = 0;
+        for (; s + NST < n_stages; ++s) step(std::true_type(), s);
+        for (; s < n_steps; ++s) step(std::false_type(), s);
+    }
+    if (KPS == 2 && (KT & 1)) {                            // the odd k-tile on its own (its fragments are read already)
 #pragma unroll
         for (int i = 0; i < TI; ++i)
 #pragma unroll
@@ -619,7 +652,7 @@ hipError_t launch_skinny(const Q8Args &A, hipStream_t s) {
 // tiles tile0 .. of the order of tiles msub times as high as G's
 template <class T, class G>
 hipError_t launch_gemm(const Q8Args &A, hipStream_t s, int tile0 = 0, int n_tiles = -1, int msub = 1) {
-    constexpr int BN = G::WN * G::TI, BM = G::WM * G::TJ, LDS = G::NST * (BN + BM) * 2048;
+    constexpr int BN = G::WN * G::TI, BM = G::WM * G::TJ, LDS = G::NST * (BN + BM) * G::KPS * 1024;
     static_assert(LDS <= 160 * 1024, "the stages must fit the LDS of a compute unit");
     static std::once_flag once;
     static hipError_t attr = hipSuccess;
@@ -666,9 +699,15 @@ Q8Kind q8_pick(int rows, int N, int KT, int64_t ld_codes) {
     offer(Q8_SQUARE, rounds(tiles(8, 8)) * (k * 38 + 2.7));
     offer(Q8_HALF, rounds(tiles(16, 8)) * (k * 63 + 4));
     const int64_t big = tiles(16, 16);
-    offer(Q8_BIG, rounds(big) * (k * 104 + 8));
-    if (big > 256 && big % 256) offer(Q8_BIG_HALF, (double)(big / 256) * (k * 104 + 8) + rounds(2 * (big % 256)) * (k * 63 + 4));
+    const double round = k * (KT >= Q8_DEEP_KT ? 98 : 104) + 8;
+    offer(Q8_BIG, rounds(big) * round);
+    if (big > 256 && big % 256) offer(Q8_BIG_HALF, (double)(big / 256) * round + rounds(2 * (big % 256)) * (k * 63 + 4));
     return best;
+}
+
+template <class T>
+hipError_t launch_big(const Q8Args &A, hipStream_t s, int tile0 = 0, int n_tiles = -1) {
+    return A.KT >= Q8_DEEP_KT ? launch_gemm<T, Q8Deep>(A, s, tile0, n_tiles) : launch_gemm<T, Q8Big>(A, s, tile0, n_tiles);
 }
 
 template <class T>
@@ -685,10 +724,10 @@ hipError_t launch_product(const Q8Args &A, hipStream_t s) {
         case Q8_SMALL: return launch_gemm<T, Q8Small>(A, s);
         case Q8_SQUARE: return launch_gemm<T, Q8Square>(A, s);
         case Q8_HALF: return launch_gemm<T, Q8Half>(A, s);
-        case Q8_BIG: return launch_gemm<T, Q8Big>(A, s);
+        case Q8_BIG: return launch_big<T>(A, s);
         case Q8_BIG_HALF: {
             const int big = ((A.NT + 15) / 16) * (int)(((int64_t)A.rows + 255) / 256), rest = big % 256;
-            const hipError_t e = launch_gemm<T, Q8Big>(A, s, 0, big - rest);
+            const hipError_t e = launch_big<T>(A, s, 0, big - rest);
             return e != hipSuccess ? e : launch_gemm<T, Q8Half>(A, s, big - rest, rest, 2);
         }
     }

@@ -767,6 +767,24 @@ def test_product_of_the_longest_contraction(gpu, rows, N):
 
 
 @gpu_test
+@pytest.mark.parametrize("rows,K,N,t,add", [(2100, 7201, 4100, "f32", False), (4500, 7232, 4104, "bf16", True), (2050, 7168, 4111, "f16", False)])
+def test_product_of_many_rows_and_a_long_contraction(gpu, rows, K, N, t, add):
+    t, g = TYPES[t], torch.Generator(device=gpu).manual_seed(rows)
+    a = torch.randint(-127, 128, (rows, (K + 15) // 16 * 16), generator=g, device=gpu).to(torch.int8)
+    w = torch.randint(-127, 128, (K, N), generator=g, device=gpu).to(torch.int8)
+    sa, sw = 0.01 + torch.rand(rows, generator=g, device=gpu), 1e-3 * (0.01 + torch.rand(N, generator=g, device=gpu))
+    y = torch.randn(rows, N, generator=g, device=gpu).to(t) * 100 if add else None
+    packed = torch.from_numpy(B.spd_q8_pack_codes(w.cpu().numpy(), sw.cpu().numpy())).to(gpu)
+    out = torch.empty(rows, N, dtype=t, device=gpu)
+    B.spd_q8_matmul(a[:, :K], sa, packed, N, y, out)
+    p = (a[:, :K].double() @ w.double()) * sa.double()[:, None] * sw.double()      # (whole numbers far below 2^53: exact)
+    want = p + (y.double() if add else 0)
+    bound = 4 * U32 * p.abs() + 2 * U32 * want.abs() + U[t] * want.abs() * 1.0001 + 2.0 ** -25
+    fits = want.abs() < torch.finfo(t).max
+    assert bool(((out.double() - want).abs() <= bound)[fits].all())
+
+
+@gpu_test
 def test_product_adds_in_place_and_keeps_its_bits(gpu):
     for rows in (5, 40, 300, 1000):
         K, N = 700, 530
