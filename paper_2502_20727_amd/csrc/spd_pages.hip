@@ -731,6 +731,11 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) put_away(c, stage[0]);
     put_scales(stage[0]);
+    // (a tile is asked for as soon as the registers of the one before are put away: the scores' time and half of the outputs' to arrive in)
+    if (4 < it.count) {
+        fetch(4, page);
+        page = page_of(P, s, my_block(8));
+    }
     __syncthreads();
     // Operands and scales are read from the LDS some instructions ahead of their use, fenced so that the compiler leaves them there (read
     // where they are used, a wave waits for the LDS 24 times a tile).
@@ -812,11 +817,6 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         bool grown = false;
         do {
             const Stage &now = stage[turn];
-            const bool more = v0 + 4 < it.count;
-            if (more) {
-                fetch(v0 + 4, page);
-                page = page_of(P, s, my_block(v0 + 8));
-            }
             i32x4 pf[4];
             float ps = 0.f, w[2];
             // element i (of 32) of the scores: its power of two, with the value's scale, a pair at a time into the operand
@@ -849,6 +849,11 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
             }
             l += ps;                             // (of the lane's half of the keys)
             put_scales(stage[turn ^ 1]);
+            if (v0 + 8 < it.count) {
+                fetch(v0 + 8, page);
+                page = page_of(P, s, my_block(v0 + 12));
+            }
+            __builtin_amdgcn_sched_barrier(0);
             __syncthreads();
             v0 += 4;
             turn ^= 1;
