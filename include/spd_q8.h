@@ -128,8 +128,8 @@ int spd_pages_read(const spd_pages *pages, const void *plan_host, const void *pl
  *   q, out     [tokens][ld_q], [tokens][ld_out] in the pool's dtype, 16-byte aligned, strides multiples of 8.  out may not overlap q.
  *   workspace  workspace_bytes of the plan, 256-byte aligned; may be NULL when that is 0.  One per stream, of use to any plan that
  *              it is large enough for, zero-filled once before its first use (calls leave its counters at zero).
- * Sums, maxima and outputs are kept in fp32; probabilities (times the value's scale) are rounded to 16 bits
- * for the second product (bf16 where values are e4m3). */
+ * Sums, maxima and outputs are kept in fp32; probabilities (times the value's scale) are rounded to the pool's dtype
+ * for the second product, in fp16 beside e4m3 relative to the largest of these products. */
 int spd_pages_attention(const spd_pages *pages, const void *plan_host, const void *plan_dev, const void *q, int64_t ld_q,
                         const void *pool, void *out, int64_t ld_out, void *workspace, void *stream);
 

@@ -426,8 +426,9 @@ __device__ __forceinline__ float2 part_get(const float *p) {
 template <int D, bool E4M3, bool F16>
 __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
     constexpr int DT = D / 16, NF = D / 32, NW = SPD_SMALL_WAVES;
-    typedef Half<F16> QK;                        // queries and keys
-    typedef Half<F16 && !E4M3> PV;               // probabilities (times a scale that may be tiny: bf16 beside e4m3) and values
+    typedef Half<F16> H;
+    // fp16 has no room for a probability times a scale that may be tiny: there the maximum kept is that of the product, log2(scale) added to the score
+    constexpr bool PRODUCT = F16 && E4M3;
     const Pages &P = A.P;
     const int head = blockIdx.x % P.kv;
     const spd_plan_item it = ((const spd_plan_item *)(P.plan + P.list))[blockIdx.x / P.kv];
@@ -477,14 +478,14 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
         for (int i = 0; i < NF; ++i) {
             i32x4 k0, k1;
             if constexpr (E4M3) {
-                k0 = QK::widen(x0.k[i >> 1][2 * (i & 1)], x0.k[i >> 1][2 * (i & 1) + 1]);
-                k1 = QK::widen(x1.k[i >> 1][2 * (i & 1)], x1.k[i >> 1][2 * (i & 1) + 1]);
+                k0 = H::widen(x0.k[i >> 1][2 * (i & 1)], x0.k[i >> 1][2 * (i & 1) + 1]);
+                k1 = H::widen(x1.k[i >> 1][2 * (i & 1)], x1.k[i >> 1][2 * (i & 1) + 1]);
             } else {
                 k0 = x0.k[i];
                 k1 = x1.k[i];
             }
-            s0 = QK::mfma16(k0, qf[i], s0);
-            s1 = QK::mfma16(k1, qf[i], s1);
+            s0 = H::mfma16(k0, qf[i], s0);
+            s1 = H::mfma16(k1, qf[i], s1);
         }
         f32x4 v0 = x0.vs, v1 = x1.vs;
 #pragma unroll
@@ -506,7 +507,14 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
                 }
             }
         }
-        float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+        float mx = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // (a hidden key's score is -inf, whatever log2 makes of its scale of 0)
+            const float a0 = PRODUCT ? s0[i] + __builtin_amdgcn_logf(fmaxf(v0[i], 0x1p-120f)) : s0[i],
+                        a1 = PRODUCT ? s1[i] + __builtin_amdgcn_logf(fmaxf(v1[i], 0x1p-120f)) : s1[i];
+            mx = fmaxf(mx, fmaxf(a0, a1));
+        }
         const float m_new = fmaxf(m, quad_max(mx)), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(m - m_use);
         float ps = 0.f, w0[4], w1[4];
@@ -519,13 +527,13 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
         }
         l = l * alpha + ps;                      // (of the lane's keys; the four lanes of a row meet at the end)
         m = m_new;
-        const i32x4 pf = {PV::pack(w0[0], w0[1]), PV::pack(w0[2], w0[3]), PV::pack(w1[0], w1[1]), PV::pack(w1[2], w1[3])};
+        const i32x4 pf = {H::pack(w0[0], w0[1]), H::pack(w0[2], w0[3]), H::pack(w1[0], w1[1]), H::pack(w1[2], w1[3])};
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
             i32x4 vf;
-            if constexpr (E4M3) vf = PV::widen(x0.v[t >> 2][t & 3], x1.v[t >> 2][t & 3]);
+            if constexpr (E4M3) vf = H::widen(x0.v[t >> 2][t & 3], x1.v[t >> 2][t & 3]);
             else vf = (i32x4){x0.v[t >> 1][2 * (t & 1)], x0.v[t >> 1][2 * (t & 1) + 1], x1.v[t >> 1][2 * (t & 1)], x1.v[t >> 1][2 * (t & 1) + 1]};
-            o[t] = PV::mfma16(vf, pf, o[t] * alpha);
+            o[t] = H::mfma16(vf, pf, o[t] * alpha);
         }
     };
     if (mine > 0) {
@@ -646,7 +654,7 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
     int *to = (int *)(A.out + (int64_t)(s.tok0 + mr / P.group) * A.ld_out + (int64_t)(head * P.group + mr % P.group) * D + f0);
     const float inv = 1.f / ll;
 #pragma unroll
-    for (int i = 0; i < N; i += 2) to[i / 2] = QK::pack(acc[i] * inv, acc[i + 1] * inv);
+    for (int i = 0; i < N; i += 2) to[i / 2] = H::pack(acc[i] * inv, acc[i + 1] * inv);
 }
 
 // Many rows (a prompt's chunk): one workgroup per 128 rows and KV head; each wave has 32 of them, tiles of 64 keys go through the LDS in 16
@@ -658,8 +666,8 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
 template <int D, bool E4M3, bool F16>
 __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     constexpr int W = E4M3 ? 1 : 2, KS = D / 16, DT = D / 32, CH = E4M3 ? D / 64 : D / 32;
-    typedef Half<F16> QK;
-    typedef Half<F16 && !E4M3> PV;
+    typedef Half<F16> H;
+    constexpr bool PRODUCT = F16 && E4M3;        // the maximum kept is that of probability times scale, as in the kernel for few rows
     const Pages &P = A.P;
     const int head = blockIdx.x % P.kv;
     const spd_plan_item it = ((const spd_plan_item *)(P.plan + P.list))[blockIdx.x / P.kv];
@@ -675,7 +683,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     // keys: [block][feature / 8][position][8]; values: [block][feature / 16][half][feature % 16][8 positions of the half]
     struct Stage {
         short k[64 * D], v[64 * D];
-        float ks[64], vs[64];      // (of the keys: times the softmax's scale)
+        float ks[64], vs[64], lv[PRODUCT ? 64 : 4];      // e4m3: the keys' scales times the softmax's; the values', and their log2
     };
     __shared__ __attribute__((aligned(16))) Stage stage[2];
     i32x4 qf[KS];
@@ -715,12 +723,12 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     auto put_away = [&](int c, Stage &to) __attribute__((always_inline)) {
         short *kd = to.k + wave * 16 * D, *vd = to.v + wave * 16 * D;
         if constexpr (E4M3) {
-            *(i32x4 *)(kd + ((8 * c + 2 * g) * 16 + r16) * 8) = QK::widen(kx[c][0], kx[c][1]);
-            *(i32x4 *)(kd + ((8 * c + 2 * g + 1) * 16 + r16) * 8) = QK::widen(kx[c][2], kx[c][3]);
+            *(i32x4 *)(kd + ((8 * c + 2 * g) * 16 + r16) * 8) = H::widen(kx[c][0], kx[c][1]);
+            *(i32x4 *)(kd + ((8 * c + 2 * g + 1) * 16 + r16) * 8) = H::widen(kx[c][2], kx[c][3]);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 *(i32x2 *)(vd + (((4 * c + t) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) =
-                    (i32x2){PV::template from_e4m3<false>(vx[c][t]), PV::template from_e4m3<true>(vx[c][t])};
+                    (i32x2){H::template from_e4m3<false>(vx[c][t]), H::template from_e4m3<true>(vx[c][t])};
         } else {
             // Scales are 1, or NaN for a row that was not finite: its key becomes NaN, so that its score is, and its codes are zero
             const bool bad = !(sx + sv < 3.f);
@@ -732,10 +740,11 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     };
     auto put_scales = [&](Stage &to) __attribute__((always_inline)) {
         if constexpr (!E4M3) return;
-        // a value that is NaN makes its key's score NaN, and nothing else: whoever sees it gets NaN, others multiply by 0
+        // a value that is NaN makes its key's score NaN, and nothing else: whoever sees it gets NaN
         const float vs = __shfl(sx, r16 + 16, 64);
-        if (lane < 16) to.ks[wave * 16 + r16] = vs == vs ? sx * A.scale : vs;
-        else if (lane < 32) to.vs[wave * 16 + r16] = vs == vs ? vs : 0.f;
+        if (g == 0) to.ks[wave * 16 + r16] = vs == vs ? sx * A.scale : vs;
+        else if (g == 1) to.vs[wave * 16 + r16] = vs == vs ? vs : 0.f;
+        else if (PRODUCT && g == 2) to.lv[wave * 16 + r16] = vs == vs ? __builtin_amdgcn_logf(fmaxf(vs, 0x1p-120f)) : 0.f;
     };
     int page = page_of(P, s, my_block(0));
     fetch(0, page);
@@ -754,7 +763,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     constexpr int AHEAD = 4;
     const int k_lane = (col >> 4) * 16 * D + (half * 16 + (col & 15)) * 8, v_lane = (((col >> 4) * 2 + half) * 16 + (col & 15)) * 8;
     i32x4 ring[AHEAD];
-    f32x4 ks[4], vs[4];
+    f32x4 ks[4], vs[4], lv[2];      // (lv: this group of four and the next; there are no registers for more)
     f32x16 sc[2];
     int v0 = 0, turn = 0;
     // Scores of tile v0, which lies in stage `turn`, and their maximum over the row: score i of half h is of block 2 h + i / 8, position
@@ -771,17 +780,21 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int n = 0; n < 2 * KS; ++n) {
-            sc[n / KS] = QK::mfma32(ring[n % AHEAD], qf[n % KS], sc[n / KS]);
+            sc[n / KS] = H::mfma32(ring[n % AHEAD], qf[n % KS], sc[n / KS]);
             __builtin_amdgcn_sched_barrier(0);
             if (n + AHEAD < 2 * KS) ring[n % AHEAD] = frag(n + AHEAD);
             if (E4M3 && n < 4) ks[n] = *(const f32x4 *)(now.ks + n * 8 + 4 * half);
+            if (PRODUCT && n >= KS - 2 && n < KS) lv[n - KS + 2] = *(const f32x4 *)(now.lv + (n - KS + 2) * 8 + 4 * half);
             if (n >= KS) {                       // beside the second half's: the first half scaled, and its maximum
                 constexpr int PER = 16 / KS;
 #pragma unroll
                 for (int i = (n - KS) * PER; i < (n - KS + 1) * PER; ++i) {
                     if constexpr (E4M3) sc[0][i] *= ks[i >> 2][i & 3];
-                    mx = fmaxf(mx, sc[0][i]);
-                    if (E4M3 && (i & 3) == 3) ks[i >> 2] = *(const f32x4 *)(now.ks + 32 + (i >> 2) * 8 + 4 * half);
+                    mx = fmaxf(mx, PRODUCT ? sc[0][i] + lv[(i >> 2) & 1][i & 3] : sc[0][i]);
+                    if (E4M3 && (i & 3) == 3) {
+                        ks[i >> 2] = *(const f32x4 *)(now.ks + 32 + (i >> 2) * 8 + 4 * half);
+                        if constexpr (PRODUCT) lv[(i >> 2) & 1] = *(const f32x4 *)(now.lv + ((i >> 2) + 2) * 8 + 4 * half);
+                    }
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -793,7 +806,8 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             if constexpr (E4M3) sc[1][i] *= ks[i >> 2][i & 3];
-            mx = fmaxf(mx, sc[1][i]);
+            mx = fmaxf(mx, PRODUCT ? sc[1][i] + lv[(i >> 2) & 1][i & 3] : sc[1][i]);
+            if (PRODUCT && (i & 3) == 3 && i < 8) lv[(i >> 2) & 1] = *(const f32x4 *)(now.lv + ((i >> 2) + 6) * 8 + 4 * half);
         }
         // is something of the tile hidden from some query of the wave?  (first and last block; a tile of sinks and window blocks is mixed)
         const int n_here = it.count - v0 < 4 ? it.count - v0 : 4;
@@ -803,12 +817,13 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 const int key0 = (q >> 1) < n_here ? list_block(it, it.first + v0 + (q >> 1)) * 16 : 0x7fffff0;
+                const f32x4 ls = *(const f32x4 *)(now.lv + (PRODUCT ? q * 8 + 4 * half : 0));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool seen = visible(key0 + 8 * (q & 1) + 4 * half + i, at, A.window, A.sinks);
                     const float x = seen ? sc[q >> 2][(q & 3) * 4 + i] : -__builtin_inff();
                     sc[q >> 2][(q & 3) * 4 + i] = x;
-                    mx = fmaxf(mx, x);
+                    mx = fmaxf(mx, PRODUCT ? x + ls[i] : x);
                 }
             }
         }
@@ -837,7 +852,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
                 const float x = sc[i >> 4][i & 15], p = __builtin_amdgcn_exp2f(E4M3 ? x - m_use : fmaf(x, A.scale, -m_use));
                 ps += p;
                 w[i & 1] = E4M3 ? p * vs[(i >> 2) & 3][i & 3] : p;
-                if (i & 1) pf[i >> 3][(i & 7) >> 1] = PV::pack(w[0], w[1]);
+                if (i & 1) pf[i >> 3][(i & 7) >> 1] = H::pack(w[0], w[1]);
                 if (E4M3 && (i & 3) == 3 && i < 16) vs[i >> 2] = *(const f32x4 *)(now.vs + 32 + (i >> 2) * 8 + 4 * half);
             };
             const short *vp = now.v + v_lane;
@@ -850,7 +865,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int n = 0; n < 4 * DT; ++n) {
-                o[n % DT] = PV::mfma32(ring[n % AHEAD], pf[n / DT], o[n % DT]);
+                o[n % DT] = H::mfma32(ring[n % AHEAD], pf[n / DT], o[n % DT]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (n + AHEAD < 4 * DT) ring[n % AHEAD] = frag(n + AHEAD);
                 if (n < 2 * DT) {                // beside the first half's outputs: the second half's weights
@@ -888,7 +903,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
                 *(i32x2 *)(mine + col * ROW + 32 * t + 2 * i + 4 * half) =
-                    (i32x2){QK::pack(o[t][i] * inv, o[t][i + 1] * inv), QK::pack(o[t][i + 2] * inv, o[t][i + 3] * inv)};
+                    (i32x2){H::pack(o[t][i] * inv, o[t][i + 1] * inv), H::pack(o[t][i + 2] * inv, o[t][i + 3] * inv)};
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int p = lane; p < 32 * PIECES; p += 64) {

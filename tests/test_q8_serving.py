@@ -577,6 +577,42 @@ def test_step_on_another_stream_in_a_graph_and_twice(gpu):
 
 
 @gpu_test
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("positions,q_lens", [([300, 40], [1, 2]), ([900], [1]), ([200, 0], [70, 40]), ([700], [90])], ids=str)
+@pytest.mark.parametrize("values", ["even", "tiny", "mixed"])
+def test_fp16_beside_e4m3_rounds_to_fp16(gpu, d, positions, q_lens, values):
+    """Probabilities times scales keep fp16's eleven digits, whatever the values' magnitudes."""
+    cfg = config(q=8, kv=2, d=d, page=16, n_pages=80, dtype=B.SPD_F16)
+
+    def spoil(step, past):
+        n = past.shape[0]
+        f = {"even": torch.ones(n), "tiny": torch.full((n,), 3e-4), "mixed": 10.0 ** (torch.arange(n) % 7 - 4.0)}[values]
+        past[:, 10 * d:] *= f[:, None].to(past.dtype)
+    step = Step(gpu, cfg, positions, q_lens, seed=4, spoil=spoil)
+    if values == "tiny":
+        step.qkv[:, 10 * d:] *= 3e-4
+        step.qkv_dev = step.qkv.to(gpu)
+    step.write()
+    got, pool = step.attend().cpu().double(), step.dp.pool.cpu()
+    want, mag = reference(step, step.q.cpu(), pool)
+    # a weight below fp16's normal numbers is off by 2^-25 of the largest weight, which stands for the largest probability times its scale;
+    # times codes of up to 448, over all keys
+    floor, first = torch.zeros_like(want), 0
+    for b, (p, n) in enumerate(zip(positions, q_lens)):
+        k, v = held(cfg, pool, step.table, b, p + n)
+        x = step.q.cpu()[first:first + n].double().view(n, 8, d)
+        hidden = torch.arange(p + n)[None] > torch.arange(p, p + n)[:, None]
+        for h in range(8):
+            w = (x[:, h] @ k[h // 4].t() / math.sqrt(d)).masked_fill(hidden, -math.inf).softmax(-1)
+            most = (w * v[h // 4].abs().amax(-1)).amax(-1)
+            floor[first:first + n, h * d:(h + 1) * d] = ((p + n) * 2.0 ** -25 * most)[:, None]
+        first += n
+    t = torch.float16
+    bound = (U[t] * 1.01 + 2e-5) * mag + U[t] * want.abs() * 1.01 + 2.0 ** -25 + floor
+    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).max())
+
+
+@gpu_test
 def test_one_workspace_for_several_plans(gpu):
     cfg = config(page=16, n_pages=200)
     steps = [Step(gpu, cfg, p, n, seed=9) for p, n in (([900], [60]), ([1000], [1]), ([640, 900], [33, 1]))]
