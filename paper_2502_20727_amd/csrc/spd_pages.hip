@@ -5,7 +5,7 @@
 // O^T = V^T P^T takes.  A "row" is a (token, query head of the KV group) pair, row = token * group + head.
 //
 // A key's scale multiplies its scores in fp32; a value's scale multiplies its probability before that is rounded for the second
-// contraction.  e4m3 codes are exact in bf16 and fp16, so that dequantising rounds nothing.  Hidden keys are taken out by selection after
+// contraction (in fp16, relative to the largest such product).  e4m3 codes are exact in bf16 and fp16, so that dequantising rounds nothing.  Hidden keys are taken out by selection after
 // the scale has been multiplied, and codes in pages are always finite: a NaN scale of a hidden key reaches nothing.
 #include <algorithm>
 #include <cmath>
