@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(256) k_rows_q8(RowArgs A) {
     }
 }
 
-// The same with rows in registers: eight elements per thread and chunk, whole and aligned.  Bound by what is read and written: 8192 rows of
+// The same with rows in registers (up to 16384 elements): eight per thread and chunk.  Bound by what is read and written: 8192 rows of
 // 8192 in 16 bits with a summand, 84 us (470 MB: 5.6 TB/s).
 template <class T>
 struct Eight {
@@ -103,7 +103,29 @@ __device__ __forceinline__ Eight<T> load8(const T *p) {
     return *(const Eight<T> *)__builtin_assume_aligned(p, 16);
 }
 
-template <class T, int KIND, bool ADD, int CH>
+// eight elements wherever they lie (the hardware takes global accesses of any alignment), `there` of them
+template <class T>
+__device__ __forceinline__ Eight<T> load8_any(const T *p, int there) {
+    Eight<T> q;
+    if (there >= 8) __builtin_memcpy(&q, p, sizeof(q));
+    else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q.v[e] = e < there ? p[e] : (T)0.f;
+    }
+    return q;
+}
+template <class T>
+__device__ __forceinline__ void store8_any(T *p, const Eight<T> &q, int there) {
+    if (there >= 8) __builtin_memcpy(p, &q, sizeof(q));
+    else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < there) p[e] = q.v[e];
+    }
+}
+
+// WHOLE: rows are whole chunks, 16-byte aligned.  Otherwise chunks lie anywhere and the last one may be short (its missing elements count as 0).
+template <class T, int KIND, bool ADD, int CH, bool WHOLE>
 __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A) {
     const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const T *x = (const T *)A.x + row * A.ld_x, *add = ADD ? (const T *)A.add + row * A.ld_add : nullptr;
@@ -112,9 +134,15 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int i = at + c * stride < A.n ? at + c * stride : 0;      // (past the row: not used)
-        in[c] = load8(x + i);
-        if constexpr (ADD) in2[c] = load8(add + i);
-        if constexpr (KIND == ROW_SWIGLU) in2[c] = load8(x + A.n + i);
+        if constexpr (WHOLE) {
+            in[c] = load8(x + i);
+            if constexpr (ADD) in2[c] = load8(add + i);
+            if constexpr (KIND == ROW_SWIGLU) in2[c] = load8(x + A.n + i);
+        } else {
+            in[c] = load8_any(x + i, A.n - i);
+            if constexpr (ADD) in2[c] = load8_any(add + i, A.n - i);
+            if constexpr (KIND == ROW_SWIGLU) in2[c] = load8_any(x + A.n + i, A.n - i);
+        }
     }
     float v[CH][8], ss = 0.f, most = 0.f;
     bool fine = true;
@@ -122,7 +150,8 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
     for (int c = 0; c < CH; ++c) {
         if (at + c * stride >= A.n) continue;
         if constexpr (KIND == ROW_NORM) {
-            const Eight<float> gain = load8(A.gain + at + c * stride);
+            const int there = A.n - at - c * stride;
+            const Eight<float> gain = WHOLE ? load8(A.gain + at + c * stride) : load8_any(A.gain + at + c * stride, there);
             Eight<T> out;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -132,7 +161,11 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
                 out.v[e] = (T)s;
                 v[c][e] = s * gain.v[e];
             }
-            if (A.sum) *(Eight<T> *)__builtin_assume_aligned((T *)A.sum + row * A.ld_sum + at + c * stride, 16) = out;
+            T *to = (T *)A.sum + row * A.ld_sum + at + c * stride;
+            if (A.sum) {
+                if constexpr (WHOLE) *(Eight<T> *)__builtin_assume_aligned(to, 16) = out;
+                else store8_any(to, out, there);
+            }
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -180,7 +213,9 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
             lo |= ((unsigned)(int)rintf(v[c][e] * factor * up) & 255u) << (8 * e);
             hi |= ((unsigned)(int)rintf(v[c][4 + e] * factor * up) & 255u) << (8 * e);
         }
-        *(uint2 *)(codes + at + c * stride) = ok ? make_uint2(lo, hi) : make_uint2(0u, 0u);
+        const uint2 q = ok ? make_uint2(lo, hi) : make_uint2(0u, 0u);
+        if constexpr (WHOLE) *(uint2 *)(codes + at + c * stride) = q;
+        else store8_any(codes + at + c * stride, __builtin_bit_cast(Eight<int8_t>, q), A.n - at - c * stride);
     }
 }
 
@@ -188,20 +223,26 @@ template <class T, int KIND, bool ADD>
 hipError_t launch_rows_of(int rows, const RowArgs &A, hipStream_t s) {
     const uintptr_t bits = (uintptr_t)A.x | (uintptr_t)A.add | (uintptr_t)A.sum | (uintptr_t)A.gain;
     const int64_t strides = A.ld_x | A.ld_add | (A.sum ? A.ld_sum : 0) | A.ld_codes;
-    if (A.n % 8 || bits % 16 || strides % 8 || (uintptr_t)A.codes % 8 || A.n > 16384) {
+    if (A.n > 16384) {
         hipLaunchKernelGGL((k_rows_q8<T, KIND, ADD>), dim3(rows), dim3(256), 0, s, A);
         return hipGetLastError();
     }
+    const bool whole = !(A.n % 8 || bits % 16 || strides % 8 || (uintptr_t)A.codes % 8);
     // few rows: as many threads as there are chunks, so that all of a row is asked for at once; many: four chunks a thread
-    const int chunks = A.n / 8, most = rows <= 512 ? 1024 : 256;
+    const int chunks = (A.n + 7) / 8, most = rows <= 512 ? 1024 : 256;
     int threads = 64;
     while (threads < most && threads * (rows <= 512 ? 1 : 4) < chunks) threads *= 2;
     const int each = (chunks + threads - 1) / threads;
-    if (each <= 1) hipLaunchKernelGGL((k_rows_q8_wide<T, KIND, ADD, 1>), dim3(rows), dim3(threads), 0, s, A);
-    else if (each <= 2) hipLaunchKernelGGL((k_rows_q8_wide<T, KIND, ADD, 2>), dim3(rows), dim3(threads), 0, s, A);
-    else if (each <= 4) hipLaunchKernelGGL((k_rows_q8_wide<T, KIND, ADD, 4>), dim3(rows), dim3(threads), 0, s, A);
-    else hipLaunchKernelGGL((k_rows_q8_wide<T, KIND, ADD, 8>), dim3(rows), dim3(threads), 0, s, A);
-    return hipGetLastError();
+    auto launch = [&](auto ch) {
+        constexpr int CH = decltype(ch)::value;
+        if (whole) hipLaunchKernelGGL((k_rows_q8_wide<T, KIND, ADD, CH, true>), dim3(rows), dim3(threads), 0, s, A);
+        else hipLaunchKernelGGL((k_rows_q8_wide<T, KIND, ADD, CH, false>), dim3(rows), dim3(threads), 0, s, A);
+        return hipGetLastError();
+    };
+    if (each <= 1) return launch(std::integral_constant<int, 1>());
+    if (each <= 2) return launch(std::integral_constant<int, 2>());
+    if (each <= 4) return launch(std::integral_constant<int, 4>());
+    return launch(std::integral_constant<int, 8>());
 }
 
 template <class T>
