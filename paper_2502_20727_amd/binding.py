@@ -512,13 +512,14 @@ def spd_pages_plan(pages: int, positions: Sequence[int], q_lens: Sequence[int], 
     if isinstance(page_table, np.ndarray):
         table = np.ascontiguousarray(page_table, dtype=np.int32)
     else:
-        table = np.zeros((len(pos), max([len(r) for r in page_table], default=0)), dtype=np.int32)
+        # (the rest of a shorter list is of no page: a sequence that needs it is refused)
+        table = np.full((len(page_table), max([len(r) for r in page_table], default=0)), -1, dtype=np.int32)
         for b, r in enumerate(page_table):
             table[b, :len(r)] = r
     if table.ndim != 2 or table.shape[0] != len(pos):
         raise ValueError("page_table has a row for each sequence")
     if table.size == 0:                       # (an address that is not NULL)
-        table = np.zeros((len(pos), 1), dtype=np.int32)
+        table = np.full((len(pos), 1), -1, dtype=np.int32)
     need = C.c_size_t(0)
 
     def call(out, n):
