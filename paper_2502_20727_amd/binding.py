@@ -503,23 +503,38 @@ def spd_pages_rope_table(pages: int) -> np.ndarray:
     return out
 
 
+def _int32(x, what: str) -> np.ndarray:
+    """Whole numbers as a contiguous int32 array."""
+    a = np.asarray(x)
+    if a.dtype != np.int32 and a.size:
+        if a.dtype.kind not in "iu":
+            raise TypeError(f"{what}: whole numbers wanted, not {a.dtype}")
+        if int(a.min()) < -(1 << 31) or int(a.max()) >= 1 << 31:
+            raise ValueError(f"{what}: beyond 32 bits")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
 def spd_pages_plan(pages: int, positions: Sequence[int], q_lens: Sequence[int], page_table, window: int = 0,
                    sinks: int = 0) -> np.ndarray:
     """The plan of a step (bytes on the host).  page_table: int32 [batch, entries], or a list of lists of pages."""
-    pos, lens = (np.ascontiguousarray(x, dtype=np.int32) for x in (positions, q_lens))
+    pos, lens = _int32(positions, "positions"), _int32(q_lens, "q_lens")
     if pos.shape != lens.shape or pos.ndim != 1:
         raise ValueError("positions and q_lens are lists of one length")
     if isinstance(page_table, np.ndarray):
-        table = np.ascontiguousarray(page_table, dtype=np.int32)
+        table = _int32(page_table, "page_table")
     else:
         # (the rest of a shorter list is of no page: a sequence that needs it is refused)
-        table = np.full((len(page_table), max([len(r) for r in page_table], default=0)), -1, dtype=np.int32)
-        for b, r in enumerate(page_table):
+        rows = [_int32(r, "page_table") for r in page_table]
+        table = np.full((len(rows), max([len(r) for r in rows], default=0)), -1, dtype=np.int32)
+        for b, r in enumerate(rows):
             table[b, :len(r)] = r
     if table.ndim != 2 or table.shape[0] != len(pos):
         raise ValueError("page_table has a row for each sequence")
     if table.size == 0:                       # (an address that is not NULL)
         table = np.full((len(pos), 1), -1, dtype=np.int32)
+    for what, n in (("window", window), ("sinks", sinks)):
+        if not -(1 << 31) <= n < 1 << 31:     # (ctypes would drop what does not fit)
+            raise ValueError(f"{what}: beyond 32 bits")
     need = C.c_size_t(0)
 
     def call(out, n):

@@ -31,3 +31,35 @@ def test_a_table_has_a_list_for_each_sequence(pages, table):
     _, ctx = pages()
     with pytest.raises(ValueError):
         B.spd_pages_plan(ctx, [0, 0], [1, 1], table)
+
+
+FAR = 1 << 32
+
+
+@pytest.mark.parametrize("over", [
+    dict(positions=np.array([FAR])), dict(q_lens=np.array([FAR + 1])), dict(table=np.array([[FAR + 3]])), dict(table=[[np.int64(FAR + 3)]]),
+    dict(table=[[FAR + 3]]), dict(positions=[FAR]), dict(window=FAR + 5), dict(window=8, sinks=FAR + 1), dict(window=FAR)], ids=str)
+def test_numbers_beyond_32_bits_are_refused(pages, over):
+    _, ctx = pages()
+    a = dict(positions=[0], q_lens=[1], table=[[3]], window=0, sinks=0)
+    a.update(over)
+    with pytest.raises((ValueError, OverflowError)):
+        B.spd_pages_plan(ctx, a["positions"], a["q_lens"], a["table"], a["window"], a["sinks"])
+
+
+@pytest.mark.parametrize("over", [dict(positions=[0.5]), dict(q_lens=np.array([1.7])), dict(table=[[2.9]]), dict(table=np.array([[2.9]]))], ids=str)
+def test_fractions_are_refused(pages, over):
+    _, ctx = pages()
+    a = dict(positions=[0], q_lens=[1], table=[[3]])
+    a.update(over)
+    with pytest.raises(TypeError):
+        B.spd_pages_plan(ctx, a["positions"], a["q_lens"], a["table"])
+
+
+def test_whole_numbers_of_any_type_make_the_same_plan(pages):
+    _, ctx = pages()
+    want = B.spd_pages_plan(ctx, [3, 40], [1, 2], [[7], [8, 9]])
+    for t in (np.int64, np.uint8, np.int32):
+        table = np.array([[7, 0], [8, 9]], t)
+        assert np.array_equal(B.spd_pages_plan(ctx, np.array([3, 40], t), np.array([1, 2], t), table), want)
+    assert np.array_equal(B.spd_pages_plan(ctx, torch.tensor([3, 40]), (1, 2), [(7,), np.array([8, 9])]), want)
