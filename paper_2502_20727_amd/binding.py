@@ -7,6 +7,7 @@ the stream.  If the HIP library cannot be loaded this module raises: there is no
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 from typing import Dict, List, Optional, Sequence
@@ -505,6 +506,8 @@ def spd_pages_rope_table(pages: int) -> np.ndarray:
 
 def _int32(x, what: str) -> np.ndarray:
     """Whole numbers as a contiguous int32 array."""
+    if isinstance(x, (list, tuple)):          # (checks every number, faster than NumPy takes them up)
+        return np.frombuffer(array.array("i", x), dtype=np.int32)
     a = np.asarray(x)
     if a.dtype != np.int32 and a.size:
         if a.dtype.kind not in "iu":
@@ -525,7 +528,7 @@ def spd_pages_plan(pages: int, positions: Sequence[int], q_lens: Sequence[int], 
     else:
         # (the rest of a shorter list is of no page: a sequence that needs it is refused)
         rows = [_int32(r, "page_table") for r in page_table]
-        table = np.full((len(rows), max([len(r) for r in rows], default=0)), -1, dtype=np.int32)
+        table = np.full((len(rows), max(map(len, rows), default=0)), -1, dtype=np.int32)
         for b, r in enumerate(rows):
             table[b, :len(r)] = r
     if table.ndim != 2 or table.shape[0] != len(pos):
