@@ -705,7 +705,8 @@ def spd_q8_pack_codes(w: np.ndarray, w_scale: np.ndarray, out: Optional[np.ndarr
     K, N = w.shape
     if out is None:
         out = np.empty(spd_q8_weight_bytes(K, N), dtype=np.uint8)
-    _check(lib().spd_q8_pack_codes(K, N, w.ctypes.data, N, np.ascontiguousarray(w_scale).ctypes.data, out.ctypes.data), "spd_q8_pack_codes")
+    scale = np.ascontiguousarray(w_scale)     # (held until the call is over)
+    _check(lib().spd_q8_pack_codes(K, N, w.ctypes.data, N, scale.ctypes.data, out.ctypes.data), "spd_q8_pack_codes")
     return out
 
 

@@ -63,3 +63,13 @@ def test_whole_numbers_of_any_type_make_the_same_plan(pages):
         table = np.array([[7, 0], [8, 9]], t)
         assert np.array_equal(B.spd_pages_plan(ctx, np.array([3, 40], t), np.array([1, 2], t), table), want)
     assert np.array_equal(B.spd_pages_plan(ctx, torch.tensor([3, 40]), (1, 2), [(7,), np.array([8, 9])]), want)
+
+
+# ------------------------------------------------------------------------------------------ CPU: packers
+
+def test_scales_of_every_other_place_are_packed():
+    K, N = 16, 700
+    r = np.random.RandomState(0)
+    codes, scale = r.randint(-127, 128, (K, N)).astype(np.int8), r.rand(2 * N).astype(np.float32)[::2]
+    c, s = B.spd_q8_unpack(K, N, B.spd_q8_pack_codes(codes, scale))
+    assert np.array_equal(s, scale) and np.array_equal(c, codes)
