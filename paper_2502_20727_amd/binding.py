@@ -328,8 +328,8 @@ def spd_unpack_shard(ctx: int, packed: np.ndarray, shapes: Dict[str, tuple]) -> 
 def spd_kv_pack(ctx: int, k: np.ndarray, v: np.ndarray, cache_host: np.ndarray) -> None:
     assert k.dtype == np.float32 and v.dtype == np.float32 and k.shape == v.shape
     batch, _, n_pos, _ = k.shape
-    _check(lib().spd_kv_pack(ctx, _ptr(np.ascontiguousarray(k)), _ptr(np.ascontiguousarray(v)), batch, n_pos,
-                             cache_host.ctypes.data), "spd_kv_pack")
+    k, v = np.ascontiguousarray(k), np.ascontiguousarray(v)      # (held until the call is over)
+    _check(lib().spd_kv_pack(ctx, _ptr(k), _ptr(v), batch, n_pos, cache_host.ctypes.data), "spd_kv_pack")
 
 
 def spd_kv_unpack(ctx: int, cache_host: np.ndarray, batch: int, n_pos: int, kv_heads: int, head_dim: int):

@@ -407,6 +407,20 @@ def test_kv_pack_roundtrip(w):
     B.spd_destroy(ctx)
 
 
+def test_kv_pack_of_strided_arrays():
+    """Keys and values laid out with the heads behind the positions: their contiguous copies live until the call is over."""
+    w = SMALL_BF16
+    ctx = B.spd_create(B.make_config(w))
+    k, v = inputs.kv_prefill(w, 0, 1, w.batch, 37)
+    caches = [np.zeros(B.spd_get_sizes(ctx).kv_bytes, dtype=np.uint8) for _ in range(2)]
+    B.spd_kv_pack(ctx, k, v, caches[0])
+    strided = [np.ascontiguousarray(x.transpose(0, 2, 1, 3)).transpose(0, 2, 1, 3) for x in (k, v)]
+    assert not strided[0].flags.c_contiguous
+    B.spd_kv_pack(ctx, *strided, caches[1])
+    assert np.array_equal(*caches)
+    B.spd_destroy(ctx)
+
+
 def test_forward_calls_reject_bad_arguments_before_any_launch():
     # fake, suitably aligned addresses: every one of these calls must fail on the host
     w = SMALL_BF16
