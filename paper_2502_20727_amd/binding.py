@@ -690,13 +690,19 @@ def spd_q8_weight_bytes(K: int, N: int) -> int:
     return lib().spd_q8_weight_bytes(K, N)
 
 
+def _packed_host(a: np.ndarray, K: int, N: int) -> np.ndarray:
+    if not a.flags.c_contiguous or a.nbytes < spd_q8_weight_bytes(K, N):
+        raise ValueError("packed weights: a contiguous array of spd_q8_weight_bytes(K, N) bytes wanted")
+    return a
+
+
 def spd_q8_pack(w: np.ndarray, out: Optional[np.ndarray] = None) -> np.ndarray:
     """Quantises and packs fp32 weights [K, N] (y = x W)."""
     assert w.dtype == np.float32 and w.ndim == 2 and w.flags.c_contiguous
     K, N = w.shape
     if out is None:
         out = np.empty(spd_q8_weight_bytes(K, N), dtype=np.uint8)
-    _check(lib().spd_q8_pack(K, N, w.ctypes.data, N, out.ctypes.data), "spd_q8_pack")
+    _check(lib().spd_q8_pack(K, N, w.ctypes.data, N, _packed_host(out, K, N).ctypes.data), "spd_q8_pack")
     return out
 
 
@@ -706,14 +712,14 @@ def spd_q8_pack_codes(w: np.ndarray, w_scale: np.ndarray, out: Optional[np.ndarr
     if out is None:
         out = np.empty(spd_q8_weight_bytes(K, N), dtype=np.uint8)
     scale = np.ascontiguousarray(w_scale)     # (held until the call is over)
-    _check(lib().spd_q8_pack_codes(K, N, w.ctypes.data, N, scale.ctypes.data, out.ctypes.data), "spd_q8_pack_codes")
+    _check(lib().spd_q8_pack_codes(K, N, w.ctypes.data, N, scale.ctypes.data, _packed_host(out, K, N).ctypes.data), "spd_q8_pack_codes")
     return out
 
 
 def spd_q8_unpack(K: int, N: int, packed: np.ndarray):
     """(codes int8 [K, N], scales fp32 [N]) of packed weights."""
     w, s = np.empty((K, N), dtype=np.int8), np.empty(N, dtype=np.float32)
-    _check(lib().spd_q8_unpack(K, N, packed.ctypes.data, w.ctypes.data, N, s.ctypes.data), "spd_q8_unpack")
+    _check(lib().spd_q8_unpack(K, N, _packed_host(packed, K, N).ctypes.data, w.ctypes.data, N, s.ctypes.data), "spd_q8_unpack")
     return w, s
 
 

@@ -73,3 +73,17 @@ def test_scales_of_every_other_place_are_packed():
     codes, scale = r.randint(-127, 128, (K, N)).astype(np.int8), r.rand(2 * N).astype(np.float32)[::2]
     c, s = B.spd_q8_unpack(K, N, B.spd_q8_pack_codes(codes, scale))
     assert np.array_equal(s, scale) and np.array_equal(c, codes)
+
+
+def test_packers_refuse_buffers_that_are_too_short():
+    K, N = 70, 20
+    need = B.spd_q8_weight_bytes(K, N)
+    w, codes, scale = np.ones((K, N), np.float32), np.ones((K, N), np.int8), np.ones(N, np.float32)
+    short, apart = np.zeros(need - 1, np.uint8), np.zeros(2 * need, np.uint8)[::2]
+    for buf in (short, apart):
+        for call in (lambda: B.spd_q8_pack(w, buf), lambda: B.spd_q8_pack_codes(codes, scale, buf), lambda: B.spd_q8_unpack(K, N, buf)):
+            with pytest.raises(ValueError):
+                call()
+        assert not buf.any()
+    whole = np.zeros(need, np.uint8)
+    assert B.spd_q8_pack(w, whole) is whole and B.spd_q8_unpack(K, N, whole)[0].all()
