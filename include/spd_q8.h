@@ -16,6 +16,7 @@
  *
  * The conventions are those of spd.h: error codes, host checks before anything is enqueued, caller-owned
  * buffers, nothing allocated, freed or waited for by a device call, work enqueued on `stream` alone.
+ * A call that has nothing to do (no tokens, no rows) needs no addresses but its plan's.
  * The device calls may be captured into a HIP graph.  Results are bit-reproducible.
  */
 #ifndef SPD_Q8_H

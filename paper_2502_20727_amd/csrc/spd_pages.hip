@@ -1037,12 +1037,12 @@ int spd_pages_write(const spd_pages *pages, const void *plan_host, const void *p
     if (rc != SPD_OK) return rc;
     const spd_pages_config &c = pages->cfg;
     if (in_dtype != SPD_F32 && in_dtype != c.dtype) return SPD_EINVAL;
+    if (!h.n_write) return SPD_OK;
     const int es = in_dtype == SPD_F32 ? 4 : 2;
     if (!qkv || !pool || !aligned(qkv, 16) || !aligned(pool, 256) || (q_out && !rope) || !aligned(rope, 16)) return SPD_EINVAL;
     if (ld < (int64_t)(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim || ld * es % 16) return SPD_EINVAL;
     if (q_out && (!aligned(q_out, 16) || ld_q < (int64_t)c.n_q_heads * c.head_dim || ld_q % 8)) return SPD_EINVAL;
     if (q_out == qkv && (in_dtype == SPD_F32 || ld_q != ld)) return SPD_EINVAL;
-    if (!h.n_write) return SPD_OK;
     (void)hipGetLastError();
     WriteArgs A;
     A.P = pages_args(pages, h, plan_dev, pool, h.write);
@@ -1074,8 +1074,8 @@ int spd_pages_read(const spd_pages *pages, const void *plan_host, const void *pl
     if (rc != SPD_OK) return rc;
     const spd_pages_config &c = pages->cfg;
     if (out_dtype != SPD_F32 && out_dtype != c.dtype) return SPD_EINVAL;
-    if (!pool || !k_out || !v_out || !aligned(pool, 256) || !aligned(k_out, 16) || !aligned(v_out, 16)) return SPD_EINVAL;
     if (!h.held) return SPD_OK;
+    if (!pool || !k_out || !v_out || !aligned(pool, 256) || !aligned(k_out, 16) || !aligned(v_out, 16)) return SPD_EINVAL;
     (void)hipGetLastError();
     const Pages P = pages_args(pages, h, plan_dev, pool, 0);
     const dim3 grid((h.max_end + 63) / 64, h.batch, c.n_kv_heads);
@@ -1097,10 +1097,10 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
     if (rc != SPD_OK) return rc;
     const spd_pages_config &c = pages->cfg;
     const int64_t width = (int64_t)c.n_q_heads * c.head_dim;
+    if (!h.tokens) return SPD_OK;
     if (!q || !pool || !out || !aligned(q, 16) || !aligned(out, 16) || !aligned(pool, 256)) return SPD_EINVAL;
     if (ld_q < width || ld_out < width || ld_q % 8 || ld_out % 8) return SPD_EINVAL;
     if (h.workspace && (!workspace || !aligned(workspace, 256))) return SPD_EINVAL;
-    if (!h.tokens) return SPD_OK;
     const uintptr_t q0 = (uintptr_t)q, q1 = q0 + ((h.tokens - 1) * ld_q + width) * 2, o0 = (uintptr_t)out,
                     o1 = o0 + ((h.tokens - 1) * ld_out + width) * 2;
     if (q0 < o1 && o0 < q1) return SPD_EINVAL;

@@ -255,12 +255,12 @@ int rows_impl(int kind, int32_t dtype, int32_t rows, const RowArgs &A, void *str
     const int64_t width = kind == ROW_SWIGLU ? 2 * (int64_t)A.n : A.n;
     if (dtype != SPD_F32 && dtype != SPD_BF16 && dtype != SPD_F16) return SPD_EINVAL;
     if (rows < 0 || rows > (1 << 23) || A.n < 0 || A.n > (1 << 30)) return SPD_EINVAL;
+    if (rows == 0 || A.n == 0) return SPD_OK;
     if (!A.x || !A.codes || !A.scales || A.ld_x < width || A.ld_codes < A.n) return SPD_EINVAL;
     if ((kind == ROW_NORM && !A.gain) || (A.add && A.ld_add < A.n) || (A.sum && A.ld_sum < A.n)) return SPD_EINVAL;
     const uintptr_t es = dtype == SPD_F32 ? 4 : 2;
     if ((uintptr_t)A.x % es || (uintptr_t)A.add % es || (uintptr_t)A.sum % es || (uintptr_t)A.scales % 4 || (uintptr_t)A.gain % 4) return SPD_EINVAL;
     if ((A.sum == A.x && A.ld_sum != A.ld_x) || (A.sum && A.sum == A.add && A.ld_sum != A.ld_add)) return SPD_EINVAL;
-    if (rows == 0 || A.n == 0) return SPD_OK;
     (void)hipGetLastError();
     hipStream_t s = (hipStream_t)stream;
     SPD_HIP(dtype == SPD_F32 ? launch_rows<float>(kind, rows, A, s)
@@ -806,13 +806,13 @@ int spd_q8_matmul(int32_t rows, int32_t K, int32_t N, const int8_t *codes, int64
                   int32_t out_dtype, const void *add, int64_t ld_add, void *out, int64_t ld_out, void *workspace, void *stream) {
     if (rows < 0 || rows > (1 << 28) || !spd_q8_weight_bytes(K, N) || (int64_t)rows * N > (int64_t)1 << 38) return SPD_EINVAL;
     if (out_dtype != SPD_F32 && out_dtype != SPD_BF16 && out_dtype != SPD_F16) return SPD_EINVAL;
+    if (rows == 0) return SPD_OK;
     if (!codes || !scales || !packed || !out || ((uintptr_t)codes & 15) || ((uintptr_t)packed & 255) || ((uintptr_t)scales & 3)) return SPD_EINVAL;
     if (ld_codes % 16 || ld_codes < (K + 15) / 16 * 16 || ld_out < N || (add && ld_add < N)) return SPD_EINVAL;
     const uintptr_t es = out_dtype == SPD_F32 ? 4 : 2;
     if ((uintptr_t)out % es || (uintptr_t)add % es) return SPD_EINVAL;
     if (add == out && ld_add != ld_out) return SPD_EINVAL;
     if (spd_q8_matmul_workspace(rows, K, N) && (!workspace || ((uintptr_t)workspace & 255))) return SPD_EINVAL;
-    if (rows == 0) return SPD_OK;
     (void)hipGetLastError();
     const uintptr_t quad = 4 * es;
     const bool quads = N % 4 == 0 && ld_out % 4 == 0 && (uintptr_t)out % quad == 0 && (!add || (ld_add % 4 == 0 && (uintptr_t)add % quad == 0));

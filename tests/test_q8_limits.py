@@ -87,3 +87,47 @@ def test_packers_refuse_buffers_that_are_too_short():
         assert not buf.any()
     whole = np.zeros(need, np.uint8)
     assert B.spd_q8_pack(w, whole) is whole and B.spd_q8_unpack(K, N, whole)[0].all()
+
+
+# ------------------------------------------------------------------------------------------ nothing to do
+
+def test_nothing_to_do_needs_no_addresses(pages):
+    _, ctx = pages()
+    lib, plan = B.lib(), B.spd_pages_plan(ctx, [], [], [])
+    ph = plan.ctypes.data
+    dev = (ph + 15) // 16 * 16                  # (never read)
+    assert lib.spd_pages_write(ctx, ph, dev, B.SPD_BF16, None, 1536, None, None, None, 0, None) == B.SPD_OK
+    assert lib.spd_pages_read(ctx, ph, dev, None, B.SPD_F32, None, None, None) == B.SPD_OK
+    assert lib.spd_pages_attention(ctx, ph, dev, None, 1024, None, None, 1024, None, None) == B.SPD_OK
+    for rows, n in ((0, 8), (2, 0)):
+        assert lib.spd_q8_norm(B.SPD_F32, rows, n, None, 8, None, 0, None, 1e-5, None, 0, None, 8, None, None) == B.SPD_OK
+        assert lib.spd_q8_rows(B.SPD_F32, rows, n, None, 8, None, 8, None, None) == B.SPD_OK
+        assert lib.spd_q8_swiglu(B.SPD_F32, rows, n, None, 16, None, 8, None, None) == B.SPD_OK
+    assert lib.spd_q8_matmul(0, 32, 8, None, 32, None, None, B.SPD_F32, None, 0, None, 8, None, None) == B.SPD_OK
+    # what is wrong without any work is still wrong
+    assert lib.spd_pages_write(ctx, ph, dev, B.SPD_F16, None, 1536, None, None, None, 0, None) == B.SPD_EINVAL
+    assert lib.spd_q8_rows(5, 0, 8, None, 8, None, 8, None, None) == B.SPD_EINVAL
+    assert lib.spd_q8_matmul(0, 0, 8, None, 32, None, None, B.SPD_F32, None, 0, None, 8, None, None) == B.SPD_EINVAL
+
+
+@gpu_test
+def test_empty_tensors(gpu):
+    cfg = config()
+    dp = B.DevicePages(cfg, gpu)
+
+    def none(n, t=torch.bfloat16, rows=0):
+        return torch.empty(rows, n, dtype=t, device=gpu)
+    plan = B.PagePlan(dp, [3, 0], [0, 0], [[1], []])
+    B.spd_pages_write(dp.ctx, plan, none(1536), dp.rope, dp.pool, none(1024))
+    B.spd_pages_attention(dp.ctx, plan, none(1024), dp.pool, none(1024), plan.workspace)
+    plan = B.PagePlan(dp, [], [], [])
+    k, v = (torch.empty(0, 2, 128, device=gpu) for _ in range(2))
+    B.spd_pages_read(dp.ctx, plan, dp.pool, k, v)
+    for rows, n in ((0, 16), (3, 0)):
+        codes, scales = none(n, torch.int8, rows), torch.full((rows,), 7.0, device=gpu)
+        B.spd_q8_norm(none(n, rows=rows), None, torch.ones(n, device=gpu), 1e-5, None, codes, scales)
+        B.spd_q8_rows(none(n, rows=rows), codes, scales)
+        B.spd_q8_swiglu(none(2 * n, rows=rows), codes, scales)
+        assert bool((scales == 7.0).all())
+    packed = torch.from_numpy(B.spd_q8_pack(np.ones((16, 16), np.float32))).to(gpu)
+    B.spd_q8_matmul(none(16, torch.int8), torch.empty(0, device=gpu), packed, 16, None, none(16))
