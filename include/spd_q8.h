@@ -114,7 +114,8 @@ int spd_pages_plan_get_info(const spd_pages *pages, const void *plan_host, spd_p
  *           pool's dtype; 16-byte aligned, ld * element size a multiple of 16
  *   rope    device copy of the rotary table, 16-byte aligned, or NULL: keys go in as they are, and q_out has to be NULL
  *   q_out   [tokens][ld_q] in the pool's dtype, receives the rotated queries, 16-byte aligned rows; may be qkv itself (with its
- *           ld) when in_dtype is the pool's dtype; NULL: not wanted
+ *           ld) when in_dtype is the pool's dtype, else it may share no memory with qkv (columns beside it in rows of the same stride in
+ *           bytes do not); NULL: not wanted
  * Must be enqueued ahead of the step's spd_pages_attention(). */
 int spd_pages_write(const spd_pages *pages, const void *plan_host, const void *plan_dev, int32_t in_dtype, const void *qkv,
                     int64_t ld, const float *rope, void *pool, void *q_out, int64_t ld_q, void *stream);

@@ -225,6 +225,22 @@ void spd_parallel_for(int n, F f) {
 
 inline size_t spd_align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
+// Do two matrices share memory?  `rows` rows of `width` bytes each, `pitch` bytes apart (at least the width).  Rows of one pitch may lie beside each
+// other, as columns of one buffer do: then it is their places in the pitch that count (also where their rows would not meet at the ends).
+struct spd_extent {
+    const void *at;
+    int64_t rows, width, pitch;
+};
+inline bool spd_share_memory(const spd_extent &a, const spd_extent &b) {
+    if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0) return false;
+    const int64_t a0 = (int64_t)(intptr_t)a.at, b0 = (int64_t)(intptr_t)b.at;
+    if (a0 + (a.rows - 1) * a.pitch + a.width <= b0 || b0 + (b.rows - 1) * b.pitch + b.width <= a0) return false;
+    const int64_t pa = a.rows == 1 ? b.pitch : a.pitch, pb = b.rows == 1 ? a.pitch : b.pitch;      // (the pitch of a single row is any)
+    if (pa != pb || (a.rows == 1 && b.rows == 1)) return true;
+    const int64_t r = (b0 - a0) % pa, d = r < 0 ? r + pa : r;      // of b in a's pitch
+    return d < a.width || d + b.width > pa;
+}
+
 // Keeps what a failing HIP call of this thread was, for spd_last_hip_error().  The macro leaves an entry point with SPD_EHIP.
 void spd_note_hip_error(hipError_t e, const char *call, const char *file, int line);
 #define SPD_HIP(x)                                              \

@@ -1042,7 +1042,11 @@ int spd_pages_write(const spd_pages *pages, const void *plan_host, const void *p
     if (!qkv || !pool || !aligned(qkv, 16) || !aligned(pool, 256) || (q_out && !rope) || !aligned(rope, 16)) return SPD_EINVAL;
     if (ld < (int64_t)(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim || ld * es % 16) return SPD_EINVAL;
     if (q_out && (!aligned(q_out, 16) || ld_q < (int64_t)c.n_q_heads * c.head_dim || ld_q % 8)) return SPD_EINVAL;
-    if (q_out == qkv && (in_dtype == SPD_F32 || ld_q != ld)) return SPD_EINVAL;
+    // queries turn in place, or where nobody reads
+    if (q_out == qkv ? in_dtype == SPD_F32 || ld_q != ld
+                     : spd_share_memory({qkv, h.tokens, (int64_t)(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim * es, ld * es},
+                                        {q_out, h.tokens, (int64_t)c.n_q_heads * c.head_dim * 2, ld_q * 2}))
+        return SPD_EINVAL;
     (void)hipGetLastError();
     WriteArgs A;
     A.P = pages_args(pages, h, plan_dev, pool, h.write);

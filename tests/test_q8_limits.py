@@ -131,3 +131,29 @@ def test_empty_tensors(gpu):
         assert bool((scales == 7.0).all())
     packed = torch.from_numpy(B.spd_q8_pack(np.ones((16, 16), np.float32))).to(gpu)
     B.spd_q8_matmul(none(16, torch.int8), torch.empty(0, device=gpu), packed, 16, None, none(16))
+
+
+# ------------------------------------------------------------------------------------------ matrices that share memory
+
+def test_rotated_queries_share_no_memory_with_what_others_read(pages):
+    """Keys and values of other workgroups, queries but not in their place, rows of another stride."""
+    _, ctx = pages()
+    lib, a = B.lib(), np.zeros(1 << 16, np.uint8)
+    base = (a.ctypes.data + 255) // 256 * 256
+    plan = B.spd_pages_plan(ctx, [0], [2], [[0]])
+    ph, w = plan.ctypes.data, (8 + 4) * 128
+    for ld, qo, ldq in ((w, base + 2 * 1024, w), (w, base + 2 * 128, w), (w, base + 2 * 1024, 1024), (2 * w, base + 2 * (w - 128), 2 * w),
+                        (2 * w, base + 2 * (2 * w - 512), 2 * w)):
+        assert lib.spd_pages_write(ctx, ph, base, B.SPD_BF16, base, ld, base, base, qo, ldq, None) == B.SPD_EINVAL, (ld, qo - base, ldq)
+    assert lib.spd_pages_write(ctx, ph, base, B.SPD_F32, base, w, base, base, base + 4 * w, 1024, None) == B.SPD_EINVAL
+
+
+@gpu_test
+def test_rotated_queries_beside_what_they_are_made_of(gpu):
+    """In rows of one buffer, behind the values, they share no memory with them."""
+    step = Step(gpu, config(q=4, kv=2, page=16), [20], [37], seed=9)
+    step.write()
+    wide = torch.zeros(37, 1024 + 512, dtype=torch.bfloat16, device=gpu)
+    wide[:, :1024] = step.qkv_dev
+    B.spd_pages_write(step.dp.ctx, step.plan, wide[:, :1024], step.rope, step.dp.pool, wide[:, 1024:])
+    assert torch.equal(wide[:, 1024:], step.q) and torch.equal(wide[:, :1024], step.qkv_dev)
