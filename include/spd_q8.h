@@ -127,7 +127,8 @@ int spd_pages_read(const spd_pages *pages, const void *plan_host, const void *pl
 
 /* out[token] = softmax over the visible positions of (q . k / sqrt(head_dim)) v, query head j on KV head
  * j / (n_q_heads / n_kv_heads).
- *   q, out     [tokens][ld_q], [tokens][ld_out] in the pool's dtype, 16-byte aligned, strides multiples of 8.  out may not overlap q.
+ *   q, out     [tokens][ld_q], [tokens][ld_out] in the pool's dtype, 16-byte aligned, strides multiples of 8.  out may share no memory
+ *              with q (other columns of rows of the same stride do not: keys and values that are put away leave theirs).
  *   workspace  workspace_bytes of the plan, 256-byte aligned; may be NULL when that is 0.  One per stream, of use to any plan that
  *              it is large enough for, zero-filled once before its first use (calls leave its counters at zero).
  * Sums, maxima and outputs are kept in fp32; probabilities (times the value's scale) are rounded to the pool's dtype

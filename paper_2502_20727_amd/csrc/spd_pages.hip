@@ -1105,9 +1105,7 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
     if (!q || !pool || !out || !aligned(q, 16) || !aligned(out, 16) || !aligned(pool, 256)) return SPD_EINVAL;
     if (ld_q < width || ld_out < width || ld_q % 8 || ld_out % 8) return SPD_EINVAL;
     if (h.workspace && (!workspace || !aligned(workspace, 256))) return SPD_EINVAL;
-    const uintptr_t q0 = (uintptr_t)q, q1 = q0 + ((h.tokens - 1) * ld_q + width) * 2, o0 = (uintptr_t)out,
-                    o1 = o0 + ((h.tokens - 1) * ld_out + width) * 2;
-    if (q0 < o1 && o0 < q1) return SPD_EINVAL;
+    if (spd_share_memory({q, h.tokens, width * 2, ld_q * 2}, {out, h.tokens, width * 2, ld_out * 2})) return SPD_EINVAL;
     (void)hipGetLastError();
     AttendArgs A;
     A.q = (const unsigned short *)q;

@@ -157,3 +157,19 @@ def test_rotated_queries_beside_what_they_are_made_of(gpu):
     wide[:, :1024] = step.qkv_dev
     B.spd_pages_write(step.dp.ctx, step.plan, wide[:, :1024], step.rope, step.dp.pool, wide[:, 1024:])
     assert torch.equal(wide[:, 1024:], step.q) and torch.equal(wide[:, :1024], step.qkv_dev)
+
+
+@gpu_test
+@pytest.mark.parametrize("q_len", [1, 3, 40])
+def test_attention_into_the_columns_of_the_keys(gpu, q_len):
+    """Rows of queries, keys and values whose keys and values are put away already take the output in their place: it shares no memory with
+    the queries beside it."""
+    step = Step(gpu, config(q=4, kv=4, page=16, n_pages=80), [600, 0], [q_len, 2], seed=q_len)
+    step.write()
+    want = step.attend()
+    wide = torch.zeros(q_len + 2, 3 * 512, dtype=torch.bfloat16, device=gpu)
+    wide[:, :512] = step.q
+    B.spd_pages_attention(step.dp.ctx, step.plan, wide[:, :512], step.dp.pool, wide[:, 512:1024], step.plan.workspace)
+    assert torch.equal(wide[:, :512], step.q) and torch.equal(wide[:, 512:1024], want) and not wide[:, 1024:].any()
+    with pytest.raises(B.SpdError):
+        B.spd_pages_attention(step.dp.ctx, step.plan, wide[:, :512], step.dp.pool, wide[:, 256:768], step.plan.workspace)
