@@ -142,12 +142,13 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
  * scale NaN.  Everything is computed in fp32.
  *   dtype    SPD_F32 | SPD_BF16 | SPD_F16, of the input rows
  *   ld*      row strides in elements; rows need no alignment beyond their elements'
- *   codes    int8 [rows][ld_codes]
+ *   codes    int8 [rows][ld_codes]; they share no memory with the rows, nor does a sum that is none of them (other columns of rows
+ *            of the same stride in bytes do not)
  *   scales   fp32 [rows]
  * rows (at most 2^23) = 0 or n = 0: nothing is done. */
 
 /* v = s / sqrt(mean(s^2) + eps) * gain with s = x + add.
- *   add   [rows][ld_add] or NULL (s = x);   sum   receives s in `dtype` or NULL, may alias x or add (same stride) */
+ *   add   [rows][ld_add] or NULL (s = x);   sum   receives s in `dtype` or NULL, may be x or add (same stride) */
 int spd_q8_norm(int32_t dtype, int32_t rows, int32_t n, const void *x, int64_t ld_x, const void *add, int64_t ld_add, const float *gain,
                 float eps, void *sum, int64_t ld_sum, int8_t *codes, int64_t ld_codes, float *scales, void *stream);
 /* v = x */
@@ -179,7 +180,8 @@ size_t spd_q8_matmul_workspace(int32_t rows, int32_t K, int32_t N);
  *   codes      int8 [rows][ld_codes], 16-byte aligned, ld_codes a multiple of 16 and at least K rounded up to that (bytes past K
  *              may hold anything)
  *   packed     device copy of the packed weights, 256-byte aligned
- *   out_dtype  SPD_F32 | SPD_BF16 | SPD_F16, of add ([rows][ld_add], or NULL) and out ([rows][ld_out]); out may be add
+ *   out_dtype  SPD_F32 | SPD_BF16 | SPD_F16, of add ([rows][ld_add], or NULL) and out ([rows][ld_out]); out may be add (same
+ *              stride), and shares no memory with it or with the codes otherwise
  *   workspace  spd_q8_matmul_workspace(rows, K, N) bytes, 256-byte aligned; may be NULL when that is 0 */
 int spd_q8_matmul(int32_t rows, int32_t K, int32_t N, const int8_t *codes, int64_t ld_codes, const float *scales, const void *packed,
                   int32_t out_dtype, const void *add, int64_t ld_add, void *out, int64_t ld_out, void *workspace, void *stream);

@@ -260,7 +260,13 @@ int rows_impl(int kind, int32_t dtype, int32_t rows, const RowArgs &A, void *str
     if ((kind == ROW_NORM && !A.gain) || (A.add && A.ld_add < A.n) || (A.sum && A.ld_sum < A.n)) return SPD_EINVAL;
     const uintptr_t es = dtype == SPD_F32 ? 4 : 2;
     if ((uintptr_t)A.x % es || (uintptr_t)A.add % es || (uintptr_t)A.sum % es || (uintptr_t)A.scales % 4 || (uintptr_t)A.gain % 4) return SPD_EINVAL;
-    if ((A.sum == A.x && A.ld_sum != A.ld_x) || (A.sum && A.sum == A.add && A.ld_sum != A.ld_add)) return SPD_EINVAL;
+    // a sum takes the place of a summand, or of neither; codes that of nothing
+    const int64_t n = A.n, e = (int64_t)es;
+    const spd_extent x{A.x, rows, width * e, A.ld_x * e}, add{A.add, rows, n * e, A.ld_add * e}, sum{A.sum, rows, n * e, A.ld_sum * e},
+        codes{A.codes, rows, n, A.ld_codes};
+    if (A.sum == A.x ? A.ld_sum != A.ld_x : spd_share_memory(x, sum)) return SPD_EINVAL;
+    if (A.sum && A.sum == A.add ? A.ld_sum != A.ld_add : spd_share_memory(add, sum)) return SPD_EINVAL;
+    if (spd_share_memory(x, codes) || spd_share_memory(add, codes) || spd_share_memory(sum, codes)) return SPD_EINVAL;
     (void)hipGetLastError();
     hipStream_t s = (hipStream_t)stream;
     SPD_HIP(dtype == SPD_F32 ? launch_rows<float>(kind, rows, A, s)
@@ -811,7 +817,11 @@ int spd_q8_matmul(int32_t rows, int32_t K, int32_t N, const int8_t *codes, int64
     if (ld_codes % 16 || ld_codes < (K + 15) / 16 * 16 || ld_out < N || (add && ld_add < N)) return SPD_EINVAL;
     const uintptr_t es = out_dtype == SPD_F32 ? 4 : 2;
     if ((uintptr_t)out % es || (uintptr_t)add % es) return SPD_EINVAL;
-    if (add == out && ld_add != ld_out) return SPD_EINVAL;
+    // the output takes the place of the summand, or of nothing that is read
+    const int64_t e = (int64_t)es;
+    const spd_extent sums{out, rows, N * e, ld_out * e};
+    if (add == out ? ld_add != ld_out : spd_share_memory({add, rows, N * e, ld_add * e}, sums)) return SPD_EINVAL;
+    if (spd_share_memory({codes, rows, K, ld_codes}, sums)) return SPD_EINVAL;
     if (spd_q8_matmul_workspace(rows, K, N) && (!workspace || ((uintptr_t)workspace & 255))) return SPD_EINVAL;
     (void)hipGetLastError();
     const uintptr_t quad = 4 * es;

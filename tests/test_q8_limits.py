@@ -173,3 +173,46 @@ def test_attention_into_the_columns_of_the_keys(gpu, q_len):
     assert torch.equal(wide[:, :512], step.q) and torch.equal(wide[:, 512:1024], want) and not wide[:, 1024:].any()
     with pytest.raises(B.SpdError):
         B.spd_pages_attention(step.dp.ctx, step.plan, wide[:, :512], step.dp.pool, wide[:, 256:768], step.plan.workspace)
+
+
+def test_rows_and_products_reject_matrices_that_share_memory():
+    """Sums and outputs in the place of a summand are fine, on a part of one they are not, nor are codes on what they are made of."""
+    lib, a = B.lib(), np.zeros(1 << 16, np.uint8)
+    base = (a.ctypes.data + 255) // 256 * 256
+    far = base + 8192
+    norm = dict(x=base, ldx=64, add=far, lda=64, s=far + 8192, lds=64, c=far + 16384, ldc=64)
+    for over in (dict(s=base + 4), dict(s=base + 256), dict(s=far + 128), dict(s=base, lds=64, x=base + 4, ldx=64), dict(c=base), dict(c=far + 64),
+                 dict(c=far + 8192 + 4), dict(s=base + 256 - 64, lds=128)):
+        x = {**norm, **over}
+        assert lib.spd_q8_norm(B.SPD_F32, 3, 64, x["x"], x["ldx"], x["add"], x["lda"], far + 24576, 1e-5, x["s"], x["lds"], x["c"], x["ldc"],
+                               far + 28672, None) == B.SPD_EINVAL, over
+    assert lib.spd_q8_rows(B.SPD_F32, 3, 64, base, 64, base + 64, 64, far, None) == B.SPD_EINVAL
+    assert lib.spd_q8_swiglu(B.SPD_F32, 3, 32, base, 64, base + 64, 64, far, None) == B.SPD_EINVAL
+    for add, lda, out, ldo, codes in ((base, 64, base + 16, 64, far), (base, 64, base + 256, 64, far), (None, 0, far, 64, far), (None, 0, far + 64, 64, far)):
+        assert lib.spd_q8_matmul(3, 64, 64, codes, 64, far + 8192, far + 16384, B.SPD_F32, add, lda, out, ldo, None, None) == B.SPD_EINVAL, (out - base)
+
+
+@gpu_test
+def test_rows_and_products_side_by_side_in_one_buffer(gpu):
+    """Columns of one buffer are as good as buffers of their own; sums and outputs in place of a summand too."""
+    g = torch.Generator().manual_seed(0)
+    wide = torch.randn(5, 96, generator=g).to(gpu)
+    x, add, total = wide[:, :32], wide[:, 32:64], wide[:, 64:]
+    gain = torch.ones(32, device=gpu)
+    codes, scales = torch.empty(5, 32, dtype=torch.int8, device=gpu), torch.empty(5, device=gpu)
+    want = x + add
+    B.spd_q8_norm(x, add, gain, 1e-5, total, codes, scales)
+    assert torch.equal(total, want)
+    again, scales2 = torch.empty_like(codes), torch.empty_like(scales)
+    for into in (x, add):
+        kept = wide.clone()
+        B.spd_q8_norm(x, add, gain, 1e-5, into, again, scales2)
+        assert torch.equal(into, want) and torch.equal(again, codes) and torch.equal(scales2, scales)
+        wide.copy_(kept)
+    packed = torch.from_numpy(B.spd_q8_pack(np.eye(32, dtype=np.float32))).to(gpu)
+    out = torch.empty(5, 32, device=gpu)
+    B.spd_q8_matmul(codes, scales, packed, 32, add, out)
+    B.spd_q8_matmul(codes, scales, packed, 32, add, total)
+    assert torch.equal(total, out)
+    B.spd_q8_matmul(codes, scales, packed, 32, add, add)
+    assert torch.equal(add, out)
