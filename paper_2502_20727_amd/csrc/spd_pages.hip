@@ -377,6 +377,11 @@ struct AttendArgs {
     float scale;                // log2(e) / sqrt(head_dim): softmax in powers of two
 };
 
+// Beside e4m3 the fp16 kernels keep the maximum of score + log2(scale).  A smaller scale (0 where a cleared page was never written) counts as this
+// one: its values are below 2^-31, nothing in fp16, and a probability, which may be 1 / scale of the maximum, stays far enough from
+// fp32's end for sums over as many keys as there can be.
+constexpr float LEAST_SCALE = 0x1p-40f;
+
 // is `key` visible to a query at position `at`?
 __device__ __forceinline__ bool visible(int key, int at, int window, int sinks) {
     return key <= at && (window == 0 || key > at - window || key < sinks);
@@ -511,8 +516,8 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             // (a hidden key's score is -inf, whatever log2 makes of its scale of 0)
-            const float a0 = PRODUCT ? s0[i] + __builtin_amdgcn_logf(fmaxf(v0[i], 0x1p-120f)) : s0[i],
-                        a1 = PRODUCT ? s1[i] + __builtin_amdgcn_logf(fmaxf(v1[i], 0x1p-120f)) : s1[i];
+            const float a0 = PRODUCT ? s0[i] + __builtin_amdgcn_logf(fmaxf(v0[i], LEAST_SCALE)) : s0[i],
+                        a1 = PRODUCT ? s1[i] + __builtin_amdgcn_logf(fmaxf(v1[i], LEAST_SCALE)) : s1[i];
             mx = fmaxf(mx, fmaxf(a0, a1));
         }
         const float m_new = fmaxf(m, quad_max(mx)), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
@@ -744,7 +749,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         const float vs = __shfl(sx, r16 + 16, 64);
         if (g == 0) to.ks[wave * 16 + r16] = vs == vs ? sx * A.scale : vs;
         else if (g == 1) to.vs[wave * 16 + r16] = vs == vs ? vs : 0.f;
-        else if (PRODUCT && g == 2) to.lv[wave * 16 + r16] = vs == vs ? __builtin_amdgcn_logf(fmaxf(vs, 0x1p-120f)) : 0.f;
+        else if (PRODUCT && g == 2) to.lv[wave * 16 + r16] = vs == vs ? __builtin_amdgcn_logf(fmaxf(vs, LEAST_SCALE)) : 0.f;
     };
     int page = page_of(P, s, my_block(0));
     fetch(0, page);

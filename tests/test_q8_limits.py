@@ -216,3 +216,34 @@ def test_rows_and_products_side_by_side_in_one_buffer(gpu):
     assert torch.equal(total, out)
     B.spd_q8_matmul(codes, scales, packed, 32, add, add)
     assert torch.equal(add, out)
+
+
+# ------------------------------------------------------------------------------------------ GPU: ends of the types
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("blank,position,q_len", [(4608, 5000, 1), (4608, 5000, 3), (800, 1000, 60), (3200, 3300, 1)])
+def test_positions_of_scale_zero(gpu, dtype, cache, blank, position, q_len):
+    """Pages as the cleared pool holds them (codes and scales 0) are keys and values of zeros like any others."""
+    cfg = config(q=4, kv=2, page=16, n_pages=330, max_ctx=5200, dtype=dtype, cache=cache)
+    step = Step(gpu, cfg, [0], [0], seed=1)
+    width, g = 8 * 128, torch.Generator().manual_seed(blank + q_len)
+    step.table = tables(cfg, [position + q_len], 1)
+    past = torch.randn(position - blank, width, generator=g).to(T16[dtype]).to(gpu)
+    B.spd_pages_write(step.dp.ctx, B.PagePlan(step.dp, [blank], [position - blank], step.table), past, step.rope, step.dp.pool)
+    step.positions, step.q_lens, step.ends = [position], [q_len], [position + q_len]
+    step.plan = B.PagePlan(step.dp, [position], [q_len], step.table)
+    step.qkv_dev = torch.randn(q_len, width, generator=g).to(T16[dtype]).to(gpu)
+    step.q = torch.empty(q_len, 4 * 128, dtype=T16[dtype], device=gpu)
+    step.write()
+    want, mag = reference(step, step.q.cpu(), step.dp.pool.cpu())
+    got = step.attend().cpu().double()
+    t = T16[dtype]
+    bound = (U[t] * 1.01 + 2e-5) * mag + U[t] * want.abs() * 1.01 + 2.0 ** -24
+    if dtype == B.SPD_F16:         # a weight below fp16's normal numbers is off by 2^-25 of the largest weight
+        k, v = held(cfg, step.dp.pool.cpu(), step.table, 0, position + q_len)
+        s = torch.einsum("nhd,hpd->hnp", step.q.cpu().double().view(q_len, 4, 128), k.repeat_interleave(2, 0)) / math.sqrt(128)
+        hidden = torch.arange(position + q_len) > torch.arange(position, position + q_len)[:, None]
+        w = s.masked_fill(hidden, -math.inf).softmax(-1).amax(-1)                                         # [4, q_len]
+        bound = bound + ((position + q_len) * 2.0 ** -25 * w.t() * float(v.abs().max())).repeat_interleave(128, 1)
+    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).nan_to_num(9e9).max())
