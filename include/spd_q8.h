@@ -147,7 +147,8 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
  *   scales   fp32 [rows]
  * rows (at most 2^23) = 0 or n = 0: nothing is done. */
 
-/* v = s / sqrt(mean(s^2) + eps) * gain with s = x + add.
+/* v = s / sqrt(mean(s^2) + eps) * gain with s = x + add.  s * gain has to be finite in fp32, the sum of squares does not: a row of any finite size
+ * has its norm (without an eps, down to the least normal number).
  *   add   [rows][ld_add] or NULL (s = x);   sum   receives s in `dtype` or NULL, may be x or add (same stride) */
 int spd_q8_norm(int32_t dtype, int32_t rows, int32_t n, const void *x, int64_t ld_x, const void *add, int64_t ld_add, const float *gain,
                 float eps, void *sum, int64_t ld_sum, int8_t *codes, int64_t ld_codes, float *scales, void *stream);

@@ -25,6 +25,42 @@ struct RowArgs {
     float eps;
 };
 
+// A thread's sum of squares.  Squares of fp32 values leave fp32 on both sides: those that may are added up once more, of values 2^80 times larger and
+// smaller.  A row whose mean is 1e-30 at most has no others (a row's length is below 2^30), and in one whose mean is 1e38 the others do not count.
+struct Squares {
+    float plain = 0.f, of_small = 0.f, of_large = 0.f;
+    // (a call of the norm of 16 rows of 8192 takes 0.03 us more than with the plain sum alone, of 8192 rows 0.4 of 87; without the branch 0.1 and 1.1)
+    template <int N>
+    __device__ __forceinline__ void add(const float (&s)[N]) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) t += s[i] * s[i];
+        plain += t;
+        if (N > 1 && t > 1e-20f && t < 1e30f) return;      // (one by itself is not worth a branch)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float up = s[i] * 0x1p80f, down = s[i] * 0x1p-80f;
+            of_small += up * up;
+            of_large += down * down;
+        }
+    }
+};
+// 1 / sqrt(mean + eps) of a row, `ss` the sum of all threads' plain sums.  The others are joined, by way of `sh`, only where they are called for,
+// which all of a workgroup see alike.
+__device__ __forceinline__ float norm_factor(float ss, const Squares &q, int n, float eps, float *sh) {
+    const float mean = ss / (float)n + eps;
+    if (mean > 1e-30f && mean < 1e38f) return 1.f / sqrtf(mean);
+    const bool small = mean <= 1e-30f;
+    float t = small ? q.of_small : q.of_large;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) t += __shfl_xor(t, d, 64);
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = t;
+    __syncthreads();
+    t = 0.f;
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) t += sh[w];
+    return small ? 0x1p80f / sqrtf(t / (float)n + eps * 0x1p80f * 0x1p80f) : 0x1p-80f / sqrtf(t / (float)n + eps * 0x1p-80f * 0x1p-80f);
+}
+
 template <class T, int KIND, bool ADD>
 struct RowSource {
     const T *x, *add;
@@ -53,18 +89,20 @@ __global__ void __launch_bounds__(256) k_rows_q8(RowArgs A) {
     src.add = ADD ? (const T *)A.add + row * A.ld_add : nullptr;
     src.gain = A.gain;
     src.n = A.n;
-    float ss = 0.f, most = 0.f;
+    Squares squares;
+    float most = 0.f;
     bool fine = true;
     for (int i = threadIdx.x; i < A.n; i += 256) {
         const float v = src.value(i);
         if constexpr (KIND == ROW_NORM) {
-            const float s = src.sum(i);
-            ss += s * s;
+            const float s[1] = {src.sum(i)};
+            squares.add(s);
         }
         fine = fine && fabsf(v) <= 3.402823466e38f;
         most = fmaxf(most, fabsf(v));
     }
     if (!fine) most = __builtin_inff();
+    float ss = squares.plain;
     __shared__ float sh[2][4];
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -78,9 +116,13 @@ __global__ void __launch_bounds__(256) k_rows_q8(RowArgs A) {
     __syncthreads();
     ss = (sh[0][0] + sh[0][1]) + (sh[0][2] + sh[0][3]);
     most = fmaxf(fmaxf(sh[1][0], sh[1][1]), fmaxf(sh[1][2], sh[1][3]));
-    const float factor = KIND == ROW_NORM ? 1.f / sqrtf(ss / (float)A.n + A.eps) : 1.f;
+    float factor = 1.f;
+    if constexpr (KIND == ROW_NORM) {
+        __shared__ float far[4];
+        factor = norm_factor(ss, squares, A.n, A.eps, far);
+    }
     // (a row of zeros without an eps has a factor of infinity, and 0 times it is NaN)
-    const bool ok = most < __builtin_inff() && (KIND != ROW_NORM || (ss < __builtin_inff() && most * factor < __builtin_inff()));
+    const bool ok = most < __builtin_inff() && (KIND != ROW_NORM || most * factor < __builtin_inff());
     const float a = fmaxf(most * factor, 0x1p-90f), up = 127.f / a;
     if (threadIdx.x == 0) A.scales[row] = ok ? a / 127.f : __builtin_nanf("");
     int8_t *codes = A.codes + row * A.ld_codes;
@@ -144,7 +186,8 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
             if constexpr (KIND == ROW_SWIGLU) in2[c] = load8_any(x + A.n + i, A.n - i);
         }
     }
-    float v[CH][8], ss = 0.f, most = 0.f;
+    Squares squares;
+    float v[CH][8], most = 0.f;
     bool fine = true;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -153,14 +196,15 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
             const int there = A.n - at - c * stride;
             const Eight<float> gain = WHOLE ? load8(A.gain + at + c * stride) : load8_any(A.gain + at + c * stride, there);
             Eight<T> out;
+            float s[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float s = (float)in[c].v[e];
-                if constexpr (ADD) s += (float)in2[c].v[e];
-                ss += s * s;
-                out.v[e] = (T)s;
-                v[c][e] = s * gain.v[e];
+                s[e] = (float)in[c].v[e];
+                if constexpr (ADD) s[e] += (float)in2[c].v[e];
+                out.v[e] = (T)s[e];
+                v[c][e] = s[e] * gain.v[e];
             }
+            squares.add(s);
             T *to = (T *)A.sum + row * A.ld_sum + at + c * stride;
             if (A.sum) {
                 if constexpr (WHOLE) *(Eight<T> *)__builtin_assume_aligned(to, 16) = out;
@@ -181,6 +225,7 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
         }
     }
     if (!fine) most = __builtin_inff();
+    float ss = squares.plain;
     __shared__ float sh[2][16];
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -198,9 +243,13 @@ __global__ void __launch_bounds__(CH >= 4 ? 256 : 1024) k_rows_q8_wide(RowArgs A
         ss += sh[0][w];
         most = fmaxf(most, sh[1][w]);
     }
-    const float factor = KIND == ROW_NORM ? 1.f / sqrtf(ss / (float)A.n + A.eps) : 1.f;
+    float factor = 1.f;
+    if constexpr (KIND == ROW_NORM) {
+        __shared__ float far[16];
+        factor = norm_factor(ss, squares, A.n, A.eps, far);
+    }
     // (a row of zeros without an eps has a factor of infinity, and 0 times it is NaN)
-    const bool ok = most < __builtin_inff() && (KIND != ROW_NORM || (ss < __builtin_inff() && most * factor < __builtin_inff()));
+    const bool ok = most < __builtin_inff() && (KIND != ROW_NORM || most * factor < __builtin_inff());
     const float a = fmaxf(most * factor, 0x1p-90f), up = 127.f / a;
     if (threadIdx.x == 0) A.scales[row] = ok ? a / 127.f : __builtin_nanf("");
     int8_t *codes = A.codes + row * A.ld_codes;

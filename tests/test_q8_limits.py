@@ -247,3 +247,21 @@ def test_positions_of_scale_zero(gpu, dtype, cache, blank, position, q_len):
         w = s.masked_fill(hidden, -math.inf).softmax(-1).amax(-1)                                         # [4, q_len]
         bound = bound + ((position + q_len) * 2.0 ** -25 * w.t() * float(v.abs().max())).repeat_interleave(128, 1)
     assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).nan_to_num(9e9).max())
+
+
+@gpu_test
+@pytest.mark.parametrize("n", [64, 5000, 8192, 20000])
+@pytest.mark.parametrize("add", [False, True])
+def test_norm_of_rows_whose_squares_leave_32_bits(gpu, n, add):
+    """The sum of squares is beyond fp32, or below it, the values and the norm are not."""
+    g = torch.Generator().manual_seed(n)
+    x = torch.randn(6, n, generator=g) * torch.tensor([1e18, 1e20, 3e30, 1e37, 1e-22, 1e-30])[:, None]
+    y = x.flip(1) * 0.5 if add else None
+    gain = 1 + 0.1 * torch.randn(n, generator=g)
+    codes, scales = torch.empty(6, n, dtype=torch.int8, device=gpu), torch.empty(6, device=gpu)
+    for eps in (0.0, 1e-5):
+        B.spd_q8_norm(x.to(gpu), None if y is None else y.to(gpu), gain.to(gpu), eps, None, codes, scales)
+        s = x.double() if y is None else x.double() + y.double()
+        v = s / (s.square().mean(-1, keepdim=True) + eps).sqrt() * gain.double()
+        # as for rows of ordinary size: a sum of n squares, at most n / 256 of them one after the other, ten levels of partial sums
+        check_rows(codes, scales, v, (n / 256 + 26) * U32)
