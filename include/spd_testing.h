@@ -129,6 +129,13 @@ int spd_down_in_tiles(const spd_ctx *ctx, int32_t tokens);
  * holds, as the runtime tells from the kernel's registers and LDS.  SPD_EINVAL: head_dim not 32, 64, 96 or 128; SPD_EHIP: the runtime does not tell. */
 int spd_prefill_attention_workgroups(int32_t head_dim);
 
+/* ---------------------------------------------------------------- kernel of an 8-bit product
+ * Which kernel spd_q8_matmul() takes for rows (1 or more) whose codes lie ld_codes bytes apart: 0 operands straight from memory, rows too far apart for
+ * offsets inside a panel; 1 to 5 weights streamed, m-tiles x n-tiles per workgroup 1 x 1, 1 x 2, 1 x 4, 2 x 2, 4 x 2; LDS-tiled, columns x rows:
+ * 6 128 x 64, 7 128 x 128, 8 256 x 128, 9 256 x 256, 10 the same with its last round in 8's tiles, 11 and 12 as 9 and 10 with the stages for a
+ * long K.  SPD_EINVAL: sizes that spd_q8_matmul() refuses or no rows.  Host only. */
+int spd_q8_kernel_of(int32_t rows, int32_t K, int32_t N, int64_t ld_codes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -145,6 +145,7 @@ _PROTOS = {
     "spd_q8_pack_codes": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
     "spd_q8_unpack": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "spd_q8_matmul_workspace": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "spd_q8_kernel_of": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int64]),
     "spd_q8_matmul": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
                                 C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
 }
@@ -726,6 +727,13 @@ def spd_q8_unpack(K: int, N: int, packed: np.ndarray):
 @functools.lru_cache(maxsize=4096)
 def spd_q8_matmul_workspace(rows: int, K: int, N: int) -> int:
     return lib().spd_q8_matmul_workspace(rows, K, N)
+
+
+def spd_q8_kernel_of(rows: int, K: int, N: int, ld_codes: Optional[int] = None) -> int:
+    rc = lib().spd_q8_kernel_of(rows, K, N, (K + 15) // 16 * 16 if ld_codes is None else ld_codes)
+    if rc < 0:
+        raise SpdError(rc, "spd_q8_kernel_of")
+    return rc
 
 
 def spd_q8_matmul(codes, scales, packed, N: int, add, out, workspace=None, stream=None) -> None:

@@ -3,6 +3,7 @@
 #include <type_traits>
 
 #include "spd_q8_internal.h"
+#include "spd_testing.h"
 
 namespace {
 
@@ -765,7 +766,7 @@ hipError_t launch_gemm(const Q8Args &A, hipStream_t s, int tile0 = 0, int n_tile
     return hipGetLastError();
 }
 
-enum Q8Kind { Q8_FAR, Q8_11, Q8_12, Q8_14, Q8_22, Q8_42, Q8_SMALL, Q8_SQUARE, Q8_HALF, Q8_BIG, Q8_BIG_HALF };
+enum Q8Kind { Q8_FAR, Q8_11, Q8_12, Q8_14, Q8_22, Q8_42, Q8_SMALL, Q8_SQUARE, Q8_HALF, Q8_BIG, Q8_BIG_HALF };      // (spd_testing.h)
 
 // Which kernel: the one that is estimated to end first.  A round of workgroups, one per compute unit, costs what a unit draws through its load
 // path (skinny kernels, small tiles) or multiplies (large ones) over K, and what comes before and after.  The figures, in us for a K of 8192
@@ -848,6 +849,12 @@ int spd_q8_rows(int32_t dtype, int32_t rows, int32_t n, const void *x, int64_t l
 int spd_q8_swiglu(int32_t dtype, int32_t rows, int32_t n, const void *x, int64_t ld_x, int8_t *codes, int64_t ld_codes, float *scales,
                   void *stream) {
     return rows_impl(ROW_SWIGLU, dtype, rows, RowArgs{x, nullptr, nullptr, nullptr, codes, scales, ld_x, 0, 0, ld_codes, n, 0.f}, stream);
+}
+
+int spd_q8_kernel_of(int32_t rows, int32_t K, int32_t N, int64_t ld_codes) {
+    if (rows < 1 || rows > (1 << 28) || !spd_q8_weight_bytes(K, N) || ld_codes < K) return SPD_EINVAL;
+    const int kind = q8_pick(rows, N, spd_q8_ktiles(K), ld_codes);
+    return kind >= Q8_BIG && spd_q8_ktiles(K) >= Q8_DEEP_KT ? kind + 2 : kind;
 }
 
 size_t spd_q8_matmul_workspace(int32_t rows, int32_t K, int32_t N) {
