@@ -1,4 +1,5 @@
-"""Every kernel of the 8-bit product, with the ways it has of storing its results, against plain computations in 64 bits."""
+"""Every kernel of the 8-bit product, with the ways it has of storing its results, and the attention of every pair of types, where the types' own code
+parts: against plain computations in 64 bits."""
 import math
 
 import pytest
@@ -6,7 +7,7 @@ import torch
 
 from paper_2502_20727_amd import binding as B
 
-from test_q8_serving import TYPES, U, U32
+from test_q8_serving import KIND_IDS, KINDS, T16, TYPES, U, U32, Step, config, held, reference
 
 gpu_test = pytest.mark.gpu
 
@@ -110,3 +111,115 @@ def test_products_beyond_fp16_are_infinities_of_their_sign(gpu, rows, K, N):
     assert beyond.any() and within.any()
     assert torch.equal(out[beyond].float(), out32[beyond].sign() * math.inf)
     assert bool(((out.float() - out32).abs()[within] <= U[torch.float16] * out32.abs()[within] * 1.0001 + 2.0 ** -25).all())
+
+
+# ------------------------------------------------------------------------------------------ attention
+
+def check_closely(step, got, q=None, more=0.0):
+    """As close as the pool's type allows: a weight is rounded to it once, and below fp16's normal numbers by 2^-25 of the largest weight.  Beside e4m3 fp16's
+    weights are probabilities times the values' scales, so that the largest is that of a probability times a row's largest value.  more: what the scores' own rounding moves a probability by."""
+    q = (step.q if q is None else q).cpu()
+    cfg, pool, t = step.cfg, step.dp.pool.cpu(), T16[step.cfg.dtype]
+    want, mag = reference(step, q, pool)
+    got = got.cpu().double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    d, group, first, floor = cfg.head_dim, cfg.n_q_heads // cfg.n_kv_heads, 0, torch.zeros_like(want)
+    if t is torch.float16:
+        for b, (p, n) in enumerate(zip(step.positions, step.q_lens)):
+            k, v = held(cfg, pool, step.table, b, p + n)
+            x = q[first:first + n].double().view(n, cfg.n_q_heads, d)
+            at, key = torch.arange(p, p + n)[:, None], torch.arange(p + n)[None]
+            hidden = key > at
+            if step.window:
+                hidden |= (key <= at - step.window) & (key >= step.sinks)
+            for h in range(cfg.n_q_heads):
+                size = v[h // group].abs().amax(-1).nan_to_num(0.0)
+                w = (x[:, h] @ k[h // group].t() / math.sqrt(d)).masked_fill(hidden, -math.inf).softmax(-1).nan_to_num(0.0)
+                most = (w * size).amax(-1) if cfg.cache_dtype == B.SPD_E4M3 else w.amax(-1) * size.max()
+                floor[first:first + n, h * d:(h + 1) * d] = ((p + n) * 2.0 ** -25 * most)[:, None]
+            first += n
+    ok = ~torch.isnan(want)
+    bound = (U[t] * 1.01 + 2e-5 + more) * mag + U[t] * want.abs() * 1.01 + 2.0 ** -24 + floor
+    err = (got - want).abs()
+    assert bool((err[ok] <= bound[ok]).all()), float((err / bound)[ok].max())
+
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (7, 3), (33, 0), (64, 40), (100, 17), (1000, 4), (5, 600)])
+@pytest.mark.parametrize("positions,q_lens", [([200, 3], [1, 1]), ([150], [90]), ([0, 400], [130, 20]), ([320], [3]), ([900, 600], [1, 3])], ids=str)
+def test_window_and_sinks_of_every_kind(gpu, dtype, cache, window, sinks, positions, q_lens):
+    step = Step(gpu, config(dtype=dtype, cache=cache, page=16, n_pages=110), positions, q_lens, window=window, sinks=sinks, seed=window)
+    step.write()
+    check_closely(step, step.attend())
+
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("q_len", [1, 3, 40])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_that_are_not_finite_in_every_kind(gpu, dtype, cache, q_len, d):
+    cfg = config(d=d, dtype=dtype, cache=cache, page=16, n_pages=60)
+    width = (cfg.n_q_heads + 2 * cfg.n_kv_heads) * d
+    key0, val0 = cfg.n_q_heads * d, (cfg.n_q_heads + cfg.n_kv_heads) * d
+
+    def spoil(step, past):
+        past[10, key0 + 3] = math.nan          # hidden from everyone: outside every window, no sink
+        past[11, val0 + 5] = math.inf
+        past[12, val0 + d + 7] = -math.inf     # head 1
+        past[190, key0 + 7] = math.inf         # visible to the first of the chunk's queries only
+        past[191, width - 1] = math.nan        # head 1
+    step = Step(gpu, cfg, [200], [q_len], window=12, sinks=4, seed=3, spoil=spoil)
+    step.write()
+    got = step.attend()
+    check_closely(step, got)
+    assert torch.isnan(got[0]).any() and (q_len < 40 or not torch.isnan(got[12:]).any())
+
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("q_len", [1, 30])
+def test_pages_that_held_other_sequences_in_every_kind(gpu, dtype, cache, q_len):
+    """Behind a sequence's end a page holds what was there: finite codes, NaN scales."""
+    cfg = config(page=64, n_pages=4, dtype=dtype, cache=cache)
+    step = Step(gpu, cfg, [70], [q_len], seed=5)
+    w = 1 if cache == B.SPD_E4M3 else 2
+    dirt = torch.randint(0, 120, step.dp.pool.shape, generator=torch.Generator().manual_seed(1)).to(torch.uint8)      # (finite in all three types)
+    raw = dirt.view(cfg.n_pages, cfg.n_kv_heads, -1)
+    raw[..., 2 * 64 * 128 * w:] = 255                       # every scale NaN
+    step.dp.pool.copy_(dirt.view(-1).to(gpu))
+    past = torch.randn(70, step.qkv.shape[1], generator=torch.Generator().manual_seed(2)).to(T16[dtype]).to(gpu)
+    B.spd_pages_write(step.dp.ctx, B.PagePlan(step.dp, [0], [70], step.table), past, step.rope, step.dp.pool)
+    step.write()
+    check_closely(step, step.attend())
+
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("q,kv,d,page", [(1, 1, 64, 16), (5, 5, 128, 64), (12, 4, 64, 128), (16, 1, 128, 256), (9, 3, 128, 32)])
+def test_heads_and_lengths_of_every_kind(gpu, dtype, cache, q, kv, d, page):
+    cfg = config(q=q, kv=kv, d=d, page=page, n_pages=6 + 1900 // page, dtype=dtype, cache=cache)
+    step = Step(gpu, cfg, [77, 300, 0, 980], [40, 1, 16, 2], seed=q)
+    step.write()
+    check_closely(step, step.attend())
+
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("up", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+def test_maxima_that_move_along_the_keys(gpu, dtype, cache, up, d):
+    """Scores that rise, with room in a tile and without, or fall, beside values whose sizes go the other way."""
+    cfg = config(q=4, kv=2, d=d, page=16, n_pages=60, dtype=dtype, cache=cache)
+
+    def spoil(step, past):
+        f = torch.linspace(0.1, 5.0, past.shape[0])[:, None].to(past.dtype)
+        past[:, 4 * d:6 * d] *= f if up else f.flip(0)
+        past[:, 6 * d:] *= f.flip(0) if up else f
+    step = Step(gpu, cfg, [400, 390], [90, 1], seed=3, spoil=spoil)
+    step.write()
+    # a score of up to s (in units of e) is a sum of d products in fp32, at most 16 of them one after the other, and three factors: 20 u s off, and
+    # a probability, with the sum that it is divided by, by twice as much
+    k = torch.cat([held(cfg, step.dp.pool.cpu(), step.table, b, step.ends[b])[0].flatten(0, 1) for b in range(2)])
+    s = float(step.q.float().cpu().view(-1, d).norm(dim=-1).max() * k.norm(dim=-1).max()) / math.sqrt(d)
+    check_closely(step, step.attend(), more=2 * 20 * U32 * s)
