@@ -174,7 +174,7 @@ int spd_q8_pack(int32_t K, int32_t N, const float *w, int64_t ld, void *packed_h
 int spd_q8_pack_codes(int32_t K, int32_t N, const int8_t *w, int64_t ld, const float *w_scale, void *packed_host);
 /* inverse of spd_q8_pack_codes() */
 int spd_q8_unpack(int32_t K, int32_t N, const void *packed_host, int8_t *w, int64_t ld, float *w_scale);
-/* scratch of a product of at most `rows` rows on one stream, may be 0 */
+/* scratch of a product of at most `rows` rows on one stream, may be 0 (and is for every size: none of the kernels needs any) */
 size_t spd_q8_matmul_workspace(int32_t rows, int32_t K, int32_t N);
 /* Device call.
  *   rows       at most 2^28, rows * N at most 2^38

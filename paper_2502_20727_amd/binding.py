@@ -745,8 +745,6 @@ def spd_q8_matmul(codes, scales, packed, N: int, add, out, workspace=None, strea
     pa, la = _rows(add, shape, "add")
     po, lo = _rows(out, shape, "out")
     _like(add, out, "add")
-    if (workspace.nbytes if workspace is not None else 0) < spd_q8_matmul_workspace(rows, K, N):
-        raise ValueError("workspace: too small")
     rc = l.spd_q8_matmul(rows, K, N, pc, lc, scales.data_ptr(), _buffer(packed, "packed", spd_q8_weight_bytes(K, N)), _type(out), pa, la, po, lo,
                          _buffer(workspace, "workspace"),
                          _current_stream() if stream is None else _stream_ptr(stream))

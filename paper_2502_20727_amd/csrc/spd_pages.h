@@ -21,9 +21,6 @@ struct spd_pages {
 // Values: lane (g, r) holds positions 4 g .. 4 g + 3 of features r + 16 t, t = (E / 4) c .. (E / 4) (c + 1) - 1: what the second
 // contraction takes beside probabilities as they leave the score tiles (four consecutive keys per lane).
 // ------------------------------------------------------------------------------------------
-SPD_HD int spd_page_key_off(int r, int f, int E) {       // element of position r, feature f inside a block
-    return (((f / (4 * E)) * 4 + (f / E) % 4) * 16 + r) * E + f % E;
-}
 SPD_HD int spd_page_value_off(int r, int f, int E) {
     const int t = f / 16;
     return (((t / (E / 4)) * 4 + r / 4) * 16 + f % 16) * E + (t % (E / 4)) * 4 + r % 4;

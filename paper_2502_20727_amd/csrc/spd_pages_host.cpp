@@ -33,17 +33,17 @@ Piece piece_of(const spd_pages *P, int seq, int pos, int row0, int rows, int win
     return w;
 }
 
-// Cuts pieces into items of at most `chunk` blocks, what each of `target` workgroups would have of them (0: not at all); `unit` blocks go
-// together.  one_round: into no more than `target` items.  most(blocks): the most items a piece is cut into.
+// Cuts pieces into items of at most `chunk` blocks, what each of `target` workgroups would have of them (0: not at all), into no more than `target`
+// items where the pieces are fewer; `unit` blocks go together.  most(blocks): the most items a piece is cut into.
 template <class Most>
-void cut(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs, int kv, int target, int unit, bool one_round, Most most, std::vector<spd_plan_item> &items,
-         std::vector<spd_plan_merge> &merges, int &slots) {
+void cut(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs, int kv, int target, int unit, Most most,
+         std::vector<spd_plan_item> &items, std::vector<spd_plan_merge> &merges, int &slots) {
     int64_t total = 0;
     for (const Piece &w : pieces) total += w.total;
     int64_t chunk = target ? std::max<int64_t>(unit, ((total * kv + target - 1) / target + unit - 1) / unit * unit) : 0;
     auto parts_of = [&](const Piece &w) { return chunk ? (int)std::min<int64_t>(most(w.total), (w.total + chunk - 1) / chunk) : 1; };
     // (what lengths leave over after whole chunks makes more items than the target: longer chunks, while cutting is what makes them)
-    for (int i = 0; i < 16 && chunk && one_round; ++i) {
+    for (int i = 0; i < 16 && chunk; ++i) {
         int64_t n = 0;
         for (const Piece &w : pieces) n += parts_of(w);
         if (n * kv <= target || n == (int64_t)pieces.size()) break;
@@ -88,7 +88,7 @@ void cut_large(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq>
         std::vector<spd_plan_item> i;
         std::vector<spd_plan_merge> m;
         int n = 0;
-        cut(pieces, seqs, kv, COMPUTE_UNITS * halves / 2, 4, true, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, i, m, n);
+        cut(pieces, seqs, kv, COMPUTE_UNITS * halves / 2, 4, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, i, m, n);
         const int64_t groups = (int64_t)i.size() * kv;
         const double tiles = (i[0].count + 3) / 4, rounds = (double)((groups + 2 * COMPUTE_UNITS - 1) / (2 * COMPUTE_UNITS));
         const double us = tiles * (groups <= COMPUTE_UNITS ? 1.65 : 2.35 * rounds) + (n ? 3.0 + 0.04 * n * kv : 0.0);
@@ -186,7 +186,7 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
     // of 500: 6.8 uncut, 8.4 in two parts)
     const int sets = P->group > 8 ? 1 : P->group > 4 ? 2 : P->group > 2 ? 4 : P->group > 1 ? 8 : 16;
     auto most_small = [&](int blocks) { return blocks <= 3 * 2 * SPD_SMALL_WAVES ? 1 : (int)std::min(std::sqrt(0.15 * blocks * sets), blocks / 8.0); };
-    cut(few, seqs, c.n_kv_heads, counted ? SMALL_TARGET : 0, 2, true, most_small, small, joined, small_slots);
+    cut(few, seqs, c.n_kv_heads, counted ? SMALL_TARGET : 0, 2, most_small, small, joined, small_slots);
     cut_large(many, seqs, c.n_kv_heads, large, merges, large_slots);
     for (const spd_plan_merge &m : merges) h.merge_rows = std::max(h.merge_rows, m.rows);
 

@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(512) k_q8_skinny(Q8Args A) {
 struct Q8Big {       // 256 x 256
     static constexpr int WN = 4, WM = 2, TI = 4, TJ = 8, KPS = 2, NST = 2;
 };
-struct Q8Deep {      // the same for a long K: copies four k-tiles ahead instead of two
+struct Q8Deep {      // the same for a long K: stages of one k-tile, copied five ahead
     static constexpr int WN = 4, WM = 2, TI = 4, TJ = 8, KPS = 1, NST = 5;
 };
 constexpr int Q8_DEEP_KT = 112;
@@ -878,7 +878,7 @@ int spd_q8_matmul(int32_t rows, int32_t K, int32_t N, const int8_t *codes, int64
     const spd_extent sums{out, rows, N * e, ld_out * e};
     if (add == out ? ld_add != ld_out : spd_share_memory({add, rows, N * e, ld_add * e}, sums)) return SPD_EINVAL;
     if (spd_share_memory({codes, rows, K, ld_codes}, sums)) return SPD_EINVAL;
-    if (spd_q8_matmul_workspace(rows, K, N) && (!workspace || ((uintptr_t)workspace & 255))) return SPD_EINVAL;
+    (void)workspace;
     (void)hipGetLastError();
     const uintptr_t quad = 4 * es;
     const bool quads = N % 4 == 0 && ld_out % 4 == 0 && (uintptr_t)out % quad == 0 && (!add || (ld_add % 4 == 0 && (uintptr_t)add % quad == 0));
