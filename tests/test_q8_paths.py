@@ -223,3 +223,37 @@ def test_maxima_that_move_along_the_keys(gpu, dtype, cache, up, d):
     k = torch.cat([held(cfg, step.dp.pool.cpu(), step.table, b, step.ends[b])[0].flatten(0, 1) for b in range(2)])
     s = float(step.q.float().cpu().view(-1, d).norm(dim=-1).max() * k.norm(dim=-1).max()) / math.sqrt(d)
     check_closely(step, step.attend(), more=2 * 20 * U32 * s)
+
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("batch,kv,d,prefix,lone", [(40, 8, 64, 9008, 0), (33, 8, 128, 8336, 0), (2100, 8, 64, 32, 3000), (300, 2, 128, 800, 4000)])
+def test_more_sequences_than_workgroups(gpu, dtype, cache, batch, kv, d, prefix, lone):
+    """Sequences that are not cut into parts, so that a wave goes through more blocks than it keeps pages of at a time; more of them, times heads, than there are
+    counters for parts, one much longer than the rest.  All but that one share their first pages."""
+    held_of = -(-(max(prefix, lone) + 16) // 16)
+    cfg = config(q=2 * kv, kv=kv, d=d, page=16, n_pages=2 * held_of + batch, dtype=dtype, cache=cache, max_ctx=9100)
+    dp = B.DevicePages(cfg, gpu)
+    g, t = torch.Generator().manual_seed(batch), T16[dtype]
+    common, own = list(range(prefix // 16)), list(range(held_of, 2 * held_of))
+    table = [common + [2 * held_of + b] for b in range(batch)]
+    positions = [prefix] * batch
+    if lone:
+        table[batch // 2], positions[batch // 2] = own, lone
+    width = 4 * kv * d
+    past = torch.randn(prefix + lone, width, generator=g).to(t).to(gpu)
+    B.spd_pages_write(dp.ctx, B.PagePlan(dp, [0, 0], [prefix, lone], [common, own]), past, dp.rope, dp.pool)
+    plan = B.PagePlan(dp, positions, [1] * batch, table)
+    qkv = torch.randn(batch, width, generator=g).to(t).to(gpu)
+    q, out = torch.empty(batch, 2 * kv * d, dtype=t, device=gpu), torch.full((batch, 2 * kv * d), math.nan, dtype=t, device=gpu)
+    B.spd_pages_write(dp.ctx, plan, qkv, dp.rope, dp.pool, q)
+    B.spd_pages_attention(dp.ctx, plan, q, dp.pool, out, plan.workspace)
+    assert not torch.isnan(out).any()
+    some = sorted({0, batch // 2, batch - 1, batch // 3})
+
+    class Part:
+        pass
+    part = Part()
+    part.cfg, part.dp, part.window, part.sinks = cfg, dp, 0, 0
+    part.positions, part.q_lens, part.table = [positions[b] for b in some], [1] * len(some), [table[b] for b in some]
+    check_closely(part, out[some], q[some])
