@@ -77,9 +77,11 @@ void cut(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs
 }
 
 // Many rows: cut so that a workgroup per compute unit has work, or one and a half, or two, whichever is estimated to end first.  A tile of four
-// blocks takes a workgroup 1.65 us by itself and 2.35 beside another (d 128); a join costs a launch and its partial results twice (66 KB each,
-// 0.04 us).  us a call, cut for 256 / 384 / 512 workgroups: three windowed chunks of 333 tokens, 5 heads 23.4 / 25.8 / 25.6, two chunks of 333 behind
-// 16000 92.9 / 72.1 / 89.1, one of 300 behind 2000, 8 heads of 8 50.9 / 42.5 / 49.3, one of 512 on 1 of 8 15.9 / 15.9 / 20.9.
+// blocks takes a workgroup 1.65 us by itself and 2.35 beside another; a join costs a launch and its partial results twice (66 KB each, 0.018 us).
+// us a call, cut for 256 / 384 / 512 workgroups: three windowed chunks of 333 tokens, 5 heads 23.2 / 26.3 / 26.1, without the window 38.8 / 37.2 / 35.4, the
+// same over e4m3 41.3 / 37.8 / 34.6, d 64 28.7 / 27.2 / 27.9, two of 333 behind 16000 64.3 / 62.1 / 55.7, one of 300 behind 2000, 8 heads of 8 63.3 / 49.1 /
+// 41.9.  Of 200 calls of all types and widths that the three cut differently this picks cuts that are 1 % slower than the best of them on average, 15 % at
+// most (with a part at 0.04 us: 3 % and 39 %).
 void cut_large(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs, int kv, std::vector<spd_plan_item> &items,
                std::vector<spd_plan_merge> &merges, int &slots) {
     if (pieces.empty()) return;
@@ -91,7 +93,7 @@ void cut_large(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq>
         cut(pieces, seqs, kv, COMPUTE_UNITS * halves / 2, 4, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, i, m, n);
         const int64_t groups = (int64_t)i.size() * kv;
         const double tiles = (i[0].count + 3) / 4, rounds = (double)((groups + 2 * COMPUTE_UNITS - 1) / (2 * COMPUTE_UNITS));
-        const double us = tiles * (groups <= COMPUTE_UNITS ? 1.65 : 2.35 * rounds) + (n ? 3.0 + 0.04 * n * kv : 0.0);
+        const double us = tiles * (groups <= COMPUTE_UNITS ? 1.65 : 2.35 * rounds) + (n ? 3.0 + 0.018 * n * kv : 0.0);
         if (halves == 2 || us < least) {
             least = us;
             items.swap(i);

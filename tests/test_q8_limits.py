@@ -265,3 +265,17 @@ def test_norm_of_rows_whose_squares_leave_32_bits(gpu, n, add):
         v = s / (s.square().mean(-1, keepdim=True) + eps).sqrt() * gain.double()
         # as for rows of ordinary size: a sum of n squares, at most n / 256 of them one after the other, ten levels of partial sums
         check_rows(codes, scales, v, (n / 256 + 26) * U32)
+
+
+# ------------------------------------------------------------------------------------------ CPU: how chunks are cut
+
+@pytest.mark.parametrize("over,batch,n,at,window,sinks,parts", [
+    (dict(q=5, kv=5), 3, 333, 5001, 0, 0, 99), (dict(q=5, kv=5), 3, 333, 5001, 2048, 4, 45), (dict(q=64, kv=8), 1, 300, 2000, 0, 0, 57),
+    (dict(q=40, kv=40), 1, 73, 1850, 0, 0, 6), (dict(q=12, kv=4, d=64), 1, 1056, 1365, 0, 0, 120), (dict(q=10, kv=10), 6, 574, 7661, 0, 0, 36),
+    (dict(q=40, kv=40), 1, 151, 0, 0, 0, 0)], ids=str)
+def test_chunks_are_cut_as_was_fastest(pages, over, batch, n, at, window, sinks, parts):
+    """The cut that took least of three that were timed on the device (partial results of all pieces)."""
+    cfg, ctx = pages(page=64, n_pages=batch * 140, max_ctx=9000, **over)
+    table = [list(range(140 * b, 140 * b + 140)) for b in range(batch)]
+    size = B.spd_pages_plan_get_info(ctx, B.spd_pages_plan(ctx, [at] * batch, [n] * batch, table, window, sinks)).workspace_bytes
+    assert max(0, size - 16384 * 4) // (128 * cfg.n_kv_heads * (cfg.head_dim + 2) * 4) == parts
