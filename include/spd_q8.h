@@ -17,7 +17,8 @@
  * The conventions are those of spd.h: error codes, host checks before anything is enqueued, caller-owned
  * buffers, nothing allocated, freed or waited for by a device call, work enqueued on `stream` alone.
  * A call that has nothing to do (no tokens, no rows) needs no addresses but its plan's.
- * The device calls may be captured into a HIP graph.  Results are bit-reproducible.
+ * The device calls may be captured into a HIP graph, which is then bound to what its calls were given on the host: a plan's launches
+ * are those of its lengths, another plan takes another capture.  Results are bit-reproducible.
  */
 #ifndef SPD_Q8_H
 #define SPD_Q8_H
@@ -79,7 +80,8 @@ int spd_pages_rope_table(const spd_pages *pages, float *host);
 /* ---------------------------------------------------------------- plan of a step (host only)
  *
  * A plan says what a step's calls work on: which sequences, where their new tokens sit, in which pages, and how
- * the work is cut into workgroups.  Every layer of a model uses the same plan.
+ * the work is cut into workgroups.  Every layer of a model uses the same plan, and every step needs one of its own: it is as long
+ * as its page table and its pieces of work, and takes the host 5 to 35 us for one to some hundred pieces (a call that asks for the size alone as long).
  *   batch       sequences; 0 is a plan of nothing
  *   positions   host, [batch]: position of each sequence's first new token = positions already in its pages
  *   q_lens      host, [batch]: new tokens of each sequence, 0 or more.  The tokens of a step are rows

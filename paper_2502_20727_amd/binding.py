@@ -847,7 +847,10 @@ class DevicePages:
 
 class PagePlan:
     """The plan of a step, on the host and on the device, and its scratch, cleared on torch's current stream.  Calls of one plan that may
-    overlap (on several streams) need a scratch each."""
+    overlap (on several streams) need a scratch each; the object has to live until its calls are over.
+
+    Every step needs one (35 to 85 us on the host).  The copy to the device waits for what torch's current stream was given before: plan a step
+    ahead of the launches of the one before it where the device is to stay busy."""
 
     def __init__(self, pages: DevicePages, positions: Sequence[int], q_lens: Sequence[int], page_table, window: int = 0, sinks: int = 0):
         import torch

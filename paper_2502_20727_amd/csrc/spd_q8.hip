@@ -136,7 +136,9 @@ __global__ void __launch_bounds__(256) k_rows_q8(RowArgs A) {
 }
 
 // The same with rows in registers (up to 16384 elements): eight per thread and chunk.  Bound by what is read and written: 8192 rows of
-// 8192 in 16 bits with a summand, 84 us (470 MB: 5.6 TB/s).
+// 8192 in 16 bits with a summand, 85 us (470 MB: 5.5 TB/s), as they are 36.5 (201 MB: 5.5).  SwiGLU is bound by its vector instructions, 37 an
+// element, most of them of the exponential and the division, which fill the SIMDs: 8192 rows of 3584 35 us (147 MB: 4.2 TB/s), 2048 13.5.  Longer rows are read twice, one workgroup of 256 threads each: 2048 SwiGLU rows of
+// 28672 166 us (1.8 TB/s).
 template <class T>
 struct Eight {
     T v[8];
@@ -471,7 +473,7 @@ __global__ void __launch_bounds__(512) k_q8_skinny(Q8Args A) {
 // with KPS 2 / 1: K 2048 33.1 / 33.9, 5120 69.0 / 69.6, 7168 100 / 94, 8192 120 / 107, 8256 111 / 109, 16384 244 / 209; K 1728 25.5 / 29.1.
 // The results leave through the LDS in whole cache lines: stored as
 // they lie in the registers (32 bytes a row and store) they took 2.2 times as long as K = 1024 did beside them (8192 rows, N 8192: 146 us a
-// call, now 79).  8192 rows, K 8192, N 7168: 414 us, 2.32 P operations a second (torch's library product of 8-bit integers: 400).  Bound by
+// call, now 79).  8192 rows, K 8192, N 7168: 406 to 417 us, 2.3 P operations a second (torch's library product of 8-bit integers: 400).  Bound by
 // the copies beside the MFMAs: 8192 cubed takes 472 us, without the copies 348, and all workgroups at one tile, out of the L2, 456; MFMAs
 // alone run at 3.55 P a second.  (A workgroup that goes on with its next tile's copies before it stores needs its descriptors in vector
 // registers: 559 us; four waves of 128 x 128 each, a third less read from the LDS: 445 beside 431; copies of the waves at different MFMAs: 426 to 496.)
@@ -772,7 +774,9 @@ enum Q8Kind { Q8_FAR, Q8_11, Q8_12, Q8_14, Q8_22, Q8_42, Q8_SMALL, Q8_SQUARE, Q8
 // path (skinny kernels, small tiles) or multiplies (large ones) over K, and what comes before and after.  The figures, in us for a K of 8192
 // and beside it, are fits to measured calls of 1 to 8192 rows, K 1024 to 8192, N 1280 to 8192.
 Q8Kind q8_pick(int rows, int N, int KT, int64_t ld_codes) {
-    if (ld_codes > (1 << 22)) return Q8_FAR;                  // 256 rows of a panel within 2^31 bytes
+    // 256 rows of a panel within 2^31 bytes.  (Few rows too, whose kernels would take them: codes 4 MiB apart are no layout of rows that this library
+    // writes, and were not timed.)
+    if (ld_codes > (1 << 22)) return Q8_FAR;
     const double k = KT / 128.0;
     const int64_t NT = spd_q8_ntiles(N), MT = ((int64_t)rows + 15) / 16;
     auto rounds = [](int64_t n) { return (double)((n + 255) / 256); };
