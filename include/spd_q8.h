@@ -32,6 +32,7 @@ extern "C" {
 /* Element types of these operators, besides SPD_F32 and SPD_BF16. */
 #define SPD_F16 2  /* IEEE binary16 */
 #define SPD_E4M3 3 /* 8 bits, 4 of exponent, 3 of fraction, largest finite value 448; a page's keys and values only */
+#define SPD_E2M1 4 /* 4 bits, 2 of exponent, 1 of fraction: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; a page's keys and values only */
 
 /* ---------------------------------------------------------------- pool of pages (host only)
  *
@@ -46,9 +47,19 @@ extern "C" {
  * not finite (or becomes infinite in a 16-bit type) is stored as codes 0 with scale NaN: it reads back as
  * NaN and makes NaN of the output of every query that sees it, and of no other.
  *
+ * With cache_dtype SPD_E2M1 every 32 consecutive features of a row have a scale of their own, a power of two 2^e: e is the least with
+ * a <= 7 * 2^e, a the largest magnitude among them, -100 to 125 with dtype SPD_BF16 and -23 to 13 with SPD_F16 (the least for a = 0), so that code *
+ * scale is a value of dtype.  The code is the e2m1 value nearest to x * 2^-e, ties to the even one, 6 for what is beyond (in SPD_F16
+ * what lies above 57344 becomes 49152).  Keys are rotated in 64 bits for it.  A row that holds a value that is not finite, or
+ * becomes infinite in dtype, has codes 0 and scales NaN.  A position takes 136 bytes of a head of 128 where e4m3 takes 264 and 16 bits 520; code *
+ * scale is at most a / 5 off (e4m3: a / 28), of normally distributed rows 11 % in the root mean square (e4m3: 2.6 %).
+ *
  * Layout, per page and head: keys [page_size/16 blocks][head_dim/64 (e4m3) | /32 (16-bit)][4][16 positions][16 bytes
  * of consecutive features]; values [blocks][same][4 groups][16 features][features 16 apart: 4 | 2][4 consecutive positions];
- * page_size key scales; page_size value scales.  The pool must be zero-filled once before its first use. */
+ * page_size key scales; page_size value scales.  With SPD_E2M1: keys [blocks][4][16 positions][head_dim/8 bytes of consecutive features, two to a byte,
+ * the first in its low half]; values [blocks][4 groups][16 features][head_dim/32 pairs of features 16 apart][4 consecutive positions], a byte for each pair;
+ * key scales [page_size][head_dim/32], bytes e + 127 (255: NaN); value scales the same.
+ * The pool must be zero-filled once before its first use. */
 typedef struct spd_pages_config {
     int32_t n_q_heads;   /* query heads of the rank */
     int32_t n_kv_heads;  /* KV heads of the rank; divides n_q_heads, at most 16 query heads per KV head */
@@ -56,7 +67,7 @@ typedef struct spd_pages_config {
     int32_t page_size;   /* positions per page: 16, 32, 64, 128 or 256 */
     int32_t n_pages;
     int32_t dtype;       /* SPD_BF16 | SPD_F16: queries and attention output */
-    int32_t cache_dtype; /* SPD_E4M3, or the same as dtype */
+    int32_t cache_dtype; /* SPD_E4M3, SPD_E2M1, or the same as dtype */
     int32_t max_ctx;     /* positions a sequence may reach (length of the rotary table) */
     float rope_base;     /* 10000 for LLaMA2 */
 } spd_pages_config;

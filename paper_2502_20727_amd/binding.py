@@ -17,7 +17,7 @@ import numpy as np
 from . import build
 from .workloads import Workload
 
-SPD_F32, SPD_BF16, SPD_F16, SPD_E4M3 = 0, 1, 2, 3
+SPD_F32, SPD_BF16, SPD_F16, SPD_E4M3, SPD_E2M1 = 0, 1, 2, 3, 4
 SPD_OK, SPD_EINVAL, SPD_EUNSUPPORTED, SPD_EHIP, SPD_ETOOBIG = 0, -1, -2, -3, -4
 SPD_STATIC_WORKSPACE_BYTES = 64 << 20
 SPD_ALL_RANKS = -1

@@ -7,7 +7,7 @@
 struct spd_pages {
     spd_pages_config cfg;
     int group;              // query heads per KV head
-    int width;              // bytes of a code: 1 (e4m3) | 2
+    int row_bytes;          // of a position's keys or values: codes and scales
     int shift;              // log2 of the 16-position blocks per page
     size_t head_bytes;      // of one head's share of a page
     size_t page_bytes;
@@ -20,6 +20,9 @@ struct spd_pages {
 // the scores runs over features in any order that queries share, a lane's 16 bytes are whole operands of the matrix cores.
 // Values: lane (g, r) holds positions 4 g .. 4 g + 3 of features r + 16 t, t = (E / 4) c .. (E / 4) (c + 1) - 1: what the second
 // contraction takes beside probabilities as they leave the score tiles (four consecutive keys per lane).
+// 4-bit codes: a block is D / 8 bytes for each lane.  Keys: lane (g, r) holds features D / 4 g .. D / 4 (g + 1) - 1 of position r, two to a byte.  Values: byte
+// 4 u + j of lane (g, r) holds features r + 32 u (low half) and r + 32 u + 16 of position 4 g + j: two that share a scale, as the instruction that
+// widens them takes one.  The scales are a byte for each position and group of 32 features, group after group, the keys' and then the values'.
 // ------------------------------------------------------------------------------------------
 SPD_HD int spd_page_value_off(int r, int f, int E) {
     const int t = f / 16;

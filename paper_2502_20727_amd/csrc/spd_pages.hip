@@ -7,6 +7,9 @@
 // A key's scale multiplies its scores in fp32; a value's scale multiplies its probability before that is rounded for the second
 // contraction (in fp16, relative to the largest such product).  e4m3 codes are exact in bf16 and fp16, so that dequantising rounds nothing.  Hidden keys are taken out by selection after
 // the scale has been multiplied, and codes in pages are always finite: a NaN scale of a hidden key reaches nothing.
+//
+// 4-bit codes (e2m1, a power of two for every 32 features) become 16-bit values whole, code * scale, which rounds nothing either: the one
+// instruction that widens two codes takes their scale along, and behind it the pages are 16-bit pages.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -69,6 +72,25 @@ struct Half {
         if constexpr (F16) return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, HI));
         else return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.0f, HI));
     }
+    // two e2m1 codes (byte I of v) times 2^e, e + 127 in bits 23 to 30 of `scale` (the others are not looked at); NaN for 255
+    template <int I>
+    static __device__ __forceinline__ int from_e2m1(int v, unsigned scale) {
+        if constexpr (F16) return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(v, __uint_as_float(scale), I));
+        else return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, __uint_as_float(scale), I));
+    }
+    // eight of them
+    static __device__ __forceinline__ i32x4 widen4(int v, unsigned scale) {
+        return (i32x4){from_e2m1<0>(v, scale), from_e2m1<1>(v, scale), from_e2m1<2>(v, scale), from_e2m1<3>(v, scale)};
+    }
+    // Values of four positions in 4 bits: byte j of `v` has features f and f + 16 of position j, whose scale is byte U of w[j].  The operands of
+    // feature f (lo) and f + 16 (hi): four positions each.
+    template <int U, class W>
+    static __device__ __forceinline__ void turn4(int v, const W &w, i32x2 &lo, i32x2 &hi) {
+        auto scale = [](unsigned x) { return U == 3 ? x >> 1 : x << (23 - 8 * U); };
+        const int a = from_e2m1<0>(v, scale(w[0])), b = from_e2m1<1>(v, scale(w[1])), c = from_e2m1<2>(v, scale(w[2])), d = from_e2m1<3>(v, scale(w[3]));
+        lo = (i32x2){(int)__builtin_amdgcn_perm(b, a, 0x05040100), (int)__builtin_amdgcn_perm(d, c, 0x05040100)};
+        hi = (i32x2){(int)__builtin_amdgcn_perm(b, a, 0x07060302), (int)__builtin_amdgcn_perm(d, c, 0x07060302)};
+    }
     // eight e4m3 codes
     static __device__ __forceinline__ i32x4 widen(int a, int b) {
         return (i32x4){from_e4m3<false>(a), from_e4m3<true>(a), from_e4m3<false>(b), from_e4m3<true>(b)};
@@ -89,6 +111,58 @@ __device__ __forceinline__ float half_max(float x) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
+
+// What the pages hold: SPD_E4M3, SPD_E2M1, or HALVES, values of the 16-bit type.
+constexpr int HALVES = 0;
+
+// The scales of four consecutive positions' values in 4 bits, one word each (its low D / 32 bytes).
+template <int D>
+struct Scales4 {
+    unsigned w[4];
+    __device__ __forceinline__ void load(const char *p) {
+        if constexpr (D == 128) {
+            const i32x4 x = *(const i32x4 *)p;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = x[j];
+        } else {
+            const i32x2 x = *(const i32x2 *)p;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (unsigned)x[j >> 1] >> (16 * (j & 1)) & 0xffff;
+        }
+    }
+    static constexpr unsigned BAD = D == 128 ? 0xffffffffu : 0xffffu;      // of a row that was not finite
+    __device__ __forceinline__ unsigned most() const {
+        const unsigned a = w[0] > w[1] ? w[0] : w[1], b = w[2] > w[3] ? w[2] : w[3];
+        return a > b ? a : b;
+    }
+};
+// a lane's 4-bit codes of a block: D / 8 bytes
+template <int D>
+struct Codes4 {
+    int c[D / 32];
+    __device__ __forceinline__ void load(const char *p) {
+        if constexpr (D == 128) {
+            const i32x4 x = *(const i32x4 *)p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] = x[i];
+        } else {
+            const i32x2 x = *(const i32x2 *)p;
+            c[0] = x[0];
+            c[1] = x[1];
+        }
+    }
+    __device__ __forceinline__ void stream(const char *p) {      // (read once)
+        if constexpr (D == 128) {
+            const i32x4 x = __builtin_nontemporal_load((const i32x4 *)p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] = x[i];
+        } else {
+            const i32x2 x = __builtin_nontemporal_load((const i32x2 *)p);
+            c[0] = x[0];
+            c[1] = x[1];
+        }
+    }
+};
 
 // what every kernel over pages is told
 struct Pages {
@@ -143,9 +217,63 @@ __device__ __forceinline__ void load_halves(const char *p, int apart, float (&a)
     }
 }
 
-template <class In, int D, bool E4M3, bool F16>
+// The float beside x that is odd in its last place where x is between two: compared with, or rounded to, anything of fewer digits it does as x does.
+__device__ __forceinline__ float to_odd(double x) {
+    const float f = (float)x;
+    const double back = f;
+    unsigned u = __float_as_uint(f);
+    if (back != x) u = (u - (fabs(back) > fabs(x))) | 1;
+    return __uint_as_float(u);
+}
+
+// Eight of a row's features, and the eight they turn with, in 4 bits: codes two to a byte, in the order of the features, and the scales' bytes.  Groups
+// of 32 features are four threads'; a row is TPR of them.  The least power of two of which the group's largest magnitude is 7 times at most: 6
+// is the largest code, and what lies between 6 and 7 is no further from it than half a step there (root mean square over N(0, 1), 7 as the limit
+// 11.2 % of it, 6 or 8 11.5).  Powers stay where code * scale is a value of the 16-bit type.
+template <int TPR, bool F16>
+__device__ __forceinline__ void quantise4(const float (&a)[8], const float (&b)[8], int &ca, int &cb, int &ea, int &eb) {
+    constexpr int LO = F16 ? -23 : -100, HI = F16 ? 13 : 125;
+    constexpr float LIMIT = F16 ? 65520.f : 0x1.ffp127f;      // becomes infinite in the 16-bit type
+    float ma = 0.f, mb = 0.f, bad = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        ma = fmaxf(ma, fabsf(a[i]));
+        mb = fmaxf(mb, fabsf(b[i]));
+        if (!(fabsf(a[i]) < LIMIT && fabsf(b[i]) < LIMIT)) bad = 1.f;
+    }
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+        ma = fmaxf(ma, __shfl_xor(ma, d, 64));
+        mb = fmaxf(mb, __shfl_xor(mb, d, 64));
+    }
+#pragma unroll
+    for (int d = 1; d < TPR; d <<= 1) bad = fmaxf(bad, __shfl_xor(bad, d, 64));
+    auto exponent = [](float m) {
+        const int u = __float_as_int(m), e = (u >> 23) - 127 - ((u & 0x7fffff) <= 0x600000 ? 2 : 1);
+        return (e < LO ? LO : e > HI ? HI : e) + 127;
+    };
+    ea = exponent(ma);
+    eb = exponent(mb);
+    const float sa = __int_as_float(ea << 23), sb = __int_as_float(eb << 23);
+    unsigned x = 0, y = 0;
+    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, a[0], a[1], sa, 0);
+    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, a[2], a[3], sa, 1);
+    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, a[4], a[5], sa, 2);
+    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, a[6], a[7], sa, 3);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(y, b[0], b[1], sb, 0);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(y, b[2], b[3], sb, 1);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(y, b[4], b[5], sb, 2);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(y, b[6], b[7], sb, 3);
+    ca = bad != 0.f ? 0 : (int)x;
+    cb = bad != 0.f ? 0 : (int)y;
+    if (bad != 0.f) ea = eb = 255;
+}
+
+template <class In, int D, int C, bool F16>
 __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
+    constexpr bool E4M3 = C == SPD_E4M3, E2M1 = C == SPD_E2M1;
     constexpr int W = E4M3 ? 1 : 2, E = 16 / W, TPR = D / 16, UNITS = 16 / TPR;      // threads per row; rows of a token side by side
+    constexpr int ROW = E2M1 ? D / 2 : D * W;                                          // bytes of a row
     const Pages &P = A.P;
     const spd_plan_block it = ((const spd_plan_block *)(P.plan + P.list))[blockIdx.x];
     const spd_plan_seq &s = it.s;
@@ -196,7 +324,7 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
     }
     // codes of the block's keys and values, rows = positions: even units keys, odd units values
     constexpr int HEADS = UNITS / 2;
-    __shared__ __attribute__((aligned(16))) char codes[UNITS][16 * D * W];
+    __shared__ __attribute__((aligned(16))) char codes[UNITS][16 * ROW];
     const int head0 = blockIdx.y * HEADS, head = head0 + unit / 2, kind = unit & 1;
     const bool there = mine && head < P.kv;
     auto scales_of = [&](const Block &B) { return (float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16; };
@@ -206,6 +334,37 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
         if (there) load_halves<In>(in + (size_t)(A.q_heads + head + kind * P.kv) * D * sizeof(In), D / 2, a, b);
+        if constexpr (E2M1) {
+            // (in 64 bits: beside a border between two codes 32 would now and then give the other, a whole step off)
+            if (kind == 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const double x = a[i], z = b[i], c = turn[i].x, n = turn[i].y;
+                    a[i] = to_odd(x * c - z * n);
+                    b[i] = to_odd(z * c + x * n);
+                }
+            }
+            int ca, cb, ea, eb;
+            quantise4<TPR, F16>(a, b, ca, cb, ea, eb);
+            char *to = codes[unit] + r * ROW;
+            // values: features f and f + 16 of a position share a byte, of which thread i has one and i + 2 the other
+            const bool upper = threadIdx.x & 2;
+            const int other = __shfl_xor(upper ? ca : cb, 2, 64);
+            if (kind == 0) {
+                *(int *)(to + f0 / 2) = ca;
+                *(int *)(to + D / 4 + f0 / 2) = cb;
+            } else {
+                const int p = upper ? other : ca, q = upper ? cb : other;
+                const int even = (p & 0x0f0f0f0f) | (q & 0x0f0f0f0f) << 4, odd = (p >> 4 & 0x0f0f0f0f) | (q & 0xf0f0f0f0);
+                *(i32x2 *)(to + (upper ? D / 2 + f0 : f0) / 32 * 16 + f0 % 16) =
+                    (i32x2){(int)__builtin_amdgcn_perm(odd, even, 0x05010400), (int)__builtin_amdgcn_perm(odd, even, 0x07030602)};
+            }
+            if (there && (threadIdx.x & 3) == 0) {
+                char *e = B0.head + (size_t)(head - head0) * P.head_bytes + (size_t)P.page_size * (D + kind * (D / 32)) + (B0.in_page * 16 + r) * (D / 32) + f0 / 32;
+                e[0] = (char)ea;
+                e[D / 64] = (char)eb;
+            }
+        } else {
         if (kind == 0) rotate(a, b);
         if constexpr (!E4M3) {       // what the 16-bit type makes of it decides whether the row is finite
 #pragma unroll
@@ -256,13 +415,33 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
             *(i32x4 *)(to + D) = fine ? y : (i32x4){0, 0, 0, 0};
         }
         if (there && f0 == 0) scales_of(B0)[(size_t)(head - head0) * (P.head_bytes / 4) + kind * P.page_size + r] = fine ? scale : __builtin_nanf("");
+        }
     }
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
         if (head0 + h >= P.kv) return;
-        char *keys = B0.head + (size_t)h * P.head_bytes + (size_t)B0.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
+        char *keys = B0.head + (size_t)h * P.head_bytes + (size_t)B0.in_page * 16 * ROW, *values = keys + (size_t)P.page_size * ROW;
         const char *kc = codes[2 * h], *vc = codes[2 * h + 1];
+        if constexpr (E2M1) {
+            constexpr int N = D / 32;            // words of a piece
+            for (int i = threadIdx.x; i < 64 * N; i += 256) {
+                const int pr = i / N & 15, g = i / N >> 4, w = i % N;
+                if (pr >= lo && pr < hi) *(int *)(keys + i * 4) = *(const int *)(kc + pr * ROW + (g * N + w) * 4);
+                if (lo == 0 && hi == 16) {
+                    int piece = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) piece |= (int)(unsigned char)vc[(4 * g + k) * ROW + w * 16 + pr] << (8 * k);
+                    *(int *)(values + i * 4) = piece;
+                }
+            }
+            if (!(lo == 0 && hi == 16))
+                for (int i = threadIdx.x; i < (hi - lo) * ROW; i += 256) {
+                    const int pr = lo + i / ROW, w = i % ROW / 16, f = i % 16;
+                    values[((pr / 4 * 16 + f) * N + w) * 4 + pr % 4] = vc[pr * ROW + i % ROW];
+                }
+            continue;
+        }
         // keys: a 16-byte piece belongs to one position
         for (int i = threadIdx.x; i < D * W; i += 256) {
             const int pr = i & 15, g = (i >> 4) & 3, ch = i >> 6;
@@ -301,9 +480,10 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
 // Reading back.  One workgroup per four 16-position blocks and KV head, a wave per block.  A lane's keys are pieces of rows; its values
 // (four positions of several features) change places in the LDS.  16 contexts of up to 4096 of one KV head, bf16: 8.7 us (33 MB: 3.8 TB/s, a launch of 3 us among them).
 // ------------------------------------------------------------------------------------------
-template <class Out, int D, bool E4M3, bool F16>
+template <class Out, int D, int C, bool F16>
 __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_out) {
-    constexpr int W = E4M3 ? 1 : 2, E = 16 / W, CH = D / (4 * E), ROW = D + 16 / (int)sizeof(Out);
+    constexpr bool E4M3 = C == SPD_E4M3;
+    constexpr int W = E4M3 ? 1 : 2, E = 16 / W, CH = D / (4 * E), ROW = D + 16 / (int)sizeof(Out), PIECES = D * sizeof(Out) / 16;
     struct Piece {
         Out v[16 / sizeof(Out)];
     };
@@ -313,6 +493,60 @@ __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_
     const int block = blockIdx.x * 4 + wave, head = blockIdx.z, r = lane & 15, g = lane >> 4;
     if (block * 16 >= s.end) return;             // (a wave works by itself)
     const Block B = block_at(P, s, head, block);
+    Out *mine = turned[wave];
+    const int n = s.end - block * 16 < 16 ? s.end - block * 16 : 16;
+    const int64_t row0 = ((s.held0 + block * 16) * P.kv + head) * D, pitch = (int64_t)P.kv * D;
+    auto put_rows = [&](Out *to) {               // of the LDS
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = lane; i < 16 * PIECES; i += 64) {
+            const int pr = i / PIECES, f = (i % PIECES) * (16 / (int)sizeof(Out));
+            if (pr < n)
+                *(Piece *)__builtin_assume_aligned(to + row0 + pr * pitch + f, 16) = *(const Piece *)__builtin_assume_aligned(mine + pr * ROW + f, 16);
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
+    if constexpr (C == SPD_E2M1) {               // (bf16 holds every code * scale)
+        constexpr int N = D / 32;
+        typedef Half<false> H;
+        const char *codes = B.head + B.in_page * (8 * D), *exps = B.head + (size_t)P.page_size * D + B.in_page * (16 * N);
+        Codes4<D> kx, vx;
+        Scales4<D> ve;
+        kx.load(codes + lane * (4 * N));
+        const unsigned ke = (unsigned)(unsigned char)exps[r * N + g * N / 4] << 23;
+        vx.load(codes + (size_t)P.page_size * (D / 2) + lane * (4 * N));
+        ve.load(exps + (size_t)P.page_size * N + 4 * N * g);
+        auto put = [&](int at, int two) {        // two features side by side
+            mine[at] = (Out)H::low(two);
+            mine[at + 1] = (Out)H::high(two);
+        };
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const i32x4 x = H::widen4(kx.c[i], ke);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) put(r * ROW + g * (D / 4) + 8 * i + 2 * j, x[j]);
+        }
+        put_rows(k_out);
+        auto turn = [&](auto u) {                // features r + 32 u and r + 32 u + 16
+            constexpr int U = decltype(u)::value;
+            i32x2 x, y;
+            H::template turn4<U>(vx.c[U], ve.w, x, y);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                Out *to = mine + (4 * g + j) * ROW + r + 32 * U;
+                to[0] = (Out)(j & 1 ? H::high(x[j >> 1]) : H::low(x[j >> 1]));
+                to[16] = (Out)(j & 1 ? H::high(y[j >> 1]) : H::low(y[j >> 1]));
+            }
+        };
+        turn(std::integral_constant<int, 0>());
+        turn(std::integral_constant<int, 1>());
+        if constexpr (D == 128) {
+            turn(std::integral_constant<int, 2>());
+            turn(std::integral_constant<int, 3>());
+        }
+        put_rows(v_out);
+        return;
+    }
     const char *keys = B.head + (size_t)B.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
     const float *scales = (const float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16;
     i32x4 kx[CH], vx[CH];
@@ -327,9 +561,6 @@ __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_
         if constexpr (E4M3) return i & 1 ? Codes::template from_e4m3<true>(x[i >> 1]) : Codes::template from_e4m3<false>(x[i >> 1]);
         else return x[i];
     };
-    Out *mine = turned[wave];
-    const int n = s.end - block * 16 < 16 ? s.end - block * 16 : 16;
-    const int64_t row0 = ((s.held0 + block * 16) * P.kv + head) * D, pitch = (int64_t)P.kv * D;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         Out piece[E];
@@ -353,14 +584,7 @@ __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_
             }
         }
     }
-    __builtin_amdgcn_wave_barrier();
-    constexpr int PIECES = D * sizeof(Out) / 16;
-#pragma unroll
-    for (int i = lane; i < 16 * PIECES; i += 64) {
-        const int pr = i / PIECES, f = (i % PIECES) * (16 / (int)sizeof(Out));
-        if (pr < n)
-            *(Piece *)__builtin_assume_aligned(v_out + row0 + pr * pitch + f, 16) = *(const Piece *)__builtin_assume_aligned(mine + pr * ROW + f, 16);
-    }
+    put_rows(v_out);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -384,7 +608,7 @@ constexpr float LEAST_SCALE = 0x1p-40f;
 
 // is `key` visible to a query at position `at`?
 __device__ __forceinline__ bool visible(int key, int at, int window, int sinks) {
-    return key <= at && (window == 0 || key > at - window || key < sinks);
+    return (key <= at) & ((window == 0) | (key > at - window) | (key < sinks));
 }
 __device__ __forceinline__ int list_block(const spd_plan_item &it, int v) { return v < it.sink_blocks ? v : it.block0 + (v - it.sink_blocks); }
 
@@ -395,8 +619,9 @@ __device__ __forceinline__ bool all_visible(int block, int first, int last, int 
 }
 
 // operands of one 16-position block, as loaded
-template <int D, bool E4M3>
+template <int D, int C>
 struct BlockLoad {
+    static constexpr bool E4M3 = C == SPD_E4M3;
     static constexpr int CH = E4M3 ? D / 64 : D / 32;      // 16-byte chunks per lane, keys and values each
     i32x4 k[CH], v[CH];
     f32x4 ks, vs;                                           // scales of keys 4 g .. 4 g + 3
@@ -414,6 +639,22 @@ struct BlockLoad {
     }
 };
 
+template <int D>
+struct BlockLoad<D, SPD_E2M1> {
+    static constexpr int N = D / 32;                        // groups of a row
+    Codes4<D> k, v;
+    Scales4<D> ve;                                          // of values 4 g .. 4 g + 3
+    unsigned char ke;                                       // of the lane's features of its key
+    __device__ __forceinline__ void load(const Pages &P, const Block &B, int lane) {
+        const char *codes = B.head + B.in_page * (8 * D), *exps = B.head + (size_t)P.page_size * D + B.in_page * (16 * N);
+        const int r = lane & 15, g = lane >> 4;
+        k.stream(codes + lane * (4 * N));
+        ke = exps[r * N + g * N / 4];
+        v.stream(codes + (size_t)P.page_size * (D / 2) + lane * (4 * N));
+        ve.load(exps + (size_t)P.page_size * N + 4 * N * g);
+    }
+};
+
 // A partial result is written by one workgroup and read by another, perhaps on another die with an L2 of its own: both go past that
 // L2, as relaxed atomics of the device's scope do.
 __device__ __forceinline__ void part_put(float *p, float a, float b) {
@@ -428,8 +669,9 @@ __device__ __forceinline__ float2 part_get(const float *p) {
 // Few rows (a decode step, a short draft): one workgroup per item and KV head, its eight waves take pairs of blocks in turn and merge
 // their states in the LDS.  Rows cut into several items are joined, in the items' order, by the workgroup that ends last.
 // Lane = 16 g + row.
-template <int D, bool E4M3, bool F16>
+template <int D, int C, bool F16>
 __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
+    constexpr bool E4M3 = C == SPD_E4M3, E2M1 = C == SPD_E2M1;
     constexpr int DT = D / 16, NF = D / 32, NW = SPD_SMALL_WAVES;
     typedef Half<F16> H;
     // fp16 has no room for a probability times a scale that may be tiny: there the maximum kept is that of the product, log2(scale) added to the score
@@ -455,7 +697,7 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
         const unsigned short *qp = A.q + (int64_t)(s.tok0 + token) * A.ld_q + (int64_t)(head * P.group + row % P.group) * D;
 #pragma unroll
         for (int i = 0; i < NF; ++i) {           // the features that lane (g, .) of a key holds
-            const int f = E4M3 ? 64 * (i >> 1) + 16 * g + 8 * (i & 1) : 32 * i + 8 * g;
+            const int f = E4M3 ? 64 * (i >> 1) + 16 * g + 8 * (i & 1) : E2M1 ? D / 4 * g + 8 * i : 32 * i + 8 * g;
             qf[i] = row < rows ? *(const i32x4 *)(qp + f) : (i32x4){0, 0, 0, 0};
         }
     }
@@ -464,7 +706,7 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
     for (int t = 0; t < DT; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = -__builtin_inff(), l = 0.f;
     struct Pair {
-        BlockLoad<D, E4M3> x[2];
+        BlockLoad<D, C> x[2];
     };
     auto load = [&](Pair &f, int j) __attribute__((always_inline)) {      // pair j of the wave
         if (j > 0 && (j & 31) == 0) pages = page_of(P, s, my_block(2 * j + lane < 2 * mine ? 2 * j + lane : 2 * j));
@@ -477,14 +719,18 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
     auto use = [&](const Pair &f, int j) __attribute__((always_inline)) {
         const bool two = 2 * (wave + NW * j) + 1 < it.count;
         const int b0 = my_block(2 * j), b1 = my_block(2 * j + 1);
-        const BlockLoad<D, E4M3> &x0 = f.x[0], &x1 = f.x[1];
+        const BlockLoad<D, C> &x0 = f.x[0], &x1 = f.x[1];
         f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+        Scales4<D> e0, e1;                       // 4 bits: of the values
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
             i32x4 k0, k1;
             if constexpr (E4M3) {
                 k0 = H::widen(x0.k[i >> 1][2 * (i & 1)], x0.k[i >> 1][2 * (i & 1) + 1]);
                 k1 = H::widen(x1.k[i >> 1][2 * (i & 1)], x1.k[i >> 1][2 * (i & 1) + 1]);
+            } else if constexpr (E2M1) {
+                k0 = H::widen4(x0.k.c[i], (unsigned)x0.ke << 23);
+                k1 = H::widen4(x1.k.c[i], (unsigned)x1.ke << 23);
             } else {
                 k0 = x0.k[i];
                 k1 = x1.k[i];
@@ -492,23 +738,48 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
             s0 = H::mfma16(k0, qf[i], s0);
             s1 = H::mfma16(k1, qf[i], s1);
         }
-        f32x4 v0 = x0.vs, v1 = x1.vs;
+        f32x4 v0, v1;
+        if constexpr (E2M1) {
+            // A value that is not finite makes its key's score NaN, and nothing else (a key's has become NaN by its scale): whoever sees it gets NaN
+            e0 = x0.ve;
+            e1 = x1.ve;
+            if (__builtin_amdgcn_ballot_w64((e0.most() > e1.most() ? e0.most() : e1.most()) == Scales4<D>::BAD))
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s0[i] *= x0.ks[i] * A.scale;
-            s1[i] *= x1.ks[i] * A.scale;
+                for (int i = 0; i < 4; ++i) {
+                    s0[i] = e0.w[i] == e0.BAD ? __builtin_nanf("") : s0[i];
+                    s1[i] = e1.w[i] == e1.BAD ? __builtin_nanf("") : s1[i];
+                    e0.w[i] = e0.w[i] == e0.BAD ? 0 : e0.w[i];
+                    e1.w[i] = e1.w[i] == e1.BAD ? 0 : e1.w[i];
+                }
+            v0 = v1 = (f32x4){1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s0[i] *= A.scale;
+                s1[i] *= A.scale;
+            }
+        } else {
+            v0 = x0.vs;
+            v1 = x1.vs;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s0[i] *= x0.ks[i] * A.scale;
+                s1[i] *= x1.ks[i] * A.scale;
+            }
         }
-        // (the scale of a hidden key's value may be NaN)
+        // (the scale of a hidden key's value may be NaN, in 4 bits some of them: behind the sequence's end a page holds anything)
         if (!(two && all_visible(b0, s.pos, last, A.window, A.sinks) && all_visible(b1, s.pos, last, A.window, A.sinks))) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (!visible(b0 * 16 + 4 * g + i, at, A.window, A.sinks)) {
-                    s0[i] = -__builtin_inff();
-                    v0[i] = 0.f;
-                }
-                if (!two || !visible(b1 * 16 + 4 * g + i, at, A.window, A.sinks)) {
-                    s1[i] = -__builtin_inff();
-                    v1[i] = 0.f;
+                // (selections, no branches: of a branch over the whole wave around one over lanes this compiler has lost the inner one's assignments)
+                const int k0 = b0 * 16 + 4 * g + i, k1 = b1 * 16 + 4 * g + i;
+                const bool see0 = visible(k0, at, A.window, A.sinks), see1 = visible(two ? k1 : 0x7fffffff, at, A.window, A.sinks);
+                s0[i] = see0 ? s0[i] : -__builtin_inff();
+                v0[i] = see0 ? v0[i] : 0.f;
+                s1[i] = see1 ? s1[i] : -__builtin_inff();
+                v1[i] = see1 ? v1[i] : 0.f;
+                if constexpr (E2M1) {            // (hidden from every row)
+                    e0.w[i] = k0 > last ? 0 : e0.w[i];
+                    e1.w[i] = k1 > last ? 0 : e1.w[i];
                 }
             }
         }
@@ -527,12 +798,28 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
         for (int i = 0; i < 4; ++i) {
             const float p0 = __builtin_amdgcn_exp2f(s0[i] - m_use), p1 = __builtin_amdgcn_exp2f(s1[i] - m_use);
             ps += p0 + p1;
-            w0[i] = p0 * v0[i];
-            w1[i] = p1 * v1[i];
+            w0[i] = E2M1 ? p0 : p0 * v0[i];
+            w1[i] = E2M1 ? p1 : p1 * v1[i];
         }
         l = l * alpha + ps;                      // (of the lane's keys; the four lanes of a row meet at the end)
         m = m_new;
         const i32x4 pf = {H::pack(w0[0], w0[1]), H::pack(w0[2], w0[3]), H::pack(w1[0], w1[1]), H::pack(w1[2], w1[3])};
+        if constexpr (E2M1) {
+            auto outputs = [&](auto u) __attribute__((always_inline)) {      // features r + 32 u and r + 32 u + 16
+                constexpr int U = decltype(u)::value;
+                i32x2 a0, b0, a1, b1;
+                H::template turn4<U>(x0.v.c[U], e0.w, a0, b0);
+                H::template turn4<U>(x1.v.c[U], e1.w, a1, b1);
+                o[2 * U] = H::mfma16((i32x4){a0[0], a0[1], a1[0], a1[1]}, pf, o[2 * U] * alpha);
+                o[2 * U + 1] = H::mfma16((i32x4){b0[0], b0[1], b1[0], b1[1]}, pf, o[2 * U + 1] * alpha);
+            };
+            outputs(std::integral_constant<int, 0>());
+            outputs(std::integral_constant<int, 1>());
+            if constexpr (D == 128) {
+                outputs(std::integral_constant<int, 2>());
+                outputs(std::integral_constant<int, 3>());
+            }
+        } else
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
             i32x4 vf;
@@ -668,9 +955,10 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
 // four prompts of 2048 tokens on 64 heads of 8 in 335 us, 0.82 PFLOP/s, where nothing but MFMAs on such data does 1.7.  (Two row tiles per wave
 // and one workgroup per compute unit, which read the LDS half as often: 541 us beside 363, no second wave to work beside the first's softmax.)
 // 16-bit pages need no scales, a bad row's key is NaN instead: three windowed chunks of 333 tokens 26.8 -> 23.7 us.
-template <int D, bool E4M3, bool F16>
+template <int D, int C, bool F16>
 __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
-    constexpr int W = E4M3 ? 1 : 2, KS = D / 16, DT = D / 32, CH = E4M3 ? D / 64 : D / 32;
+    constexpr bool E4M3 = C == SPD_E4M3, E2M1 = C == SPD_E2M1;
+    constexpr int W = E4M3 ? 1 : 2, KS = D / 16, DT = D / 32, CH = C == HALVES ? D / 32 : D / 64, N4 = D / 32;
     typedef Half<F16> H;
     constexpr bool PRODUCT = F16 && E4M3;        // the maximum kept is that of probability times scale, as in the kernel for few rows
     const Pages &P = A.P;
@@ -708,8 +996,20 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     auto my_block = [&](int v0) { return list_block(it, it.first + (v0 + wave < it.count ? v0 + wave : it.count - 1)); };
     i32x4 kx[CH], vx[CH];
     float sx = 0.f, sv = 0.f;
+    Codes4<D> kx4, vx4;                          // 4 bits: codes, scales of four positions' values, of the lane's features of its key, one of its value
+    Scales4<D> ve;
+    unsigned ke = 0, vbad = 0;
     auto fetch = [&](int v0, int page) __attribute__((always_inline)) {
         const Block B = block_in(P, page, head, my_block(v0));
+        if constexpr (E2M1) {
+            const char *codes = B.head + B.in_page * (8 * D), *exps = B.head + (size_t)P.page_size * D + B.in_page * (16 * N4);
+            kx4.load(codes + lane * (4 * N4));
+            vx4.load(codes + (size_t)P.page_size * (D / 2) + lane * (4 * N4));
+            ke = (unsigned char)exps[r16 * N4 + g * N4 / 4];
+            vbad = (unsigned char)exps[(size_t)P.page_size * N4 + r16 * N4];
+            ve.load(exps + (size_t)P.page_size * N4 + 4 * N4 * g);
+            return;
+        }
         const char *keys = B.head + (size_t)B.in_page * 16 * D * W, *values = keys + (size_t)P.page_size * D * W;
         const float *scales = (const float *)(B.head + (size_t)2 * P.page_size * D * W) + B.in_page * 16;
 #pragma unroll
@@ -727,7 +1027,30 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     // (after the last tile what is put away is not read)
     auto put_away = [&](int c, Stage &to) __attribute__((always_inline)) {
         short *kd = to.k + wave * 16 * D, *vd = to.v + wave * 16 * D;
-        if constexpr (E4M3) {
+        if constexpr (E2M1) {
+            if (c == 0) {
+                // the key of a value that was not finite is NaN, so that its score is, and its codes are zero
+                ke = (vbad == 255 ? 255u : ke) << 23;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)      // (any byte of 255: behind the sequence's end a page holds anything)
+                    ve.w[j] = (~ve.w[j] - 0x01010101u) & ve.w[j] & 0x80808080u ? 0 : ve.w[j];
+            }
+            auto half4 = [&](auto u) __attribute__((always_inline)) {
+                constexpr int U = decltype(u)::value;
+                *(i32x4 *)(kd + ((N4 * g + U) * 16 + r16) * 8) = H::widen4(kx4.c[U], ke);
+                i32x2 a, b;
+                H::template turn4<U>(vx4.c[U], ve.w, a, b);
+                *(i32x2 *)(vd + ((2 * U * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) = a;
+                *(i32x2 *)(vd + (((2 * U + 1) * 2 + (g & 1)) * 16 + r16) * 8 + (g >> 1) * 4) = b;
+            };
+            if (c == 0) {
+                half4(std::integral_constant<int, 0>());
+                half4(std::integral_constant<int, 1>());
+            } else if constexpr (D == 128) {
+                half4(std::integral_constant<int, 2>());
+                half4(std::integral_constant<int, 3>());
+            }
+        } else if constexpr (E4M3) {
             *(i32x4 *)(kd + ((8 * c + 2 * g) * 16 + r16) * 8) = H::widen(kx[c][0], kx[c][1]);
             *(i32x4 *)(kd + ((8 * c + 2 * g + 1) * 16 + r16) * 8) = H::widen(kx[c][2], kx[c][3]);
 #pragma unroll
@@ -1009,16 +1332,18 @@ Pages pages_args(const spd_pages *p, const spd_plan_header &h, const void *plan_
     return P;
 }
 
-// f(D, E4M3, F16) for the handle's kind
+// f(D, what the pages hold, F16) for the handle's kind
 template <class F>
 hipError_t by_kind(const spd_pages *p, F f) {
-    typedef std::true_type T;
-    typedef std::false_type N;
-    typedef std::integral_constant<int, 64> D64;
-    typedef std::integral_constant<int, 128> D128;
-    const bool e = p->cfg.cache_dtype == SPD_E4M3, h = p->cfg.dtype == SPD_F16;
-    if (p->cfg.head_dim == 64) return e ? (h ? f(D64(), T(), T()) : f(D64(), T(), N())) : (h ? f(D64(), N(), T()) : f(D64(), N(), N()));
-    return e ? (h ? f(D128(), T(), T()) : f(D128(), T(), N())) : (h ? f(D128(), N(), T()) : f(D128(), N(), N()));
+    auto type = [&](auto d, auto c) { return p->cfg.dtype == SPD_F16 ? f(d, c, std::true_type()) : f(d, c, std::false_type()); };
+    auto codes = [&](auto d) {
+        switch (p->cfg.cache_dtype) {
+            case SPD_E4M3: return type(d, std::integral_constant<int, SPD_E4M3>());
+            case SPD_E2M1: return type(d, std::integral_constant<int, SPD_E2M1>());
+            default: return type(d, std::integral_constant<int, HALVES>());
+        }
+    };
+    return p->cfg.head_dim == 64 ? codes(std::integral_constant<int, 64>()) : codes(std::integral_constant<int, 128>());
 }
 
 inline bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -1068,7 +1393,8 @@ int spd_pages_write(const spd_pages *pages, const void *plan_host, const void *p
     const dim3 grid(h.n_write, A.kv_groups + A.q_groups);
     SPD_HIP(by_kind(pages, [&](auto d, auto e, auto f) {
         constexpr int D = decltype(d)::value;
-        constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+        constexpr int E = decltype(e)::value;
+        constexpr bool F = decltype(f)::value;
         if (in_dtype == SPD_F32) hipLaunchKernelGGL((k_pages_write<float, D, E, F>), grid, dim3(256), 0, (hipStream_t)stream, A);
         else hipLaunchKernelGGL((k_pages_write<std::conditional_t<F, _Float16, __bf16>, D, E, F>), grid, dim3(256), 0, (hipStream_t)stream, A);
         return hipGetLastError();
@@ -1090,7 +1416,8 @@ int spd_pages_read(const spd_pages *pages, const void *plan_host, const void *pl
     const dim3 grid((h.max_end + 63) / 64, h.batch, c.n_kv_heads);
     SPD_HIP(by_kind(pages, [&](auto d, auto e, auto f) {
         constexpr int D = decltype(d)::value;
-        constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+        constexpr int E = decltype(e)::value;
+        constexpr bool F = decltype(f)::value;
         typedef std::conditional_t<F, _Float16, __bf16> H;
         if (out_dtype == SPD_F32) hipLaunchKernelGGL((k_pages_read<float, D, E, F>), grid, dim3(256), 0, (hipStream_t)stream, P, (float *)k_out, (float *)v_out);
         else hipLaunchKernelGGL((k_pages_read<H, D, E, F>), grid, dim3(256), 0, (hipStream_t)stream, P, (H *)k_out, (H *)v_out);
@@ -1126,7 +1453,8 @@ int spd_pages_attention(const spd_pages *pages, const void *plan_host, const voi
     hipStream_t s = (hipStream_t)stream;
     SPD_HIP(by_kind(pages, [&](auto d, auto e, auto f) {
         constexpr int D = decltype(d)::value;
-        constexpr bool E = decltype(e)::value, F = decltype(f)::value;
+        constexpr int E = decltype(e)::value;
+        constexpr bool F = decltype(f)::value;
         if (h.n_large) {
             A.P = pages_args(pages, h, plan_dev, pool, h.large);
             A.part = large;

@@ -243,9 +243,9 @@ int spd_pages_create(const spd_pages_config *cfg, spd_pages **out) {
     if (c.n_q_heads <= 0 || c.n_kv_heads <= 0 || c.head_dim <= 0 || c.page_size <= 0 || c.n_pages <= 0 || c.max_ctx <= 0) return SPD_EINVAL;
     if (c.n_q_heads % c.n_kv_heads) return SPD_EINVAL;
     if (!(c.rope_base > 0.f) || !std::isfinite(c.rope_base)) return SPD_EINVAL;
-    if ((c.dtype != SPD_BF16 && c.dtype != SPD_F16) || (c.cache_dtype != SPD_E4M3 && c.cache_dtype != SPD_BF16 && c.cache_dtype != SPD_F16))
-        return SPD_EINVAL;
-    if (c.cache_dtype != SPD_E4M3 && c.cache_dtype != c.dtype) return SPD_EUNSUPPORTED;
+    const bool coded = c.cache_dtype == SPD_E4M3 || c.cache_dtype == SPD_E2M1;
+    if ((c.dtype != SPD_BF16 && c.dtype != SPD_F16) || (!coded && c.cache_dtype != SPD_BF16 && c.cache_dtype != SPD_F16)) return SPD_EINVAL;
+    if (!coded && c.cache_dtype != c.dtype) return SPD_EUNSUPPORTED;
     if (c.head_dim != 64 && c.head_dim != 128) return SPD_EUNSUPPORTED;
     if (c.page_size != 16 && c.page_size != 32 && c.page_size != 64 && c.page_size != 128 && c.page_size != 256) return SPD_EUNSUPPORTED;
     if (c.n_q_heads / c.n_kv_heads > 16 || c.n_q_heads > 1024) return SPD_EUNSUPPORTED;
@@ -254,10 +254,10 @@ int spd_pages_create(const spd_pages_config *cfg, spd_pages **out) {
     if (!p) return SPD_EINVAL;
     p->cfg = c;
     p->group = c.n_q_heads / c.n_kv_heads;
-    p->width = c.cache_dtype == SPD_E4M3 ? 1 : 2;
+    p->row_bytes = c.cache_dtype == SPD_E2M1 ? c.head_dim / 2 + c.head_dim / 32 : c.head_dim * (c.cache_dtype == SPD_E4M3 ? 1 : 2) + 4;
     p->shift = 0;
     while ((16 << p->shift) < c.page_size) ++p->shift;
-    p->head_bytes = (size_t)c.page_size * (2 * (size_t)c.head_dim * p->width + 8);
+    p->head_bytes = (size_t)c.page_size * 2 * p->row_bytes;
     p->page_bytes = p->head_bytes * c.n_kv_heads;
     *out = p;
     return SPD_OK;
