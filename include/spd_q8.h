@@ -119,6 +119,59 @@ typedef struct spd_pages_plan_info {
 } spd_pages_plan_info;
 int spd_pages_plan_get_info(const spd_pages *pages, const void *plan_host, spd_pages_plan_info *out);
 
+/* ---------------------------------------------------------------- plan of a step, made on the device
+ *
+ * Where lengths are on the device (a step's tokens were drawn there, requests end there), so can the plan be made: spd_pages_reserve() says once, on the
+ * host, how large steps may get, and spd_pages_build() turns the requests' lengths into a step's plan, as often as there are steps, without the host. It takes pages
+ * from a free list for positions that have none yet, writes them into the page table, takes back those of requests that have ended, and says
+ * which row of the step's matrices is which position and slot.  spd_pages_write() and spd_pages_attention() take the plan as they take one
+ * that was made on the host, and give the same bits.  A captured graph holds for every step within the limits. */
+typedef struct spd_pages_limits {
+    int32_t batch;    /* requests: entries of the arrays below; at most 4096 */
+    int32_t tokens;   /* rows of the step's matrices */
+    int32_t q_len;    /* new tokens of a request.  Up to 16 / (query heads per KV head) steps take one launch of attention, else three */
+    int32_t entries;  /* pages of a request: columns of the page table */
+    int32_t window, sinks;      /* as for spd_pages_plan() */
+} spd_pages_limits;
+
+/* Host only.  plan_host: receives what the calls take for plan_host, or NULL; capacity: its bytes; bytes: receives its size; device_bytes: receives the size of
+ * plan_dev, which spd_pages_build() fills.  tokens of the plan's info are the limit's, its workspace_bytes serve every step within the limits, held is 0.
+ * SPD_EINVAL: NULL, sizes that are not positive, q_len above tokens, sinks without a window, capacity too small.
+ * SPD_EUNSUPPORTED: more than 4096 requests, 2^24 tokens, 2^28 entries in all, or 8192 pieces of 128 rows (tokens * query heads per KV head / 128, and one
+ * for every request that can have more than 16 rows). */
+int spd_pages_reserve(const spd_pages *pages, const spd_pages_limits *limits, void *plan_host, size_t capacity, size_t *bytes, size_t *device_bytes);
+
+#define SPD_STEP_RELEASE (-1)  /* q_lens[b]: the request has ended, its pages come back */
+#define SPD_STEP_LENGTHS (-1)  /* served[b]: lengths out of range, or more rows than there are */
+#define SPD_STEP_PAGE (-2)     /* served[b]: a page of the request, in the table or from the free list, is not of the pool */
+#define SPD_STEP_NO_PAGES (-3) /* served[b]: not enough free pages */
+
+/* Device arrays, int32 but for row_slot. */
+typedef struct spd_pages_step {
+    const int32_t *positions;  /* [batch] positions that are in a request's pages already */
+    const int32_t *q_lens;     /* [batch] its new tokens: 1 .. q_len of the limits, 0 (no part in the step), or SPD_STEP_RELEASE */
+    int32_t *page_table;       /* [batch][ld_table] pages of the request's positions; entries for positions that are new and in no page yet are written */
+    int64_t ld_table;          /* at least the limits' entries */
+    int32_t *free_pages;       /* [n_pages] a stack of free pages: the first *n_free are free.  NULL, with n_free and n_free_out: the table has every page */
+    const int32_t *n_free;
+    int32_t *n_free_out;       /* free pages after the step; may be n_free */
+    int32_t *positions_out;    /* [batch] positions + q_lens for requests that are served, 0 for those that have ended; may be positions, or NULL, as may the others */
+    int32_t *served;           /* [batch] new tokens of the request, or why it has no part in the step */
+    int32_t *first_row;        /* [batch + 1] where its rows begin; last, rows in use */
+    int32_t *row_seq;          /* [tokens] of each row: its request, */
+    int32_t *row_pos;          /* [tokens] its position, */
+    int64_t *row_slot;         /* [tokens] its place in the pool, page * page_size + position % page_size.  -1 for rows that are no request's, or of one not served */
+} spd_pages_step;
+
+/* Device call.  Rows go to requests in order, max(q_len, 0) to each, whether it is served or not (within the limit).  Pages that come back are pushed in the
+ * requests' order, each request's in the order of its positions; then pages are popped in the same order, for requests that need more than
+ * are left and for all that need any after them none (SPD_STEP_NO_PAGES).  A request that is not served keeps its positions (and pages that were handed to it), its
+ * rows of outputs stay as they were.  Two requests may share pages for reading; that the page of a new token is one request's alone, and a page at most once in the
+ * free list and the tables of those that have ended, is the caller's to see to: it is not checked.
+ * plan_dev: device_bytes, 16-byte aligned.  Arrays may share no memory but for what is said above.
+ * SPD_EINVAL: NULL, a plan made on the host, alignment, ld_table, shared memory. */
+int spd_pages_build(const spd_pages *pages, const void *plan_host, void *plan_dev, const spd_pages_step *step, void *stream);
+
 /* ---------------------------------------------------------------- device calls on pages
  * plan_host / plan_dev: the plan and its copy on the device (16-byte aligned).  pool: pool_bytes, 256-byte aligned. */
 
@@ -134,7 +187,7 @@ int spd_pages_write(const spd_pages *pages, const void *plan_host, const void *p
                     int64_t ld, const float *rope, void *pool, void *q_out, int64_t ld_q, void *stream);
 
 /* Reads every position of every sequence back: k_out, v_out [held][n_kv_heads][head_dim], sequence after sequence, out_dtype
- * SPD_F32 or the pool's dtype, code * scale rounded once; 16-byte aligned. */
+ * SPD_F32 or the pool's dtype, code * scale rounded once; 16-byte aligned.  SPD_EUNSUPPORTED: a plan made on the device, whose lengths the host does not know. */
 int spd_pages_read(const spd_pages *pages, const void *plan_host, const void *plan_dev, const void *pool, int32_t out_dtype,
                    void *k_out, void *v_out, void *stream);
 

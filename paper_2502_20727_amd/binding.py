@@ -18,6 +18,7 @@ from . import build
 from .workloads import Workload
 
 SPD_F32, SPD_BF16, SPD_F16, SPD_E4M3, SPD_E2M1 = 0, 1, 2, 3, 4
+SPD_STEP_RELEASE, SPD_STEP_LENGTHS, SPD_STEP_PAGE, SPD_STEP_NO_PAGES = -1, -1, -2, -3
 SPD_OK, SPD_EINVAL, SPD_EUNSUPPORTED, SPD_EHIP, SPD_ETOOBIG = 0, -1, -2, -3, -4
 SPD_STATIC_WORKSPACE_BYTES = 64 << 20
 SPD_ALL_RANKS = -1
@@ -72,6 +73,16 @@ class spd_pages_sizes(C.Structure):
 
 class spd_pages_plan_info(C.Structure):
     _fields_ = [("batch", C.c_int32), ("tokens", C.c_int32), ("held", C.c_int64), ("workspace_bytes", C.c_size_t)]
+
+
+class spd_pages_limits(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "tokens", "q_len", "entries", "window", "sinks")]
+
+
+class spd_pages_step(C.Structure):
+    _fields_ = [("positions", C.c_void_p), ("q_lens", C.c_void_p), ("page_table", C.c_void_p), ("ld_table", C.c_int64)] + \
+               [(n, C.c_void_p) for n in ("free_pages", "n_free", "n_free_out", "positions_out", "served", "first_row", "row_seq", "row_pos",
+                                          "row_slot")]
 
 
 _lib = _torch = _int8 = _float32 = _raw_stream = _device = None
@@ -131,6 +142,9 @@ _PROTOS = {
     "spd_pages_plan": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                  C.c_void_p, C.c_size_t, C.POINTER(C.c_size_t)]),
     "spd_pages_plan_get_info": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(spd_pages_plan_info)]),
+    "spd_pages_reserve": (C.c_int, [C.c_void_p, C.POINTER(spd_pages_limits), C.c_void_p, C.c_size_t, C.POINTER(C.c_size_t),
+                                    C.POINTER(C.c_size_t)]),
+    "spd_pages_build": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(spd_pages_step), C.c_void_p]),
     "spd_pages_write": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_int64, C.c_void_p]),
     "spd_pages_read": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
@@ -556,6 +570,43 @@ def spd_pages_plan_get_info(pages: int, plan: np.ndarray) -> spd_pages_plan_info
     return i
 
 
+def spd_pages_reserve(pages: int, limits: spd_pages_limits):
+    """(host part of the plans that spd_pages_build() makes for steps within the limits, bytes of the device's part)."""
+    need, device = C.c_size_t(0), C.c_size_t(0)
+
+    def call(out, n):
+        _check(lib().spd_pages_reserve(pages, C.byref(limits), out, n, C.byref(need), C.byref(device)), "spd_pages_reserve")
+    call(None, 0)
+    plan = np.empty(need.value, dtype=np.uint8)
+    call(plan.ctypes.data, plan.size)
+    return plan, device.value
+
+
+def spd_pages_build(pages: int, plan: "DevicePlan", positions, q_lens, page_table, free_pages=None, n_free=None, n_free_out=None, positions_out=None,
+                    served=None, first_row=None, row_seq=None, row_pos=None, row_slot=None, stream=None) -> None:
+    """Device tensors, int32 (row_slot: int64): positions, q_lens, positions_out, served [batch], page_table [batch, entries or more] with contiguous rows,
+    free_pages [n_pages], n_free, n_free_out [1], first_row [batch + 1], row_seq, row_pos, row_slot [tokens]."""
+    int32 = _torch.int32
+
+    def array(t, n, what, dtype=int32):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.numel() != n or not (t.is_cuda and t.is_contiguous()):
+            raise ValueError(f"{what}: a contiguous tensor of {n} {dtype} on the device wanted")
+        return t.data_ptr()
+    batch, tokens = plan.batch, plan.tokens
+    if page_table.dtype is not int32 or page_table.dim() != 2 or page_table.shape[1] < plan.entries:
+        raise ValueError(f"page_table: int32 [{batch}, {plan.entries} or more] wanted")
+    table, ld = _rows(page_table, (batch, page_table.shape[1]), "page_table")
+    step = spd_pages_step(array(positions, batch, "positions"), array(q_lens, batch, "q_lens"), table, ld,
+                          array(free_pages, plan.n_pages, "free_pages"), array(n_free, 1, "n_free"), array(n_free_out, 1, "n_free_out"),
+                          array(positions_out, batch, "positions_out"), array(served, batch, "served"), array(first_row, batch + 1, "first_row"),
+                          array(row_seq, tokens, "row_seq"), array(row_pos, tokens, "row_pos"), array(row_slot, tokens, "row_slot", _torch.int64))
+    rc = _lib.spd_pages_build(pages, plan.host_ptr, plan.device_ptr, step, _current_stream() if stream is None else _stream_ptr(stream))
+    if rc:
+        raise SpdError(rc, "spd_pages_build")
+
+
 def _type(t) -> int:
     """SPD_* code of a torch tensor's element type."""
     code = _TYPES.get(t.dtype)
@@ -859,6 +910,28 @@ class PagePlan:
         self.info = spd_pages_plan_get_info(pages.ctx, self.host)
         self.device = torch.from_numpy(self.host).to(pages.device)
         c = pages.cfg
+        self.tokens, self.workspace_bytes, self.dtype = self.info.tokens, self.info.workspace_bytes, c.dtype
+        self.qkv_cols = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
+        self.q_shape, self.held_shape = (self.tokens, c.n_q_heads * c.head_dim), (self.info.held, c.n_kv_heads, c.head_dim)
+        self.pool_bytes, self.rope_bytes = pages.sizes.pool_bytes, pages.sizes.rope_bytes
+        self.host_ptr, self.device_ptr = self.host.ctypes.data, self.device.data_ptr()
+        n = self.workspace_bytes
+        self.workspace = torch.zeros(n, dtype=torch.uint8, device=pages.device) if n else None
+
+
+class DevicePlan:
+    """Plans of steps that spd_pages_build() makes on the device, one after the other in the same place, for steps within the limits; their scratch, cleared on
+    torch's current stream.  Takes the place of a PagePlan in spd_pages_write() and spd_pages_attention(), whose matrices have `limits.tokens` rows: those that are no
+    request's are neither read nor written.  The object has to live until its calls, and graphs that hold them, are over."""
+
+    def __init__(self, pages: DevicePages, limits: spd_pages_limits):
+        import torch
+        self.pages, self.limits = pages, limits
+        self.host, device_bytes = spd_pages_reserve(pages.ctx, limits)
+        self.info = spd_pages_plan_get_info(pages.ctx, self.host)
+        self.device = torch.zeros(device_bytes, dtype=torch.uint8, device=pages.device)
+        c = pages.cfg
+        self.batch, self.entries, self.n_pages = limits.batch, limits.entries, c.n_pages
         self.tokens, self.workspace_bytes, self.dtype = self.info.tokens, self.info.workspace_bytes, c.dtype
         self.qkv_cols = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
         self.q_shape, self.held_shape = (self.tokens, c.n_q_heads * c.head_dim), (self.info.held, c.n_kv_heads, c.head_dim)

@@ -18,7 +18,7 @@ HIP_LIB = os.path.join(PKG_DIR, "libspd_hip.so")
 INPUTS_LIB = os.path.join(PKG_DIR, "libspd_inputs.so")
 
 HIP_SOURCES = ["spd_host.cpp", "spd_pages_host.cpp", "spd_q8_host.cpp", "spd_kernels_f32.hip", "spd_kernels_bf16.hip",
-               "spd_forward.hip", "spd_pages.hip", "spd_q8.hip"]
+               "spd_forward.hip", "spd_pages.hip", "spd_pages_build.hip", "spd_q8.hip"]
 
 
 def _run(cmd):

@@ -1,6 +1,8 @@
 // Paged KV cache: the handle, the plan of a step as host and kernels read it, and the layout of a page.
 #pragma once
 
+#include <cmath>
+
 #include "spd_internal.h"
 #include "spd_q8.h"
 
@@ -39,6 +41,72 @@ constexpr int SPD_SMALL_WAVES = 8;       // of a workgroup of the kernel for few
 constexpr int SPD_SMALL_ROWS = 16;       // rows (token x query head of the KV group) of an item of the kernel for few of them
 constexpr int SPD_LARGE_ROWS = 128;      // ... and of the kernel for many
 
+// ------------------------------------------------------------------------------------------
+// How work is cut, on the host and on the device alike: a step has the same items, and the same results, whoever planned it.
+// ------------------------------------------------------------------------------------------
+// The chip holds this many workgroups of the kernel for few rows at once (one of eight waves per compute unit: 48 sequences of up to 16000
+// 31.0 us, two of four waves 33 to 38), two per compute unit of the one for many.
+constexpr int SPD_SMALL_TARGET = 256, SPD_COMPUTE_UNITS = 256;
+constexpr int SPD_LARGE_MIN_BLOCKS = 8;
+
+// the visible blocks of rows row0 .. row0 + rows - 1 of a sequence whose first new position is `pos`
+struct spd_piece {
+    int32_t sink_blocks, block0, total;
+};
+SPD_HD spd_piece spd_piece_of(int group, int pos, int row0, int rows, int window, int sinks) {
+    spd_piece w;
+    const int first = pos + row0 / group, last = pos + (row0 + rows - 1) / group;
+    const int low = window && first >= window ? (first - window + 1) / 16 : 0;      // first block of the first row's window
+    w.sink_blocks = (int)(((int64_t)(sinks < last + 1 ? sinks : last + 1) + 15) / 16);
+    w.block0 = low;
+    if (w.sink_blocks >= low) w.sink_blocks = w.block0 = 0;
+    w.total = w.sink_blocks + last / 16 + 1 - w.block0;
+    return w;
+}
+
+// Pieces are cut into items of at most `chunk` blocks, first what each of `target` workgroups would have of them; `unit` blocks go together.
+SPD_HD int64_t spd_first_chunk(int64_t total, int kv, int target, int unit) {
+    const int64_t c = ((total * kv + target - 1) / target + unit - 1) / unit * unit;
+    return c > unit ? c : unit;
+}
+// what lengths leave over after whole chunks makes more items than the target: longer chunks, SPD_LONGER times at most, while cutting is what makes them
+constexpr int SPD_LONGER = 16;
+SPD_HD int64_t spd_next_chunk(int64_t chunk, int unit) { return (chunk + chunk / 16 + unit) / unit * unit; }
+SPD_HD int spd_parts(int total, int64_t chunk, int most) {
+    const int64_t n = (total + chunk - 1) / chunk;
+    return n < most ? (int)n : most;
+}
+// the most items a piece is cut into.  Many rows:
+SPD_HD int spd_most_large(int blocks) { return blocks / SPD_LARGE_MIN_BLOCKS > 1 ? blocks / SPD_LARGE_MIN_BLOCKS : 1; }
+// Rows whose blocks go round a workgroup's waves three times or less are not cut.  Beyond that a turn of a wave (a pair of blocks) takes
+// about as long as 0.15 of the join of a part by one of `sets` sets of threads, which gives the number of parts that ends first when
+// there is room for all of them.  (us a call, 0.05 / 0.1 / 0.3: 16 sequences of 4096 11.5 / 11.0 / 11.5, one of 32000 17.9 / 15.8 / 14.6; 64
+// of 500: 6.8 uncut, 8.4 in two parts)
+SPD_HD int spd_sets(int group) { return group > 8 ? 1 : group > 4 ? 2 : group > 2 ? 4 : group > 1 ? 8 : 16; }
+SPD_HD int spd_most_small(int blocks, int sets) {
+    if (blocks <= 3 * 2 * SPD_SMALL_WAVES) return 1;
+    const double a = sqrt(0.15 * blocks * sets), b = blocks / 8.0;
+    return (int)(a < b ? a : b);
+}
+// Many rows: cut so that a workgroup per compute unit has work, or one and a half, or two (halves = 2, 3, 4), whichever is estimated to end first: the time
+// in us of `items` whose longest has `longest` blocks, `slots` of them parts.  A tile of four
+// blocks takes a workgroup 1.65 us by itself and 2.35 beside another; a join costs a launch and its partial results twice (66 KB each, 0.018 us).
+// us a call, cut for 256 / 384 / 512 workgroups: three windowed chunks of 333 tokens, 5 heads 23.2 / 26.3 / 26.1, without the window 38.8 / 37.2 / 35.4, the
+// same over e4m3 41.3 / 37.8 / 34.6, d 64 28.7 / 27.2 / 27.9, two of 333 behind 16000 64.3 / 62.1 / 55.7, one of 300 behind 2000, 8 heads of 8 63.3 / 49.1 /
+// 41.9.  Of 200 calls of all types and widths that the three cut differently this picks cuts that are 1 % slower than the best of them on average, 15 % at
+// most (with a part at 0.04 us: 3 % and 39 %).
+SPD_HD double spd_estimate_large(int longest, int64_t items, int64_t slots, int kv) {
+    const int64_t groups = items * kv;
+    const double tiles = (longest + 3) / 4, rounds = (double)((groups + 2 * SPD_COMPUTE_UNITS - 1) / (2 * SPD_COMPUTE_UNITS));
+    return tiles * (groups <= SPD_COMPUTE_UNITS ? 1.65 : 2.35 * rounds) + (slots ? 3.0 + 0.018 * slots * kv : 0.0);
+}
+// blocks of the i-th of `parts` items of a piece of `total` blocks
+SPD_HD int spd_item_first(int total, int unit, int parts, int i) { return (int)((int64_t)i * ((total + unit - 1) / unit) / parts) * unit; }
+SPD_HD int spd_item_count(int total, int unit, int parts, int i) {
+    const int end = spd_item_first(total, unit, parts, i + 1);
+    return (end < total ? end : total) - spd_item_first(total, unit, parts, i);
+}
+
 struct spd_plan_seq {
     int32_t pos, q_len, tok0, table;     // first new position, new tokens, row of the first, first entry in the plan's page table
     int64_t held0;                       // row of position 0 in spd_pages_read()'s output
@@ -72,7 +140,26 @@ struct spd_plan_header {
     int32_t seqs, table, small, large, merge, write;            // byte offsets
     int32_t merge_rows, max_end;         // most rows of a merge, most positions of a sequence
     size_t bytes, part_small, part_large, workspace;             // of the plan; byte offsets into the workspace (counters at 0); its size
+    // A plan that is made on the device: on the host the n_* are the most there can be (and so many workgroups are launched), on the device those of the step.
+    int32_t on_device;
+    int32_t q_len, entries;              // limits: new tokens of a request, entries of its row of the page table
+    int32_t reqs, cuts;                  // byte offsets of what the first of its kernels leaves for the second
+    size_t device_bytes;
+    int32_t rows, free0, top;            // of the step: rows in use, free pages before it, and with those that came back
 };
+// what is known of a request, and of a piece of 128 of its rows, between the two kernels
+struct spd_plan_req {
+    int32_t pos, q_len, tok0, state;     // first position, rows, the first row; 0: fine, 1: pages come back, else why it is not served
+    int32_t need0, back0, back;          // new pages, pages that come back: of those before it, its own
+    int32_t item0, parts, slot0, group;  // few rows
+    int32_t piece0, pieces;              // many
+    int32_t write0, writes;              // 16-position blocks that receive new tokens
+    int32_t pad;
+};
+struct spd_plan_cut {
+    int32_t item0, parts, slot0, merge;
+};
+constexpr int SPD_BUILD_BATCH = 4096, SPD_BUILD_PIECES = 8192;      // most requests, pieces of 128 rows, of a plan made on the device
 
 // partial results: per slot and KV head `rows` x (d outputs, then maximum and sum), fp32
 inline size_t spd_part_floats(int rows, int d) { return (size_t)rows * (d + 2); }

@@ -172,6 +172,8 @@ struct Pages {
     int seqs, table, list;      // offsets into the plan
     int shift, page_size, kv, group;
 };
+// (a plan made on the device has as many items as the step has; more workgroups may have been launched)
+__device__ __forceinline__ const spd_plan_header &header_of(const Pages &P) { return *(const spd_plan_header *)P.plan; }
 // where a sequence's block of 16 positions lies, for one head: its page's share of the head, and the block in the page
 struct Block {
     char *head;
@@ -276,6 +278,7 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
     constexpr int ROW = E2M1 ? D / 2 : D * W;                                          // bytes of a row
     const Pages &P = A.P;
     const spd_plan_block it = ((const spd_plan_block *)(P.plan + P.list))[blockIdx.x];
+    if ((int)blockIdx.x >= header_of(P).n_write || it.block < 0) return;
     const spd_plan_seq &s = it.s;
     const int r = threadIdx.x >> 4, unit = (threadIdx.x & 15) / TPR, f0 = (threadIdx.x % TPR) * 8;
     const int pos = it.block * 16 + r, lo = it.block * 16 > s.pos ? 0 : s.pos - it.block * 16,
@@ -679,6 +682,7 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
     const Pages &P = A.P;
     const int head = blockIdx.x % P.kv;
     const spd_plan_item it = ((const spd_plan_item *)(P.plan + P.list))[blockIdx.x / P.kv];
+    if ((int)(blockIdx.x / P.kv) >= header_of(P).n_small || it.count == 0) return;
     const spd_plan_seq &s = it.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 15, g = lane >> 4;
@@ -964,6 +968,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     const Pages &P = A.P;
     const int head = blockIdx.x % P.kv;
     const spd_plan_item it = ((const spd_plan_item *)(P.plan + P.list))[blockIdx.x / P.kv];
+    if ((int)(blockIdx.x / P.kv) >= header_of(P).n_large || it.count == 0) return;
     const spd_plan_seq &s = it.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
@@ -1264,7 +1269,7 @@ __global__ void __launch_bounds__(64) k_attend_merge(Pages P, const float *part,
     const spd_plan_merge j = ((const spd_plan_merge *)(P.plan + P.list))[blockIdx.x / P.kv];
     const int lane = threadIdx.x, t = blockIdx.z, col = lane & 31, half = lane >> 5;
     const int r0 = blockIdx.y * 32;
-    if (r0 >= j.rows) return;                    // (whole workgroup)
+    if ((int)(blockIdx.x / P.kv) >= header_of(P).n_merge || r0 >= j.rows) return;      // (whole workgroup)
     const spd_plan_seq &s = j.s;
     const size_t step = (size_t)P.kv * CAP * (D + 2);
     const float *p = part + ((size_t)j.slot0 * P.kv + head) * (CAP * (D + 2));
@@ -1409,6 +1414,7 @@ int spd_pages_read(const spd_pages *pages, const void *plan_host, const void *pl
     if (rc != SPD_OK) return rc;
     const spd_pages_config &c = pages->cfg;
     if (out_dtype != SPD_F32 && out_dtype != c.dtype) return SPD_EINVAL;
+    if (h.on_device) return SPD_EUNSUPPORTED;
     if (!h.held) return SPD_OK;
     if (!pool || !k_out || !v_out || !aligned(pool, 256) || !aligned(k_out, 16) || !aligned(v_out, 16)) return SPD_EINVAL;
     (void)hipGetLastError();

@@ -9,57 +9,44 @@
 
 namespace {
 
-// The chip holds SMALL_TARGET workgroups of the kernel for few rows at once (one of eight waves per compute unit: 48 sequences of up to 16000
-// 31.0 us, two of four waves 33 to 38), two per compute unit of the one for many.
-constexpr int SMALL_TARGET = 256, COMPUTE_UNITS = 256;
-constexpr int LARGE_MIN_BLOCKS = 8;
-
-struct Piece {
-    int seq, row0, rows, sink_blocks, block0, total;
+struct Piece : spd_piece {
+    int seq, row0, rows;
 };
 
-// the visible blocks of rows row0 .. row0 + rows - 1
 Piece piece_of(const spd_pages *P, int seq, int pos, int row0, int rows, int window, int sinks) {
     Piece w;
+    (spd_piece &)w = spd_piece_of(P->group, pos, row0, rows, window, sinks);
     w.seq = seq;
     w.row0 = row0;
     w.rows = rows;
-    const int first = pos + row0 / P->group, last = pos + (row0 + rows - 1) / P->group;
-    const int low = window && first >= window ? (first - window + 1) / 16 : 0;      // first block of the first row's window
-    w.sink_blocks = (int)(((int64_t)std::min(sinks, last + 1) + 15) / 16);
-    w.block0 = low;
-    if (w.sink_blocks >= low) w.sink_blocks = w.block0 = 0;
-    w.total = w.sink_blocks + last / 16 + 1 - w.block0;
     return w;
 }
 
-// Cuts pieces into items of at most `chunk` blocks, what each of `target` workgroups would have of them (0: not at all), into no more than `target`
-// items where the pieces are fewer; `unit` blocks go together.  most(blocks): the most items a piece is cut into.
+// Cuts pieces into items for `target` workgroups (0: not at all), into no more than so many where the pieces are fewer.  most(blocks): the most items a
+// piece is cut into.
 template <class Most>
 void cut(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs, int kv, int target, int unit, Most most,
          std::vector<spd_plan_item> &items, std::vector<spd_plan_merge> &merges, int &slots) {
     int64_t total = 0;
     for (const Piece &w : pieces) total += w.total;
-    int64_t chunk = target ? std::max<int64_t>(unit, ((total * kv + target - 1) / target + unit - 1) / unit * unit) : 0;
-    auto parts_of = [&](const Piece &w) { return chunk ? (int)std::min<int64_t>(most(w.total), (w.total + chunk - 1) / chunk) : 1; };
-    // (what lengths leave over after whole chunks makes more items than the target: longer chunks, while cutting is what makes them)
-    for (int i = 0; i < 16 && chunk; ++i) {
+    int64_t chunk = target ? spd_first_chunk(total, kv, target, unit) : 0;
+    auto parts_of = [&](const Piece &w) { return chunk ? spd_parts(w.total, chunk, most(w.total)) : 1; };
+    for (int i = 0; i < SPD_LONGER && chunk; ++i) {
         int64_t n = 0;
         for (const Piece &w : pieces) n += parts_of(w);
         if (n * kv <= target || n == (int64_t)pieces.size()) break;
-        chunk = (chunk + chunk / 16 + unit) / unit * unit;
+        chunk = spd_next_chunk(chunk, unit);
     }
     for (const Piece &w : pieces) {
-        const int units = (w.total + unit - 1) / unit;
-        const int parts = std::min(units, parts_of(w));
+        const int parts = std::min((w.total + unit - 1) / unit, parts_of(w));
         for (int i = 0; i < parts; ++i) {
             spd_plan_item it;
             it.s = seqs[w.seq];
             it.row0 = w.row0;
             it.sink_blocks = w.sink_blocks;
             it.block0 = w.block0;
-            it.first = (int)((int64_t)i * units / parts) * unit;
-            it.count = std::min((int)((int64_t)(i + 1) * units / parts) * unit, w.total) - it.first;
+            it.first = spd_item_first(w.total, unit, parts, i);
+            it.count = spd_item_count(w.total, unit, parts, i);
             it.slot = parts > 1 ? slots + i : -1;
             it.slot0 = slots;
             it.parts = parts;
@@ -76,12 +63,6 @@ void cut(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs
     std::stable_sort(items.begin(), items.end(), [](const spd_plan_item &a, const spd_plan_item &b) { return a.count > b.count; });
 }
 
-// Many rows: cut so that a workgroup per compute unit has work, or one and a half, or two, whichever is estimated to end first.  A tile of four
-// blocks takes a workgroup 1.65 us by itself and 2.35 beside another; a join costs a launch and its partial results twice (66 KB each, 0.018 us).
-// us a call, cut for 256 / 384 / 512 workgroups: three windowed chunks of 333 tokens, 5 heads 23.2 / 26.3 / 26.1, without the window 38.8 / 37.2 / 35.4, the
-// same over e4m3 41.3 / 37.8 / 34.6, d 64 28.7 / 27.2 / 27.9, two of 333 behind 16000 64.3 / 62.1 / 55.7, one of 300 behind 2000, 8 heads of 8 63.3 / 49.1 /
-// 41.9.  Of 200 calls of all types and widths that the three cut differently this picks cuts that are 1 % slower than the best of them on average, 15 % at
-// most (with a part at 0.04 us: 3 % and 39 %).
 void cut_large(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs, int kv, std::vector<spd_plan_item> &items,
                std::vector<spd_plan_merge> &merges, int &slots) {
     if (pieces.empty()) return;
@@ -90,10 +71,8 @@ void cut_large(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq>
         std::vector<spd_plan_item> i;
         std::vector<spd_plan_merge> m;
         int n = 0;
-        cut(pieces, seqs, kv, COMPUTE_UNITS * halves / 2, 4, [](int blocks) { return std::max(1, blocks / LARGE_MIN_BLOCKS); }, i, m, n);
-        const int64_t groups = (int64_t)i.size() * kv;
-        const double tiles = (i[0].count + 3) / 4, rounds = (double)((groups + 2 * COMPUTE_UNITS - 1) / (2 * COMPUTE_UNITS));
-        const double us = tiles * (groups <= COMPUTE_UNITS ? 1.65 : 2.35 * rounds) + (n ? 3.0 + 0.018 * n * kv : 0.0);
+        cut(pieces, seqs, kv, SPD_COMPUTE_UNITS * halves / 2, 4, spd_most_large, i, m, n);
+        const double us = spd_estimate_large(i[0].count, (int64_t)i.size(), n, kv);
         if (halves == 2 || us < least) {
             least = us;
             items.swap(i);
@@ -182,13 +161,9 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
     std::vector<spd_plan_merge> joined, merges;      // (the rows of the kernel for few are joined by the last of their items)
     int small_slots = 0, large_slots = 0;
     const bool counted = (int64_t)few.size() * c.n_kv_heads <= SPD_COUNTERS;
-    // Rows whose blocks go round a workgroup's waves three times or less are not cut.  Beyond that a turn of a wave (a pair of blocks) takes
-    // about as long as 0.15 of the join of a part by one of `sets` sets of threads, which gives the number of parts that ends first when
-    // there is room for all of them.  (us a call, 0.05 / 0.1 / 0.3: 16 sequences of 4096 11.5 / 11.0 / 11.5, one of 32000 17.9 / 15.8 / 14.6; 64
-    // of 500: 6.8 uncut, 8.4 in two parts)
-    const int sets = P->group > 8 ? 1 : P->group > 4 ? 2 : P->group > 2 ? 4 : P->group > 1 ? 8 : 16;
-    auto most_small = [&](int blocks) { return blocks <= 3 * 2 * SPD_SMALL_WAVES ? 1 : (int)std::min(std::sqrt(0.15 * blocks * sets), blocks / 8.0); };
-    cut(few, seqs, c.n_kv_heads, counted ? SMALL_TARGET : 0, 2, most_small, small, joined, small_slots);
+    const int sets = spd_sets(P->group);
+    auto most_small = [&](int blocks) { return spd_most_small(blocks, sets); };
+    cut(few, seqs, c.n_kv_heads, counted ? SPD_SMALL_TARGET : 0, 2, most_small, small, joined, small_slots);
     cut_large(many, seqs, c.n_kv_heads, large, merges, large_slots);
     for (const spd_plan_merge &m : merges) h.merge_rows = std::max(h.merge_rows, m.rows);
 
@@ -311,6 +286,66 @@ int spd_pages_plan_get_info(const spd_pages *pages, const void *plan_host, spd_p
     out->tokens = h.tokens;
     out->held = h.held;
     out->workspace_bytes = h.workspace;
+    return SPD_OK;
+}
+
+int spd_pages_reserve(const spd_pages *pages, const spd_pages_limits *limits, void *plan_host, size_t capacity, size_t *bytes, size_t *device_bytes) {
+    if (!pages || !limits || !bytes || !device_bytes) return SPD_EINVAL;
+    const spd_pages_config &c = pages->cfg;
+    const spd_pages_limits &l = *limits;
+    if (l.batch <= 0 || l.tokens <= 0 || l.q_len <= 0 || l.q_len > l.tokens || l.entries <= 0 || l.window < 0 || l.sinks < 0 || (l.sinks && !l.window)) return SPD_EINVAL;
+    if (l.batch > SPD_BUILD_BATCH || l.tokens > (1 << 24) || (int64_t)l.batch * l.entries > (1 << 28)) return SPD_EUNSUPPORTED;
+    const int64_t rows = (int64_t)l.tokens * pages->group, kv = c.n_kv_heads;
+    const int64_t most_few = std::min(l.batch, l.tokens);
+    int64_t pieces = 0;      // of many rows
+    if ((int64_t)l.q_len * pages->group > SPD_SMALL_ROWS) pieces = rows / SPD_LARGE_ROWS + std::min<int64_t>(l.batch, rows / (SPD_SMALL_ROWS + 1));
+    if (pieces > SPD_BUILD_PIECES) return SPD_EUNSUPPORTED;
+    // Items, and those of them that are parts: with no more items than the target no more parts than that; with chunks made longer SPD_LONGER times, 2.6 times
+    // what a workgroup would have, a piece that is longer than that has less than twice its length's worth of them.
+    const int64_t small_slots = SPD_SMALL_TARGET / kv, large_slots = pieces ? 2 * SPD_COMPUTE_UNITS / kv : 0;
+    spd_plan_header h;
+    std::memset(&h, 0, sizeof(h));
+    h.magic = SPD_PLAN_MAGIC;
+    h.batch = l.batch;
+    h.tokens = l.tokens;
+    h.window = l.window;
+    h.sinks = l.sinks;
+    h.n_small = (int)(most_few + small_slots);
+    h.n_large = (int)(pieces + large_slots);
+    h.n_merge = (int)std::min<int64_t>(pieces, large_slots / 2);
+    h.n_write = (int)std::min<int64_t>(l.tokens, l.tokens / 16 + 2 * most_few);
+    h.cfg = c;
+    h.merge_rows = SPD_LARGE_ROWS;
+    h.on_device = 1;
+    h.q_len = l.q_len;
+    h.entries = l.entries;
+    size_t at = sizeof(h);
+    auto room = [&](size_t n, size_t size) {
+        at = (at + 15) & ~(size_t)15;
+        const size_t here = at;
+        at += n * size;
+        return (int)here;
+    };
+    h.seqs = room(l.batch, sizeof(spd_plan_seq));
+    h.reqs = room(l.batch, sizeof(spd_plan_req));
+    h.cuts = room(pieces, sizeof(spd_plan_cut));
+    h.small = room(h.n_small, sizeof(spd_plan_item));
+    h.large = room(h.n_large, sizeof(spd_plan_item));
+    h.merge = room(h.n_merge, sizeof(spd_plan_merge));
+    h.write = room(h.n_write, sizeof(spd_plan_block));
+    h.table = room((size_t)l.batch * l.entries, 4);
+    at = spd_align256(at);
+    if (at > 0x7fffffffull) return SPD_EUNSUPPORTED;
+    *bytes = (sizeof(h) + 15) & ~(size_t)15;
+    *device_bytes = h.device_bytes = at;
+    h.bytes = *bytes;
+    h.part_small = small_slots || large_slots ? SPD_COUNTERS * 4 : 0;
+    h.part_large = h.part_small + spd_align256((size_t)(small_slots * kv) * spd_part_floats(SPD_SMALL_ROWS, c.head_dim) * 4);
+    h.workspace = h.part_large + spd_align256((size_t)(large_slots * kv) * spd_part_floats(SPD_LARGE_ROWS, c.head_dim) * 4);
+    if (!plan_host) return SPD_OK;
+    if (capacity < h.bytes) return SPD_EINVAL;
+    std::memset(plan_host, 0, h.bytes);
+    std::memcpy(plan_host, &h, sizeof(h));
     return SPD_OK;
 }
 
