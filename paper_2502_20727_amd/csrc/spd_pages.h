@@ -53,15 +53,17 @@ constexpr int SPD_LARGE_MIN_BLOCKS = 8;
 struct spd_piece {
     int32_t sink_blocks, block0, total;
 };
-SPD_HD spd_piece spd_piece_of(int group, int pos, int row0, int rows, int window, int sinks) {
+SPD_HD spd_piece spd_piece_between(int first, int last, int window, int sinks) {      // to queries at positions first .. last
     spd_piece w;
-    const int first = pos + row0 / group, last = pos + (row0 + rows - 1) / group;
     const int low = window && first >= window ? (first - window + 1) / 16 : 0;      // first block of the first row's window
     w.sink_blocks = (int)(((int64_t)(sinks < last + 1 ? sinks : last + 1) + 15) / 16);
     w.block0 = low;
     if (w.sink_blocks >= low) w.sink_blocks = w.block0 = 0;
     w.total = w.sink_blocks + last / 16 + 1 - w.block0;
     return w;
+}
+SPD_HD spd_piece spd_piece_of(int group, int pos, int row0, int rows, int window, int sinks) {
+    return spd_piece_between(pos + row0 / group, pos + (row0 + rows - 1) / group, window, sinks);
 }
 
 // Pieces are cut into items of at most `chunk` blocks, first what each of `target` workgroups would have of them; `unit` blocks go together.
@@ -85,8 +87,11 @@ SPD_HD int spd_most_large(int blocks) { return blocks / SPD_LARGE_MIN_BLOCKS > 1
 SPD_HD int spd_sets(int group) { return group > 8 ? 1 : group > 4 ? 2 : group > 2 ? 4 : group > 1 ? 8 : 16; }
 SPD_HD int spd_most_small(int blocks, int sets) {
     if (blocks <= 3 * 2 * SPD_SMALL_WAVES) return 1;
-    const double a = sqrt(0.15 * blocks * sets), b = blocks / 8.0;
-    return (int)(a < b ? a : b);
+    const int square = 3 * blocks * sets / 20;      // (blocks: 2^23 at most)
+    int n = (int)sqrtf((float)square);
+    while (n * n > square) --n;
+    while ((n + 1) * (n + 1) <= square) ++n;
+    return n < blocks / 8 ? n : blocks / 8;
 }
 // Many rows: cut so that a workgroup per compute unit has work, or one and a half, or two (halves = 2, 3, 4), whichever is estimated to end first: the time
 // in us of `items` whose longest has `longest` blocks, `slots` of them parts.  A tile of four
@@ -101,7 +106,10 @@ SPD_HD double spd_estimate_large(int longest, int64_t items, int64_t slots, int 
     return tiles * (groups <= SPD_COMPUTE_UNITS ? 1.65 : 2.35 * rounds) + (slots ? 3.0 + 0.018 * slots * kv : 0.0);
 }
 // blocks of the i-th of `parts` items of a piece of `total` blocks
-SPD_HD int spd_item_first(int total, int unit, int parts, int i) { return (int)((int64_t)i * ((total + unit - 1) / unit) / parts) * unit; }
+SPD_HD int spd_item_first(int total, int unit, int parts, int i) {      // i * units / parts whole units (parts: some hundred at most)
+    const unsigned units = (total + unit - 1) / unit, n = parts;
+    return (int)(i * (units / n) + i * (units % n) / n) * unit;
+}
 SPD_HD int spd_item_count(int total, int unit, int parts, int i) {
     const int end = spd_item_first(total, unit, parts, i + 1);
     return (end < total ? end : total) - spd_item_first(total, unit, parts, i);
@@ -143,21 +151,24 @@ struct spd_plan_header {
     // A plan that is made on the device: on the host the n_* are the most there can be (and so many workgroups are launched), on the device those of the step.
     int32_t on_device;
     int32_t q_len, entries;              // limits: new tokens of a request, entries of its row of the page table
-    int32_t reqs, cuts;                  // byte offsets of what the first of its kernels leaves for the second
+    int32_t reqs, cuts, backs, order;           // byte offsets of what the first of its kernels leaves for the second
     size_t device_bytes;
-    int32_t rows, free0, top;            // of the step: rows in use, free pages before it, and with those that came back
+    int32_t rows, free0, top, n_backs;   // of the step: rows in use, free pages before it, and with those that came back; requests that gave some back
+    int32_t sorted;                      // pieces of few rows begin at the items that `order` says
 };
 // what is known of a request, and of a piece of 128 of its rows, between the two kernels
 struct spd_plan_req {
     int32_t pos, q_len, tok0, state;     // first position, rows, the first row; 0: fine, 1: pages come back, else why it is not served
-    int32_t need0, back0, back;          // new pages, pages that come back: of those before it, its own
+    int32_t need0, back0, back, few;     // new pages, pages that come back: of those before it, its own; number of its piece of few rows
     int32_t item0, parts, slot0, group;  // few rows
     int32_t piece0, pieces;              // many
     int32_t write0, writes;              // 16-position blocks that receive new tokens
-    int32_t pad;
 };
 struct spd_plan_cut {
     int32_t item0, parts, slot0, merge;
+};
+struct spd_plan_back {                   // a request whose pages come back: pages that come back before its own
+    int32_t back0, req;
 };
 constexpr int SPD_BUILD_BATCH = 4096, SPD_BUILD_PIECES = 8192;      // most requests, pieces of 128 rows, of a plan made on the device
 

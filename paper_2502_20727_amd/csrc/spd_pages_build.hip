@@ -20,424 +20,419 @@ struct BuildArgs {
     char *plan;
     int64_t ld_table;
     int batch, tokens, q_len, entries, window, sinks;      // limits
-    int page_size, n_pages, kv, group, most_end;           // most_end: positions a request may have
-    int seqs, reqs, cuts, small, large, merge, write, table;      // byte offsets
+    unsigned by_group;                                     // 2^32 / group, rounded up
+    int page_size, page_shift, n_pages, kv, group, most_end;      // most_end: positions a request may have
+    int seqs, reqs, cuts, backs, order, small, large, merge, write, table;      // byte offsets
     int tails;                                             // workgroups of the second kernel for rows behind the last request
 };
 
-constexpr int THREADS = 1024, WAVES = THREADS / 64;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+constexpr int THREADS = 1024, WAVES = THREADS / 64;      // of the first kernel, at most
 
-// Exclusive prefix sums over the workgroup of N numbers a thread, and their totals.  `lds`: WAVES * N.
+__device__ __forceinline__ int ceil_div(int a, int b) { return (int)((unsigned)(a + b - 1) / (unsigned)b); }
+
+// a row's token: rows are below 2^28 and by_group is 2^32 / group rounded up, so that this divides by the group, 16 at most
+__device__ __forceinline__ int token_of(const BuildArgs &A, int row) { return A.group == 1 ? row : (int)__umulhi(row, A.by_group); }
+
+// Sums stop at 2^30: what goes beyond any limit does not come round to within it.
+__device__ __forceinline__ unsigned add(unsigned a, unsigned b) {
+    const unsigned c = a + b;
+    return c < 1u << 30 ? c : 1u << 30;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned shifted(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false); }
+// inclusive prefix sums over rows of 16 lanes, over the wave
+__device__ __forceinline__ unsigned row_sums(unsigned x) {
+    x = add(x, shifted<0x111, 0xf>(x));
+    x = add(x, shifted<0x112, 0xf>(x));
+    x = add(x, shifted<0x114, 0xf>(x));
+    return add(x, shifted<0x118, 0xf>(x));
+}
+__device__ __forceinline__ unsigned wave_sums(unsigned x) {
+    x = row_sums(x);
+    x = add(x, shifted<0x142, 0xa>(x));          // the last lane of rows 0 and 2 into rows 1 and 3
+    return add(x, shifted<0x143, 0xc>(x));       // ... of the lower half into the upper
+}
+__device__ __forceinline__ unsigned last_lane(unsigned x) { return (unsigned)__builtin_amdgcn_readlane((int)x, 63); }
+
+// Exclusive prefix sums over the workgroup of N numbers a thread, and their totals.  `lds`: WAVES * N, which nobody reads any more.
 template <int N>
-__device__ __forceinline__ void scan(int (&v)[N], int (&total)[N], int *lds) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int mine[N];
+__device__ __forceinline__ void scan(unsigned (&v)[N], unsigned (&total)[N], unsigned *lds) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    unsigned mine[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        int x = v[n];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d, 64);
-            x += lane >= d ? y : 0;
-        }
+        const unsigned x = wave_sums(v[n]);
         mine[n] = x - v[n];
         if (lane == 63) lds[wave * N + n] = x;
     }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        int before = 0, all = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const int x = lds[w * N + n];
-            before += w < wave ? x : 0;
-            all += x;
-        }
-        v[n] = before + mine[n];
-        total[n] = all;
+        const unsigned x = row_sums(lane < waves ? lds[lane * N + n] : 0);
+        const unsigned before = wave ? (unsigned)__builtin_amdgcn_readlane((int)x, wave - 1) : 0;
+        total[n] = (unsigned)__builtin_amdgcn_readlane((int)x, 15);
+        v[n] = add(before, mine[n]);
     }
-    __syncthreads();
 }
 
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
-    return x;
-}
-__device__ __forceinline__ int wave_max(int x) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_xor(x, d, 64);
-        x = y > x ? y : x;
-    }
-    return x;
-}
+// n / d rounded up, less one, of whole numbers in floats, `inverse` = 1 / d rounded to the nearest.  (n - 0.5) / d is 0.5 / d from a whole number at least, and the
+// result less than n / d * 2^-23 off: exact for n below 2^22, which is the blocks of the longest sequence.
+__device__ __forceinline__ float times_less_one(float n, float inverse) { return floorf(fmaf(n, inverse, -0.5f * inverse)); }
 
-// The first kernel.  PER requests, and as many pieces of 128 rows as are needed, in a thread, one after the other.
+// The first kernel.  PER requests a thread, one after the other.  Bound by how long one thing waits for another: loads, about six
+// sums over the workgroup, barriers, and the fetching of its own instructions, which is why little of it is unrolled or divides in 64 bits.
 template <int PER>
 __global__ void __launch_bounds__(THREADS) k_build_sums(BuildArgs A) {
-    __shared__ int lds[WAVES * 4];
-    __shared__ int few_total[PER * THREADS], many_total[SPD_BUILD_PIECES];
-    __shared__ unsigned short few_most[PER * THREADS];
+    __shared__ unsigned lds[3][WAVES * 8];
+    __shared__ int many_pos[PER * THREADS], many_rows[PER * THREADS], many_first[PER * THREADS];      // requests of many rows: position, rows, first piece
+    // Of the pieces of few rows, of many: blocks; the most items that each may be cut into, later those that it is, less one.  Whole numbers in floats, which
+    // divide faster.
+    __shared__ float2 few_pieces[PER * THREADS], many_pieces[SPD_BUILD_PIECES];
     __shared__ unsigned long long sums[2];                 // blocks of the pieces of few rows, of many
-    __shared__ int fits[4][WAVES];                         // does a chunk make few enough items?  few rows; many, for 2, 3 and 4 halves
-    __shared__ double us[3];
-    __shared__ int bucket[2][256], longest[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // few rows; many, for 2, 3 and 4 halves: the chunks that are tried, and does one make few enough items?
+    __shared__ int chunks[4][SPD_LONGER], fits[4][SPD_LONGER];
+    __shared__ int counts[3][3];                           // items, those that are parts, blocks of the longest, as many rows might be cut
+    __shared__ int bucket[256], longest;
+    __shared__ unsigned took;                              // pages, where there are not enough
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     spd_plan_header &H = *(spd_plan_header *)A.plan;
-    if (tid < 2) {
-        sums[tid] = 0;
-        longest[tid] = 1;
-    }
-    for (int i = tid; i < 512; i += THREADS) bucket[i >> 8][i & 255] = 0;
     const int free_now = A.n_free ? *A.n_free : 0, free0 = free_now < 0 ? 0 : free_now > A.n_pages ? A.n_pages : free_now;
-    int pos[PER], q[PER], rows[PER];
-    // rows
-    int v1[1] = {0}, t1[1];
+    int pos[PER], q[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int b = tid * PER + k;
         pos[k] = b < A.batch ? A.positions[b] : 0;
         q[k] = b < A.batch ? A.q_lens[b] : 0;
-        rows[k] = q[k] > 0 && q[k] <= A.q_len ? q[k] : 0;
     }
-    const int most_rows = A.tokens + 1;          // (where their sums stop, lest they overflow)
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        v1[0] += rows[k];
-        v1[0] = v1[0] < most_rows ? v1[0] : most_rows;
-    }
-    {
-        // as scan(), of sums that stop
-        int x = v1[0];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d, 64);
-            x += lane >= d ? y : 0;
-            x = x < most_rows ? x : most_rows;
-        }
-        const int up = __shfl_up(x, 1, 64);
-        if (lane == 63) lds[wave] = x;
-        __syncthreads();
-        int before = 0, all = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            if (w == wave) before = all;
-            all += lds[w];
-            all = all < most_rows ? all : most_rows;
-        }
-        before += lane ? up : 0;
-        v1[0] = before < most_rows ? before : most_rows;
-        t1[0] = all;
-        __syncthreads();
-    }
-    // pages that come back, pages that are needed
-    int tok0[PER], back[PER], need[PER];
-    bool fine[PER];
-    int v2[2] = {0, 0}, t2[2];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        tok0[k] = v1[0] < A.tokens ? v1[0] : A.tokens;
-        v1[0] += rows[k];
-        fine[k] = pos[k] >= 0 && q[k] >= SPD_STEP_RELEASE && q[k] <= A.q_len && pos[k] <= A.most_end - (q[k] > 0 ? q[k] : 0) && v1[0] <= A.tokens;
-        v1[0] = v1[0] < most_rows ? v1[0] : most_rows;
-        back[k] = need[k] = 0;
-        if (fine[k] && A.free_pages) {
-            const int held = ceil_div(pos[k], A.page_size);
-            if (q[k] > 0) need[k] = ceil_div(pos[k] + q[k], A.page_size) - held;
-            if (q[k] < 0) back[k] = held;
-        }
-        v2[0] += back[k];
-        v2[1] += need[k];
-    }
-    scan(v2, t2, lds);
-    const int top = t2[0] < A.n_pages - free0 ? free0 + t2[0] : A.n_pages;
-    // pieces
-    int back0[PER], need0[PER], few[PER], pieces[PER], writes[PER];
-    int v4[4] = {0, 0, 0, 0}, t4[4];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        back0[k] = v2[0];
-        need0[k] = v2[1];
-        v2[0] += back[k];
-        v2[1] += need[k];
-        few[k] = pieces[k] = writes[k] = 0;
-        const bool got = fine[k] && (need[k] == 0 || v2[1] <= top);
-        if (got && q[k] > 0) {
-            const int n = q[k] * A.group;
-            few[k] = n <= SPD_SMALL_ROWS;
-            pieces[k] = few[k] ? 0 : ceil_div(n, SPD_LARGE_ROWS);
-            writes[k] = (pos[k] + q[k] - 1) / 16 - pos[k] / 16 + 1;
-        }
-        if (!fine[k]) need[k] = SPD_STEP_LENGTHS;          // (from here on: why not)
-        else if (!got) need[k] = SPD_STEP_NO_PAGES;
-        v4[0] += few[k];
-        v4[1] += pieces[k];
-        v4[2] += writes[k];
-        v4[3] += got ? need[k] : 0;
-    }
-    scan(v4, t4, lds);
-    const int n_few = t4[0], n_many = t4[1];
-    const int sets = spd_sets(A.group);
-    int few0[PER], piece0[PER], write0[PER];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        few0[k] = v4[0];
-        piece0[k] = v4[1];
-        write0[k] = v4[2];
-        v4[0] += few[k];
-        v4[1] += pieces[k];
-        v4[2] += writes[k];
-        int total = 0;
-        if (few[k]) {
-            total = spd_piece_of(A.group, pos[k], 0, q[k] * A.group, A.window, A.sinks).total;
-            few_total[few0[k]] = total;
-            const int most = spd_most_small(total, sets);
-            few_most[few0[k]] = (unsigned short)(most < 65535 ? most : 65535);
-        }
-        if (n_few) {
-            total = wave_sum(total);                       // (at most 64 * 2^23)
-            if (lane == 0 && total) atomicAdd(&sums[0], (unsigned long long)total);
-        }
-        // a wave together for each of its requests of many rows
-        unsigned long long todo = __builtin_amdgcn_ballot_w64(pieces[k] > 0);
-        while (todo) {
-            const int from = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            const int p = __builtin_amdgcn_readlane(pos[k], from), n = __builtin_amdgcn_readlane(q[k], from) * A.group,
-                      at = __builtin_amdgcn_readlane(piece0[k], from);
-            unsigned long long all = 0;
-            for (int i = lane; i * SPD_LARGE_ROWS < n; i += 64) {
-                const int row0 = i * SPD_LARGE_ROWS, left = n - row0;
-                const int blocks = spd_piece_of(A.group, p, row0, left < SPD_LARGE_ROWS ? left : SPD_LARGE_ROWS, A.window, A.sinks).total;
-                many_total[at + i] = blocks;
-                all += blocks;
-            }
-            atomicAdd(&sums[1], all);
-        }
-    }
-    __syncthreads();
-    // The chunks: every wave tries the one that is `wave` times longer than the first
-    const bool cut_few = n_few && (int64_t)n_few * A.kv <= SPD_COUNTERS;
-    auto longer = [](int64_t chunk, int times, int unit) {
-        for (int i = 0; i < times; ++i) chunk = spd_next_chunk(chunk, unit);
-        return chunk;
-    };
-    const int64_t first_few = spd_first_chunk((int64_t)sums[0], A.kv, SPD_SMALL_TARGET, 2);
-    auto first_many = [&](int h) { return spd_first_chunk((int64_t)sums[1], A.kv, SPD_COMPUTE_UNITS * (h + 2) / 2, 4); };
-    // (chunks and pieces are less than 2^31 blocks, so that 32 bits divide: a chunk that is longer than any piece is as good as the longest of 2^30)
-    auto short_of = [](int64_t chunk) { return (int)(chunk < 1 << 30 ? chunk : 1 << 30); };
-    if (cut_few) {
-        const int chunk = short_of(longer(first_few, wave, 2));
-        int n = 0;
-        for (int i = lane; i < n_few; i += 64) {
-            const int parts = ceil_div(few_total[i], chunk), most = few_most[i];
-            n += parts < most ? parts : most;
-        }
-        n = wave_sum(n);
-        if (lane == 0) fits[0][wave] = (int64_t)n * A.kv <= SPD_SMALL_TARGET || n == n_few;
-    }
-    if (n_many) {
-#pragma unroll
-        for (int h = 0; h < 3; ++h) {
-            const int chunk = short_of(longer(first_many(h), wave, 4));
-            int n = 0;
-            for (int i = lane; i < n_many; i += 64) {
-                const int parts = ceil_div(many_total[i], chunk), most = spd_most_large(many_total[i]);
-                n += parts < most ? parts : most;
-            }
-            n = wave_sum(n);
-            if (lane == 0) fits[h + 1][wave] = (int64_t)n * A.kv <= SPD_COMPUTE_UNITS * (h + 2) / 2 || n == n_many;
-        }
-    }
-    __syncthreads();
-    auto chosen = [&](int which, int64_t first, int unit) {
-        int times = 0;
-        while (times < SPD_LONGER && !fits[which][times]) ++times;
-        return short_of(longer(first, times, unit));
-    };
-    static_assert(WAVES == SPD_LONGER, "a wave for each chunk that is tried");
-    const int few_chunk = cut_few ? chosen(0, first_few, 2) : 0;
-    auto parts_few = [&](int i) {
-        if (!few_chunk) return 1;
-        const int parts = ceil_div(few_total[i], few_chunk), most = few_most[i], units = ceil_div(few_total[i], 2);
-        const int n = parts < most ? parts : most;
-        return n < units ? n : units;
-    };
-    auto parts_many = [&](int i, int chunk) {
-        const int parts = ceil_div(many_total[i], chunk), most = spd_most_large(many_total[i]), units = ceil_div(many_total[i], 4);
-        const int n = parts < most ? parts : most;
-        return n < units ? n : units;
-    };
-    int many_chunk = 1 << 30;
-    if (n_many) {
-        if (wave < 3) {
-            const int chunk = chosen(wave + 1, first_many(wave), 4);
-            int n = 0, slots = 0, most = 0;
-            for (int i = lane; i < n_many; i += 64) {
-                const int parts = parts_many(i, chunk);
-                n += parts;
-                slots += parts > 1 ? parts : 0;
-                // the longest of a piece's items is its last, or (as the last may have less than four blocks in its last unit) the one before
-                for (int k = parts > 2 ? parts - 2 : 0; k < parts; ++k) {
-                    const int c = spd_item_count(many_total[i], 4, parts, k);
-                    most = c > most ? c : most;
-                }
-                if (parts > 2) {                           // an earlier one has all of the units that the last has where two or more have one more
-                    const int units = ceil_div(many_total[i], 4), c = units % parts >= 2 ? ceil_div(units, parts) * 4 : 0;
-                    most = c > most ? c : most;
-                }
-            }
-            n = wave_sum(n);
-            slots = wave_sum(slots);
-            most = wave_max(most);
-            if (lane == 0) us[wave] = spd_estimate_large(most, n, slots, A.kv);
-        }
-        __syncthreads();
-        int h = 0;
-        if (us[1] < us[0]) h = 1;
-        if (us[2] < us[h]) h = 2;
-        many_chunk = chosen(h + 1, first_many(h), 4);
-    }
-    // Items: those of a piece one after the other, the pieces with the longest items first, by 256 lengths
-    int parts[PER], v3[3] = {0, 0, 0}, t3[3];
-    int longest_few = 0;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        parts[k] = few[k] ? parts_few(few0[k]) : 0;
-        v3[0] += parts[k];
-        v3[1] += parts[k] > 1 ? parts[k] : 0;
-        v3[2] += parts[k] > 1;
-        const int c = few[k] ? ceil_div(few_total[few0[k]], parts[k]) : 0;
-        longest_few = c > longest_few ? c : longest_few;
-    }
-    scan(v3, t3, lds);
-    const int n_small = t3[0];
-    const int per = ceil_div(n_many, THREADS);             // pieces a thread
-    int m3[3] = {0, 0, 0}, tm[3] = {0, 0, 0};
-    int longest_many = 0;
-    if (n_many) {
-        for (int k = 0; k < per; ++k) {
-            const int i = tid * per + k;
-            if (i >= n_many) break;
-            const int n = parts_many(i, many_chunk), c = ceil_div(many_total[i], n);
-            m3[0] += n;
-            m3[1] += n > 1 ? n : 0;
-            m3[2] += n > 1;
-            longest_many = c > longest_many ? c : longest_many;
-        }
-        scan(m3, tm, lds);
-    }
-    longest_few = wave_max(longest_few);
-    longest_many = wave_max(longest_many);
-    if (lane == 0) {
-        atomicMax(&longest[0], longest_few);
-        atomicMax(&longest[1], longest_many);
-    }
-    __syncthreads();
-    auto bucket_of = [&](int which, int total, int n) { return 255 - (int)((int64_t)ceil_div(total, n) * 255 / longest[which]); };
+    if (tid < 2) sums[tid] = took = 0;
+    if (tid < 9) counts[tid / 3][tid % 3] = 0;
+    if (tid < 64) fits[tid / SPD_LONGER][tid % SPD_LONGER] = 0;
+    bool fine[PER], got[PER];                              // its lengths are within the limits; there are pages for it
 #pragma unroll
     for (int k = 0; k < PER; ++k)
-        if (few[k]) atomicAdd(&bucket[0][bucket_of(0, few_total[few0[k]], parts[k])], parts[k]);
-    for (int k = 0; k < per; ++k) {
-        const int i = tid * per + k;
-        if (i >= n_many) break;
-        const int n = parts_many(i, many_chunk);
-        atomicAdd(&bucket[1][bucket_of(1, many_total[i], n)], n);
+        fine[k] = got[k] = pos[k] >= 0 && q[k] >= SPD_STEP_RELEASE && q[k] <= A.q_len && pos[k] <= A.most_end - (q[k] > 0 ? q[k] : 0);
+    auto rows_of = [&](int k) { return q[k] > 0 && q[k] <= A.q_len ? q[k] : 0; };
+    auto held_of = [&](int k) { return (pos[k] + A.page_size - 1) >> A.page_shift; };
+    auto back_of = [&](int k) { return A.free_pages && fine[k] && q[k] < 0 ? held_of(k) : 0; };
+    auto need_of = [&](int k) { return A.free_pages && fine[k] && q[k] > 0 ? ((pos[k] + q[k] + A.page_size - 1) >> A.page_shift) - held_of(k) : 0; };
+    auto few_of = [&](int k) { return got[k] && q[k] > 0 && q[k] * A.group <= SPD_SMALL_ROWS; };
+    auto pieces_of = [&](int k) { return got[k] && q[k] > 0 && q[k] * A.group > SPD_SMALL_ROWS ? (q[k] * A.group + SPD_LARGE_ROWS - 1) / SPD_LARGE_ROWS : 0; };
+    auto writes_of = [&](int k) { return got[k] && q[k] > 0 ? (pos[k] + q[k] - 1) / 16 - pos[k] / 16 + 1 : 0; };
+    // Rows, pages that come back, those of whom; pages needed; pieces of few rows, of many, blocks written; requests of many rows.  Who has no rows or no pages left is found by
+    // sums of those before it, after which there are new ones to be taken: in most steps nobody is.
+    unsigned v[8], t[8];
+    int top;
+    bool short_of_rows = false, short_of_pages = false;
+    for (int turn = 0;; ++turn) {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) v[n] = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            v[0] += rows_of(k);
+            v[1] += back_of(k);
+            v[2] += back_of(k) > 0;
+            v[3] += need_of(k);
+            v[4] += few_of(k);
+            v[5] += pieces_of(k);
+            v[6] += writes_of(k);
+            v[7] += pieces_of(k) > 0;
+        }
+        scan(v, t, lds[turn]);
+        top = (int)t[1] < A.n_pages - free0 ? free0 + (int)t[1] : A.n_pages;
+        if (!short_of_rows && (int)t[0] > A.tokens) {
+            short_of_rows = true;
+            unsigned r = v[0];
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                r = add(r, rows_of(k));
+                if ((int)r > A.tokens) fine[k] = got[k] = false;
+            }
+        } else if (!short_of_pages && (int)t[3] > top) {
+            short_of_pages = short_of_rows = true;
+            unsigned n = v[3];
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                n = add(n, need_of(k));
+                if (need_of(k) && (int)n > top) got[k] = false;
+            }
+        } else break;
     }
-    __syncthreads();
-    if (wave < 2) {
-        int x[4], all = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = bucket[wave][lane * 4 + i];
-            all += x[i];
-        }
-        int sum = all;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(sum, d, 64);
-            sum += lane >= d ? y : 0;
-        }
-        sum -= all;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bucket[wave][lane * 4 + i] = sum;
-            sum += x[i];
-        }
-    }
-    __syncthreads();
-    // (which of the pieces of one length comes first is left to chance: it is the order they are started in, and nothing else)
+    const int n_few = t[4], n_many = t[5], n_long = t[7];
     spd_plan_req *reqs = (spd_plan_req *)(A.plan + A.reqs);
+    // what is known of each so far is put away, and the pieces are measured
+    int few0 = v[4];
+    unsigned taken = 0;
+    {
+        unsigned row = v[0], back = v[1], backs = v[2], need = v[3];
+        int few = few0, piece = v[5], write = v[6], many = v[7];
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int b = tid * PER + k;
-        if (b >= A.batch) break;
-        spd_plan_req r;
-        r.pos = pos[k];
-        r.q_len = rows[k];
-        r.tok0 = tok0[k];
-        r.state = need[k] < 0 ? need[k] : q[k] < 0 ? 1 : 0;
-        r.need0 = need0[k];
-        r.back0 = back0[k];
-        r.back = back[k];
-        r.item0 = few[k] ? atomicAdd(&bucket[0][bucket_of(0, few_total[few0[k]], parts[k])], parts[k]) : 0;
-        r.parts = parts[k];
-        r.slot0 = v3[1];
-        r.group = v3[2];
-        v3[1] += parts[k] > 1 ? parts[k] : 0;
-        v3[2] += parts[k] > 1;
-        r.piece0 = piece0[k];
-        r.pieces = pieces[k];
-        r.write0 = write0[k];
-        r.writes = writes[k];
-        r.pad = 0;
-        reqs[b] = r;
-        if (A.first_row) {
-            A.first_row[b] = tok0[k];
-            if (b == A.batch - 1) A.first_row[A.batch] = t1[0] < A.tokens ? t1[0] : A.tokens;
+        for (int k = 0; k < PER; ++k) {
+            const int b = tid * PER + k, tok0 = (int)row < A.tokens ? (int)row : A.tokens;
+            if (b < A.batch) {
+                spd_plan_req &r = reqs[b];
+                *(i32x4 *)&r.pos = (i32x4){pos[k], rows_of(k), tok0, !fine[k] ? SPD_STEP_LENGTHS : !got[k] ? SPD_STEP_NO_PAGES : q[k] < 0 ? 1 : 0};
+                *(i32x4 *)&r.need0 = (i32x4){(int)need, (int)back, back_of(k), few};
+                *(i32x4 *)&r.piece0 = (i32x4){piece, pieces_of(k), write, writes_of(k)};
+                if (back_of(k)) ((spd_plan_back *)(A.plan + A.backs))[backs] = spd_plan_back{(int)back, b};
+                if (A.first_row) A.first_row[b] = tok0;
+            }
+            if (few_of(k)) few_pieces[few].x = (float)spd_piece_between(pos[k], pos[k] + q[k] - 1, A.window, A.sinks).total;
+            if (pieces_of(k)) {
+                many_pos[many] = pos[k];
+                many_rows[many] = q[k] * A.group;
+                many_first[many++] = piece;
+            }
+            row = add(row, rows_of(k));
+            back += back_of(k);
+            backs += back_of(k) > 0;
+            need = add(need, need_of(k));
+            taken += got[k] ? need_of(k) : 0;
+            few += few_of(k);
+            piece += pieces_of(k);
+            write += writes_of(k);
         }
     }
-    spd_plan_cut *cuts = (spd_plan_cut *)(A.plan + A.cuts);
-    for (int k = 0; k < per; ++k) {
-        const int i = tid * per + k;
-        if (i >= n_many) break;
-        spd_plan_cut c;
-        c.parts = parts_many(i, many_chunk);
-        c.item0 = atomicAdd(&bucket[1][bucket_of(1, many_total[i], c.parts)], c.parts);
-        c.slot0 = m3[1];
-        c.merge = m3[2];
-        m3[1] += c.parts > 1 ? c.parts : 0;
-        m3[2] += c.parts > 1;
-        cuts[i] = c;
+    __syncthreads();
+    const int sets = spd_sets(A.group);
+#pragma unroll 1
+    for (int i = tid; i - lane < n_few; i += blockDim.x) {
+        const int total = i < n_few ? (int)few_pieces[i].x : 0;
+        const unsigned all = last_lane(wave_sums(total));  // (64 * 2^22 at most)
+        if (lane == 0) atomicAdd(&sums[0], (unsigned long long)all);
+        if (i < n_few) few_pieces[i].y = (float)(spd_most_small(total, sets) - 1);
+    }
+#pragma unroll 1
+    for (int i = tid; i - lane < n_many; i += blockDim.x) {
+        int total = 0;
+        if (i < n_many) {
+            int lo = 0, hi = n_long;                       // its request: the last that begins no later
+#pragma unroll 1
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2, first = many_first[mid];
+                lo = first <= i ? mid : lo;
+                hi = first <= i ? hi : mid;
+            }
+            const int row0 = (i - many_first[lo]) * SPD_LARGE_ROWS, left = many_rows[lo] - row0, row1 = row0 + (left < SPD_LARGE_ROWS ? left : SPD_LARGE_ROWS) - 1;
+            auto token = [&](int row) { return token_of(A, row); };
+            total = spd_piece_between(many_pos[lo] + token(row0), many_pos[lo] + token(row1), A.window, A.sinks).total;
+            many_pieces[i] = make_float2((float)total, (float)(spd_most_large(total) - 1));
+        }
+        const unsigned all = last_lane(wave_sums(total));
+        if (lane == 0) atomicAdd(&sums[1], (unsigned long long)all);
+    }
+    __syncthreads();
+    // The chunks: of those tried the first that makes few enough items.  Each wave tries one, of few rows or of many for one of three numbers of workgroups, and
+    // others after it if that is too short.
+    const bool cut_few = n_few && (int64_t)n_few * A.kv <= SPD_COUNTERS;
+    {
+        const int which = n_many ? wave & 3 : 0, c0 = n_many ? wave >> 2 : wave, step = n_many ? WAVES / 4 : waves;
+        const int n = which ? n_many : n_few, unit = which ? 4 : 2;
+        const int target = which == 0 ? SPD_SMALL_TARGET : SPD_COMPUTE_UNITS / 2 * (which + 1);
+        const float2 *pieces = which ? many_pieces : few_pieces;
+        if (which || cut_few) {
+            // spd_first_chunk(), in 32 bits: no piece has more than 2^22 blocks, and 2^29 does for all that is more
+            static_assert(SPD_SMALL_TARGET == 256 && SPD_COMPUTE_UNITS == 256, "targets are 128 times 2, 3 or 4");
+            const unsigned long long share = (sums[which ? 1 : 0] * A.kv + 127) >> 7;
+            const unsigned y = share < 1u << 31 ? (unsigned)share : 1u << 31;
+            const unsigned first = ((which == 2 ? (y + 2) / 3 : which == 3 ? (y + 3) / 4 : (y + 1) / 2) + unit - 1) & -unit;
+            int chunk = first < (unsigned)unit ? unit : first < 1u << 29 ? (int)first : 1 << 29;
+            auto next = [&]() {                            // spd_next_chunk(): units are powers of two
+                chunk = (chunk + chunk / 16 + unit) & -unit;
+                chunk = chunk < 1 << 29 ? chunk : 1 << 29;
+            };
+            auto skip = [&](int times) {
+#pragma unroll 1
+                for (int i = 0; i < times; ++i) next();
+            };
+            skip(c0);
+#pragma unroll 1
+            for (int c = c0; c < SPD_LONGER; c += step, skip(step)) {
+                const float inverse = 1.f / (float)chunk;
+                float more = 0.f;                          // items beyond one for each piece
+#pragma unroll 4
+                for (int i = lane; i < n; i += 64) more += fminf(times_less_one(pieces[i].x, inverse), pieces[i].y);
+                const unsigned items = n + last_lane(wave_sums((unsigned)more));
+                const bool fit = (int64_t)items * A.kv <= target || (int)items == n;
+                if (lane == 0) {
+                    fits[which][c] = fit;
+                    chunks[which][c] = chunk;
+                }
+                if (fit) break;                            // (a wave's later ones are not asked for)
+            }
+        }
+    }
+    __syncthreads();
+    auto chosen = [&](int which) {                         // 1 / the chunk
+        const unsigned long long fit = __builtin_amdgcn_ballot_w64(lane < SPD_LONGER && fits[which][lane < SPD_LONGER ? lane : 0]);
+        int chunk = chunks[which][fit ? __builtin_ctzll(fit) : SPD_LONGER - 1];
+        const int unit = which ? 4 : 2;
+        if (!fit) chunk = (chunk + chunk / 16 + unit) & -unit;
+        return 1.f / (float)chunk;
+    };
+    int halves = 0;
+    // items of a piece, less one: no more than whole units
+    auto parts_less_one = [&](float2 p, float inverse, float by_unit) { return fminf(fminf(times_less_one(p.x, inverse), p.y), times_less_one(p.x, by_unit)); };
+    if (n_many) {
+        // (where there are many rows there are sixteen waves: five for each number of halves)
+        if (wave < 15) {
+            const int h = wave % 3;
+            const float inverse = chosen(h + 1);
+            unsigned items = 0, slots = 0;
+            int most = 0;
+#pragma unroll 1
+            for (int i = wave / 3 * 64 + lane; i < n_many; i += 5 * 64) {
+                const float2 p = many_pieces[i];
+                const int total = (int)p.x, parts = (int)parts_less_one(p, inverse, 0.25f) + 1, units = (total + 3) / 4;
+                items += parts;
+                slots += parts > 1 ? parts : 0;
+                // The longest of its items has units / parts of them, rounded up: the last, which the last unit may leave shorter, and an earlier one if
+                // as many as two have one more than the others (or none has)
+                const int each = (int)times_less_one((float)units, 1.f / (float)parts) + 1, c = each * 4, more = units - (each - 1) * parts;
+                const int last = total - (units - each) * 4;
+                const int longest_here = (more == 1 || parts == 1) ? (last > c - 4 ? last : c - 4) : c;
+                most = longest_here > most ? longest_here : most;
+            }
+            items = last_lane(wave_sums(items));
+            slots = last_lane(wave_sums(slots));
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int y = __shfl_xor(most, d, 64);
+                most = y > most ? y : most;
+            }
+            if (lane == 0) {
+                atomicAdd(&counts[h][0], (int)items);
+                atomicAdd(&counts[h][1], (int)slots);
+                atomicMax(&counts[h][2], most);
+            }
+        }
+        __syncthreads();
+        const int h = lane < 3 ? lane : 0;
+        const double us = spd_estimate_large(counts[h][2], counts[h][0], counts[h][1], A.kv), us0 = __shfl(us, 0), us1 = __shfl(us, 1), us2 = __shfl(us, 2);
+        halves = us1 < us0 ? us2 < us1 ? 2 : 1 : us2 < us0 ? 2 : 0;
+    }
+    {
+        const float few_inverse = cut_few ? chosen(0) : 0.f, many_inverse = n_many ? chosen(halves + 1) : 0.f;      // (few rows: uncut where there are not enough counters)
+#pragma unroll 1
+        for (int i = tid; i < n_few; i += blockDim.x) few_pieces[i].y = cut_few ? parts_less_one(few_pieces[i], few_inverse, 0.5f) : 0.f;
+#pragma unroll 1
+        for (int i = tid; i < n_many; i += blockDim.x) many_pieces[i].y = parts_less_one(many_pieces[i], many_inverse, 0.25f);
+        __syncthreads();
+    }
+    // Items, those of a piece one after the other.  Where the chip does not hold them all at once, the pieces with the longest items come first, by 256 lengths;
+    // which of one length is first is left to chance: it is the order they are started in, and nothing else.
+    auto place = [&](int n_pieces, const float2 *pieces, int *to, int step) {
+        auto blocks = [&](int i) { return pieces[i].x * __builtin_amdgcn_rcpf(pieces[i].y + 1.f); };      // of its items, about
+        if (tid == 0) longest = 0;
+        for (int i = tid; i < 256; i += blockDim.x) bucket[i] = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int i = tid; i - lane < n_pieces; i += blockDim.x) {
+            int most = i < n_pieces ? __float_as_int(blocks(i)) : 0;      // (as whole numbers floats of one sign stay in order)
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int y = __shfl_xor(most, d, 64);
+                most = y > most ? y : most;
+            }
+            if (lane == 0) atomicMax(&longest, most);
+        }
+        __syncthreads();
+        const float by = 255.f / __int_as_float(longest);
+        auto bucket_of = [&](int i) {
+            const int n = (int)(blocks(i) * by);
+            return n < 255 ? 255 - n : 0;
+        };
+#pragma unroll 1
+        for (int i = tid; i < n_pieces; i += blockDim.x) atomicAdd(&bucket[bucket_of(i)], (int)pieces[i].y + 1);
+        __syncthreads();
+        if (wave == 0) {
+            unsigned x[4], all = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) all += x[i] = bucket[lane * 4 + i];
+            unsigned sum = wave_sums(all) - all;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                bucket[lane * 4 + i] = sum;
+                sum += x[i];
+            }
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int i = tid; i < n_pieces; i += blockDim.x) to[i * step] = atomicAdd(&bucket[bucket_of(i)], (int)pieces[i].y + 1);
+        __syncthreads();
+    };
+    int n_small, n_large = 0, n_merge = 0;
+    {
+        unsigned s[3] = {0, 0, 0}, all[3];
+        int few = few0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int parts = few_of(k) ? (int)few_pieces[few].y + 1 : 0;
+            few += few_of(k);
+            s[0] += parts;
+            s[1] += parts > 1 ? parts : 0;
+            s[2] += parts > 1;
+        }
+        scan(s, all, lds[1]);
+        n_small = all[0];
+        few = few0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int b = tid * PER + k, parts = few_of(k) ? (int)few_pieces[few].y + 1 : 0;
+            if (b < A.batch) *(i32x4 *)&reqs[b].item0 = (i32x4){(int)s[0], parts, (int)s[1], (int)s[2]};
+            few += few_of(k);
+            s[0] += parts;
+            s[1] += parts > 1 ? parts : 0;
+            s[2] += parts > 1;
+        }
+    }
+    const bool sorted = n_small * A.kv > 2 * SPD_COMPUTE_UNITS;      // (few rows: the first items are then those in `order`)
+    if (sorted) place(n_few, few_pieces, (int *)(A.plan + A.order), 1);
+    if (n_many) {
+        spd_plan_cut *cuts = (spd_plan_cut *)(A.plan + A.cuts);
+        const int per = ceil_div(n_many, blockDim.x);
+        unsigned s[3] = {0, 0, 0}, all[3];
+#pragma unroll 1
+        for (int i = tid * per; i < n_many && i < (tid + 1) * per; ++i) {
+            const int n = (int)many_pieces[i].y + 1;
+            s[0] += n;
+            s[1] += n > 1 ? n : 0;
+            s[2] += n > 1;
+        }
+        scan(s, all, lds[2]);
+#pragma unroll 1
+        for (int i = tid * per; i < n_many && i < (tid + 1) * per; ++i) {
+            const int n = (int)many_pieces[i].y + 1;
+            *(i32x4 *)&cuts[i] = (i32x4){(int)s[0], n, (int)s[1], (int)s[2]};
+            s[0] += n;
+            s[1] += n > 1 ? n : 0;
+            s[2] += n > 1;
+        }
+        n_large = all[0];
+        n_merge = all[2];
+        __syncthreads();
+        if (n_large * A.kv > 2 * SPD_COMPUTE_UNITS) place(n_many, many_pieces, &cuts[0].item0, sizeof(spd_plan_cut) / 4);
+    }
+    if (short_of_pages) {
+        __syncthreads();
+        taken = last_lane(wave_sums(taken));
+        if (lane == 0) atomicAdd(&took, taken);
+        __syncthreads();
     }
     if (tid == 0) {
         H.n_small = n_small;
-        H.n_large = tm[0];
-        H.n_merge = tm[2];
-        H.n_write = t4[2];
-        H.rows = t1[0] < A.tokens ? t1[0] : A.tokens;
+        H.n_large = n_large;
+        H.n_merge = n_merge;
+        H.n_write = t[6];
+        H.rows = (int)t[0] < A.tokens ? (int)t[0] : A.tokens;
         H.free0 = free0;
         H.top = top;
-        if (A.n_free_out) *A.n_free_out = top - t4[3];
+        H.n_backs = t[2];
+        H.sorted = sorted;
+        if (A.n_free_out) *A.n_free_out = top - (int)(short_of_pages ? took : t[3]);
+        if (A.first_row) A.first_row[A.batch] = (int)t[0] < A.tokens ? (int)t[0] : A.tokens;
     }
-}
-
-// The k-th of the pages that are handed out: from the top of the free ones, where those that came back lie.
-__device__ __forceinline__ int new_page(const BuildArgs &A, const spd_plan_req *reqs, int free0, int top, int k) {
-    const int at = top - 1 - k;
-    if (at < free0) return A.free_pages[at];
-    // (it is being put there by another workgroup: the last request with no more than so many before it has it)
-    const int j = at - free0;
-    int lo = 0, hi = A.batch;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (reqs[mid].back0 <= j) lo = mid;
-        else hi = mid;
-    }
-    return A.page_table[lo * A.ld_table + (j - reqs[lo].back0)];
 }
 
 constexpr int CHUNK_ROWS = 2048, CHUNK_PAGES = CHUNK_ROWS / 16 + 1;
@@ -458,8 +453,15 @@ __global__ void __launch_bounds__(256) k_build_requests(BuildArgs A) {
     }
     const int b = blockIdx.x, free0 = H.free0, top = H.top;
     const spd_plan_req *reqs = (const spd_plan_req *)(A.plan + A.reqs);
-    const spd_plan_req r = reqs[b];
+    const spd_plan_back *backs = (const spd_plan_back *)(A.plan + A.backs);
     int32_t *row = A.page_table + b * A.ld_table;
+    // (what a thread will most likely want is asked for before it is known that it does: one wait for memory instead of three)
+    constexpr int EARLY = 4;
+    int early[EARLY];
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k) early[k] = tid + 256 * k < A.entries ? row[tid + 256 * k] : 0;
+    const int early_back = tid < A.batch ? backs[tid].back0 : 0;
+    const spd_plan_req r = reqs[b];
     const bool first = chunk == 0;
     if (r.state == 1) {                          // its pages come back
         if (!first) return;
@@ -481,8 +483,22 @@ __global__ void __launch_bounds__(256) k_build_requests(BuildArgs A) {
     if (r.state == 0 && r.q_len > 0) {
         const int n = ceil_div(end, A.page_size), held = A.free_pages ? ceil_div(r.pos, A.page_size) : n, from = (r.pos + row0) / A.page_size;
         int32_t *table = (int32_t *)(A.plan + A.table) + (size_t)b * A.entries;
-        for (int i = tid; i < n; i += 256) {
-            const int page = i < held ? row[i] : new_page(A, reqs, free0, top, r.need0 + i - held);
+        // New pages come from the top of the free ones, where those that came back lie (put there by other workgroups, at this moment: they are taken
+        // from their requests' rows of the table).  `giver`: the last of these that has the first of them, the next are its or the ones' before it.
+        const int top_new = top - 1 - r.need0;
+        int giver = 0;
+        if (n > held && top_new >= free0) {
+            giver = __syncthreads_count(tid < H.n_backs && early_back <= top_new - free0) - 1;
+            for (int i = tid + 256; i - tid < H.n_backs; i += 256) giver += __syncthreads_count(i < H.n_backs && backs[i].back0 <= top_new - free0);
+        }
+        auto new_page = [&](int k) {
+            const int j = top_new - k - free0;
+            if (j < 0) return A.free_pages[top_new - k];
+            int g = giver;
+            while (backs[g].back0 > j) --g;
+            return A.page_table[backs[g].req * A.ld_table + (j - backs[g].back0)];
+        };
+        auto enter = [&](int i, int page) {
             const bool none = (unsigned)page >= (unsigned)A.n_pages;
             bad |= none;
             if (first) {
@@ -490,7 +506,11 @@ __global__ void __launch_bounds__(256) k_build_requests(BuildArgs A) {
                 table[i] = none ? 0 : page;
             }
             if (i >= from && i - from < CHUNK_PAGES) pages[i - from] = page;
-        }
+        };
+#pragma unroll
+        for (int k = 0; k < EARLY; ++k)
+            if (tid + 256 * k < n) enter(tid + 256 * k, tid + 256 * k < held ? early[k] : new_page(tid + 256 * k - held));
+        for (int i = tid + 256 * EARLY; i < n; i += 256) enter(i, i < held ? row[i] : new_page(i - held));
     }
     bad = __syncthreads_or(bad);
     const bool served = r.state == 0 && !bad;
@@ -532,15 +552,16 @@ __global__ void __launch_bounds__(256) k_build_requests(BuildArgs A) {
     };
     const int n = r.q_len * A.group;
     if (r.parts) {
-        const spd_piece w = spd_piece_of(A.group, r.pos, 0, n, A.window, A.sinks);
-        for (int i = tid; i < r.parts; i += 256) item((spd_plan_item *)(A.plan + A.small) + r.item0 + i, w, 0, 2, r.parts, i, r.slot0, r.group);
+        const spd_piece w = spd_piece_between(r.pos, end - 1, A.window, A.sinks);
+        const int item0 = H.sorted ? ((const int *)(A.plan + A.order))[r.few] : r.item0;
+        for (int i = tid; i < r.parts; i += 256) item((spd_plan_item *)(A.plan + A.small) + item0 + i, w, 0, 2, r.parts, i, r.slot0, r.group);
     }
-    for (int k = tid; k < r.pieces; k += 256) {
+    for (int k = tid >> 3; k < r.pieces; k += 32) {        // eight threads a piece
         const spd_plan_cut c = ((const spd_plan_cut *)(A.plan + A.cuts))[r.piece0 + k];
         const int first_row = k * SPD_LARGE_ROWS, left = n - first_row, mine = left < SPD_LARGE_ROWS ? left : SPD_LARGE_ROWS;
-        const spd_piece w = spd_piece_of(A.group, r.pos, first_row, mine, A.window, A.sinks);
-        for (int i = 0; i < c.parts; ++i) item((spd_plan_item *)(A.plan + A.large) + c.item0 + i, w, first_row, 4, c.parts, i, c.slot0, c.merge);
-        if (c.parts > 1) ((spd_plan_merge *)(A.plan + A.merge))[c.merge] = spd_plan_merge{s, first_row, served ? mine : 0, c.slot0, c.parts};
+        const spd_piece w = spd_piece_between(r.pos + token_of(A, first_row), r.pos + token_of(A, first_row + mine - 1), A.window, A.sinks);
+        for (int i = tid & 7; i < c.parts; i += 8) item((spd_plan_item *)(A.plan + A.large) + c.item0 + i, w, first_row, 4, c.parts, i, c.slot0, c.merge);
+        if (c.parts > 1 && (tid & 7) == 0) ((spd_plan_merge *)(A.plan + A.merge))[c.merge] = spd_plan_merge{s, first_row, served ? mine : 0, c.slot0, c.parts};
     }
 }
 
@@ -599,13 +620,17 @@ extern "C" int spd_pages_build(const spd_pages *pages, const void *plan_host, vo
     A.window = h.window;
     A.sinks = h.sinks;
     A.page_size = c.page_size;
+    A.page_shift = pages->shift + 4;
     A.n_pages = c.n_pages;
     A.kv = c.n_kv_heads;
     A.group = pages->group;
+    A.by_group = (unsigned)(((1ull << 32) + pages->group - 1) / pages->group);
     A.most_end = (int)std::min<int64_t>(c.max_ctx, (int64_t)h.entries * c.page_size);
     A.seqs = h.seqs;
     A.reqs = h.reqs;
     A.cuts = h.cuts;
+    A.backs = h.backs;
+    A.order = h.order;
     A.small = h.small;
     A.large = h.large;
     A.merge = h.merge;
@@ -614,9 +639,9 @@ extern "C" int spd_pages_build(const spd_pages *pages, const void *plan_host, vo
     const bool by_row = t.row_seq || t.row_pos || t.row_slot;
     A.tails = by_row ? std::min(64, (h.tokens + 255) / 256) : 0;
     hipStream_t s = (hipStream_t)stream;
-    if (h.batch <= THREADS) hipLaunchKernelGGL((k_build_sums<1>), dim3(1), dim3(THREADS), 0, s, A);
-    else if (h.batch <= 2 * THREADS) hipLaunchKernelGGL((k_build_sums<2>), dim3(1), dim3(THREADS), 0, s, A);
-    else hipLaunchKernelGGL((k_build_sums<4>), dim3(1), dim3(THREADS), 0, s, A);
+    const int threads = h.n_large ? THREADS : std::min(THREADS, (h.batch + 63) / 64 * 64);
+    if (h.batch <= THREADS) hipLaunchKernelGGL((k_build_sums<1>), dim3(1), dim3(threads), 0, s, A);
+    else hipLaunchKernelGGL((k_build_sums<SPD_BUILD_BATCH / THREADS>), dim3(1), dim3(THREADS), 0, s, A);
     SPD_HIP(hipGetLastError());
     hipLaunchKernelGGL(k_build_requests, dim3(h.batch + A.tails, by_row ? (h.q_len + CHUNK_ROWS - 1) / CHUNK_ROWS : 1), dim3(256), 0, s, A);
     SPD_HIP(hipGetLastError());

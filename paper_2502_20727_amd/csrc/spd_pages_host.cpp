@@ -329,6 +329,8 @@ int spd_pages_reserve(const spd_pages *pages, const spd_pages_limits *limits, vo
     h.seqs = room(l.batch, sizeof(spd_plan_seq));
     h.reqs = room(l.batch, sizeof(spd_plan_req));
     h.cuts = room(pieces, sizeof(spd_plan_cut));
+    h.backs = room(l.batch, sizeof(spd_plan_back));
+    h.order = room(most_few, 4);
     h.small = room(h.n_small, sizeof(spd_plan_item));
     h.large = room(h.n_large, sizeof(spd_plan_item));
     h.merge = room(h.n_merge, sizeof(spd_plan_merge));
