@@ -97,19 +97,22 @@ struct Half {
     }
 };
 
-__device__ __forceinline__ float quad_sum(float x) {      // over lanes l, l^16, l^32, l^48
-    x += __shfl_xor(x, 16, 64);
-    return x + __shfl_xor(x, 32, 64);
-}
-__device__ __forceinline__ float quad_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16, 64));
-    return fmaxf(x, __shfl_xor(x, 32, 64));
-}
-
-// over lanes l, l^32
+// over lanes l, l^32 and l, l^16 (exchanged between registers: through the LDS a wave waits for it twice a pair of blocks)
 __device__ __forceinline__ float half_max(float x) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ __forceinline__ float quad_max(float x) {      // over lanes l, l^16, l^32, l^48
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return half_max(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return half_sum(__uint_as_float(a[0]) + __uint_as_float(a[1]));
 }
 
 // What the pages hold: SPD_E4M3, SPD_E2M1, or HALVES, values of the 16-bit type.
@@ -648,14 +651,29 @@ struct BlockLoad<D, SPD_E2M1> {
     Codes4<D> k, v;
     Scales4<D> ve;                                          // of values 4 g .. 4 g + 3
     unsigned char ke;                                       // of the lane's features of its key
-    __device__ __forceinline__ void load(const Pages &P, const Block &B, int lane) {
-        const char *codes = B.head + B.in_page * (8 * D), *exps = B.head + (size_t)P.page_size * D + B.in_page * (16 * N);
+    __device__ __forceinline__ void load_keys(const Pages &P, const Block &B, int lane) {
         const int r = lane & 15, g = lane >> 4;
-        k.stream(codes + lane * (4 * N));
-        ke = exps[r * N + g * N / 4];
-        v.stream(codes + (size_t)P.page_size * (D / 2) + lane * (4 * N));
-        ve.load(exps + (size_t)P.page_size * N + 4 * N * g);
+        k.stream(B.head + B.in_page * (8 * D) + lane * (4 * N));
+        ke = B.head[(size_t)P.page_size * D + B.in_page * (16 * N) + r * N + g * N / 4];
     }
+    __device__ __forceinline__ void load_values(const Pages &P, const Block &B, int lane) {
+        v.stream(B.head + (size_t)P.page_size * (D / 2) + B.in_page * (8 * D) + lane * (4 * N));
+        ve.load(B.head + (size_t)P.page_size * (D + N) + B.in_page * (16 * N) + 4 * N * (lane >> 4));
+    }
+};
+
+// what of a block is asked for
+struct Both {
+    template <class L>
+    __device__ __forceinline__ void operator()(L &x, const Pages &P, const Block &B, int lane) const { x.load(P, B, lane); }
+};
+struct Keys {
+    template <class L>
+    __device__ __forceinline__ void operator()(L &x, const Pages &P, const Block &B, int lane) const { x.load_keys(P, B, lane); }
+};
+struct Values {
+    template <class L>
+    __device__ __forceinline__ void operator()(L &x, const Pages &P, const Block &B, int lane) const { x.load_values(P, B, lane); }
 };
 
 // A partial result is written by one workgroup and read by another, perhaps on another die with an L2 of its own: both go past that
@@ -673,7 +691,7 @@ __device__ __forceinline__ float2 part_get(const float *p) {
 // their states in the LDS.  Rows cut into several items are joined, in the items' order, by the workgroup that ends last.
 // Lane = 16 g + row.
 template <int D, int C, bool F16>
-__global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
+__global__ void __launch_bounds__(512, C == SPD_E2M1 ? 4 : 1) k_attend_small(AttendArgs A) {
     constexpr bool E4M3 = C == SPD_E4M3, E2M1 = C == SPD_E2M1;
     constexpr int DT = D / 16, NF = D / 32, NW = SPD_SMALL_WAVES;
     typedef Half<F16> H;
@@ -712,15 +730,19 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
     struct Pair {
         BlockLoad<D, C> x[2];
     };
-    auto load = [&](Pair &f, int j) __attribute__((always_inline)) {      // pair j of the wave
-        if (j > 0 && (j & 31) == 0) pages = page_of(P, s, my_block(2 * j + lane < 2 * mine ? 2 * j + lane : 2 * j));
+    auto load = [&](Pair &f, int j, auto ask) __attribute__((always_inline)) {      // pair j of the wave, or its keys or values (keys first)
+        if (!std::is_same<decltype(ask), Values>::value && j > 0 && (j & 31) == 0) {
+            pages = page_of(P, s, my_block(2 * j + lane < 2 * mine ? 2 * j + lane : 2 * j));
+            if constexpr (E2M1) asm volatile("" : "+v"(pages));      // (waited for here, and not, with all that is on its way, wherever pages are looked up)
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int page = __builtin_amdgcn_readlane(pages, (2 * j + h) & 63);
-            f.x[h].load(P, block_in(P, page, head, my_block(2 * j + h)), lane);
+            ask(f.x[h], P, block_in(P, page, head, my_block(2 * j + h)), lane);
         }
     };
-    auto use = [&](const Pair &f, int j) __attribute__((always_inline)) {
+    auto use = [&](Pair &f, int j, auto more) __attribute__((always_inline)) {      // more: the next pair is asked for into the same registers
+        constexpr bool MORE = decltype(more)::value;
         const bool two = 2 * (wave + NW * j) + 1 < it.count;
         const int b0 = my_block(2 * j), b1 = my_block(2 * j + 1);
         const BlockLoad<D, C> &x0 = f.x[0], &x1 = f.x[1];
@@ -744,23 +766,9 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
         }
         f32x4 v0, v1;
         if constexpr (E2M1) {
-            // A value that is not finite makes its key's score NaN, and nothing else (a key's has become NaN by its scale): whoever sees it gets NaN
-            e0 = x0.ve;
-            e1 = x1.ve;
-            if (__builtin_amdgcn_ballot_w64((e0.most() > e1.most() ? e0.most() : e1.most()) == Scales4<D>::BAD))
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s0[i] = e0.w[i] == e0.BAD ? __builtin_nanf("") : s0[i];
-                    s1[i] = e1.w[i] == e1.BAD ? __builtin_nanf("") : s1[i];
-                    e0.w[i] = e0.w[i] == e0.BAD ? 0 : e0.w[i];
-                    e1.w[i] = e1.w[i] == e1.BAD ? 0 : e1.w[i];
-                }
+            if constexpr (MORE) load(f, j + 1, Keys());
+            __builtin_amdgcn_sched_barrier(0);   // (ahead of anything that waits for this pair's values)
             v0 = v1 = (f32x4){1.f, 1.f, 1.f, 1.f};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s0[i] *= A.scale;
-                s1[i] *= A.scale;
-            }
         } else {
             v0 = x0.vs;
             v1 = x1.vs;
@@ -770,8 +778,9 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
                 s1[i] *= x1.ks[i] * A.scale;
             }
         }
-        // (the scale of a hidden key's value may be NaN, in 4 bits some of them: behind the sequence's end a page holds anything)
-        if (!(two && all_visible(b0, s.pos, last, A.window, A.sinks) && all_visible(b1, s.pos, last, A.window, A.sinks))) {
+        // (the scale of a hidden key's value may be NaN)
+        const bool mixed = !(two && all_visible(b0, s.pos, last, A.window, A.sinks) && all_visible(b1, s.pos, last, A.window, A.sinks));
+        if (mixed) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 // (selections, no branches: of a branch over the whole wave around one over lanes this compiler has lost the inner one's assignments)
@@ -781,13 +790,10 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
                 v0[i] = see0 ? v0[i] : 0.f;
                 s1[i] = see1 ? s1[i] : -__builtin_inff();
                 v1[i] = see1 ? v1[i] : 0.f;
-                if constexpr (E2M1) {            // (hidden from every row)
-                    e0.w[i] = k0 > last ? 0 : e0.w[i];
-                    e1.w[i] = k1 > last ? 0 : e1.w[i];
-                }
             }
         }
         float mx = -__builtin_inff();
+        if constexpr (E2M1) s0 *= A.scale, s1 *= A.scale;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             // (a hidden key's score is -inf, whatever log2 makes of its scale of 0)
@@ -795,8 +801,23 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
                         a1 = PRODUCT ? s1[i] + __builtin_amdgcn_logf(fmaxf(v1[i], LEAST_SCALE)) : s1[i];
             mx = fmaxf(mx, fmaxf(a0, a1));
         }
-        const float m_new = fmaxf(m, quad_max(mx)), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+        float alpha = 1.f, m_new, m_use;
+        if constexpr (E2M1) {
+            // The maximum only keeps the powers of two in range: while it grows by less than 2^8 it stays, and the outputs with it
+            const float top = quad_max(mx);
+            m_new = m;
+            if (__builtin_amdgcn_ballot_w64(top > m + 8.f)) {
+                m_new = fmaxf(m, top);
+                alpha = __builtin_amdgcn_exp2f(m - (m_new == -__builtin_inff() ? 0.f : m_new));
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[t] *= alpha;
+            }
+            m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+        } else {
+            m_new = fmaxf(m, quad_max(mx));
+            m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+            alpha = __builtin_amdgcn_exp2f(m - m_use);
+        }
         float ps = 0.f, w0[4], w1[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -804,6 +825,28 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
             ps += p0 + p1;
             w0[i] = E2M1 ? p0 : p0 * v0[i];
             w1[i] = E2M1 ? p1 : p1 * v1[i];
+        }
+        if constexpr (E2M1) {
+            e0 = x0.ve;
+            e1 = x1.ve;
+            // behind the sequence's end a page holds anything
+            if (mixed)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e0.w[i] = b0 * 16 + 4 * g + i > last ? 0 : e0.w[i];
+                    e1.w[i] = b1 * 16 + 4 * g + i > last ? 0 : e1.w[i];
+                }
+            // A value that is not finite makes NaN of whoever sees it, and nothing else (a key's score has become NaN by its scale)
+            if (__builtin_amdgcn_ballot_w64((e0.most() > e1.most() ? e0.most() : e1.most()) == Scales4<D>::BAD))
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool bad0 = (e0.w[i] == e0.BAD) & (s0[i] != -__builtin_inff()), bad1 = (e1.w[i] == e1.BAD) & (s1[i] != -__builtin_inff());
+                    w0[i] = bad0 ? __builtin_nanf("") : w0[i];
+                    w1[i] = bad1 ? __builtin_nanf("") : w1[i];
+                    ps = (bad0 | bad1) ? __builtin_nanf("") : ps;
+                    e0.w[i] = e0.w[i] == e0.BAD ? 0 : e0.w[i];
+                    e1.w[i] = e1.w[i] == e1.BAD ? 0 : e1.w[i];
+                }
         }
         l = l * alpha + ps;                      // (of the lane's keys; the four lanes of a row meet at the end)
         m = m_new;
@@ -814,8 +857,8 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
                 i32x2 a0, b0, a1, b1;
                 H::template turn4<U>(x0.v.c[U], e0.w, a0, b0);
                 H::template turn4<U>(x1.v.c[U], e1.w, a1, b1);
-                o[2 * U] = H::mfma16((i32x4){a0[0], a0[1], a1[0], a1[1]}, pf, o[2 * U] * alpha);
-                o[2 * U + 1] = H::mfma16((i32x4){b0[0], b0[1], b1[0], b1[1]}, pf, o[2 * U + 1] * alpha);
+                o[2 * U] = H::mfma16((i32x4){a0[0], a0[1], a1[0], a1[1]}, pf, o[2 * U]);
+                o[2 * U + 1] = H::mfma16((i32x4){b0[0], b0[1], b1[0], b1[1]}, pf, o[2 * U + 1]);
             };
             outputs(std::integral_constant<int, 0>());
             outputs(std::integral_constant<int, 1>());
@@ -823,6 +866,7 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
                 outputs(std::integral_constant<int, 2>());
                 outputs(std::integral_constant<int, 3>());
             }
+            if constexpr (MORE) load(f, j + 1, Values());
         } else
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
@@ -832,15 +876,26 @@ __global__ void __launch_bounds__(512) k_attend_small(AttendArgs A) {
             o[t] = H::mfma16(vf, pf, o[t] * alpha);
         }
     };
-    if (mine > 0) {
+    if constexpr (E2M1) {
+        // The next keys are asked for into the registers of those whose scores are done, the next values into theirs: half of the registers, so
+        // that two workgroups fit on a compute unit
+        if (mine > 0) {
+            Pair f;
+            load(f, 0, Keys());
+            __builtin_amdgcn_sched_barrier(0);   // (in this order, so that the wait for keys is none for values)
+            load(f, 0, Values());
+            for (int j = 0; j < mine - 1; ++j) use(f, j, std::true_type());
+            use(f, mine - 1, std::false_type());
+        }
+    } else if (mine > 0) {
         Pair f0, f1;
-        load(f0, 0);
+        load(f0, 0, Both());
         for (int j = 0; j < mine; j += 2) {      // the next pair is on its way while one is used
-            if (j + 1 < mine) load(f1, j + 1);
-            use(f0, j);
+            if (j + 1 < mine) load(f1, j + 1, Both());
+            use(f0, j, std::false_type());
             if (j + 1 < mine) {
-                if (j + 2 < mine) load(f0, j + 2);
-                use(f1, j + 1);
+                if (j + 2 < mine) load(f0, j + 2, Both());
+                use(f1, j + 1, std::false_type());
             }
         }
     }
@@ -1224,7 +1279,7 @@ __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
         } while (!grown);
         if (!grown) break;
     }
-    l += __shfl_xor(l, 32, 64);
+    l = half_sum(l);
     if (it.slot < 0) {
         // through the LDS, so that rows leave in whole cache lines
         constexpr int ROW = D + 8, PIECES = D / 8;

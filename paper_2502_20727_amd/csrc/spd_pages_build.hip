@@ -21,7 +21,7 @@ struct BuildArgs {
     int64_t ld_table;
     int batch, tokens, q_len, entries, window, sinks;      // limits
     unsigned by_group;                                     // 2^32 / group, rounded up
-    int page_size, page_shift, n_pages, kv, group, most_end;      // most_end: positions a request may have
+    int cache_dtype, page_size, page_shift, n_pages, kv, group, most_end;      // most_end: positions a request may have
     int seqs, reqs, cuts, backs, order, small, large, merge, write, table;      // byte offsets
     int tails;                                             // workgroups of the second kernel for rows behind the last request
 };
@@ -229,14 +229,14 @@ __global__ void __launch_bounds__(THREADS) k_build_sums(BuildArgs A) {
     {
         const int which = n_many ? wave & 3 : 0, c0 = n_many ? wave >> 2 : wave, step = n_many ? WAVES / 4 : waves;
         const int n = which ? n_many : n_few, unit = which ? 4 : 2;
-        const int target = which == 0 ? SPD_SMALL_TARGET : SPD_COMPUTE_UNITS / 2 * (which + 1);
+        const int target = which == 0 ? spd_small_target(A.cache_dtype, (int64_t)n_few * A.kv) : SPD_COMPUTE_UNITS / 2 * (which + 1);
         const float2 *pieces = which ? many_pieces : few_pieces;
         if (which || cut_few) {
             // spd_first_chunk(), in 32 bits: no piece has more than 2^22 blocks, and 2^29 does for all that is more
             static_assert(SPD_SMALL_TARGET == 256 && SPD_COMPUTE_UNITS == 256, "targets are 128 times 2, 3 or 4");
             const unsigned long long share = (sums[which ? 1 : 0] * A.kv + 127) >> 7;
             const unsigned y = share < 1u << 31 ? (unsigned)share : 1u << 31;
-            const unsigned first = ((which == 2 ? (y + 2) / 3 : which == 3 ? (y + 3) / 4 : (y + 1) / 2) + unit - 1) & -unit;
+            const unsigned first = ((target == 384 ? (y + 2) / 3 : target == 512 ? (y + 3) / 4 : (y + 1) / 2) + unit - 1) & -unit;
             int chunk = first < (unsigned)unit ? unit : first < 1u << 29 ? (int)first : 1 << 29;
             auto next = [&]() {                            // spd_next_chunk(): units are powers of two
                 chunk = (chunk + chunk / 16 + unit) & -unit;
@@ -619,6 +619,7 @@ extern "C" int spd_pages_build(const spd_pages *pages, const void *plan_host, vo
     A.entries = h.entries;
     A.window = h.window;
     A.sinks = h.sinks;
+    A.cache_dtype = c.cache_dtype;
     A.page_size = c.page_size;
     A.page_shift = pages->shift + 4;
     A.n_pages = c.n_pages;

@@ -163,7 +163,7 @@ int plan_impl(const spd_pages *P, int32_t batch, const int32_t *positions, const
     const bool counted = (int64_t)few.size() * c.n_kv_heads <= SPD_COUNTERS;
     const int sets = spd_sets(P->group);
     auto most_small = [&](int blocks) { return spd_most_small(blocks, sets); };
-    cut(few, seqs, c.n_kv_heads, counted ? SPD_SMALL_TARGET : 0, 2, most_small, small, joined, small_slots);
+    cut(few, seqs, c.n_kv_heads, counted ? spd_small_target(c.cache_dtype, (int64_t)few.size() * c.n_kv_heads) : 0, 2, most_small, small, joined, small_slots);
     cut_large(many, seqs, c.n_kv_heads, large, merges, large_slots);
     for (const spd_plan_merge &m : merges) h.merge_rows = std::max(h.merge_rows, m.rows);
 
@@ -302,7 +302,7 @@ int spd_pages_reserve(const spd_pages *pages, const spd_pages_limits *limits, vo
     if (pieces > SPD_BUILD_PIECES) return SPD_EUNSUPPORTED;
     // Items, and those of them that are parts: with no more items than the target no more parts than that; with chunks made longer SPD_LONGER times, 2.6 times
     // what a workgroup would have, a piece that is longer than that has less than twice its length's worth of them.
-    const int64_t small_slots = SPD_SMALL_TARGET / kv, large_slots = pieces ? 2 * SPD_COMPUTE_UNITS / kv : 0;
+    const int64_t small_slots = spd_small_target(c.cache_dtype, most_few * kv) / kv, large_slots = pieces ? 2 * SPD_COMPUTE_UNITS / kv : 0;
     spd_plan_header h;
     std::memset(&h, 0, sizeof(h));
     h.magic = SPD_PLAN_MAGIC;
