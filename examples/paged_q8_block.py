@@ -2,16 +2,18 @@
 
 The operators of include/spd_q8.h put together the way a serving program would: 8-bit projections, keys and values quantised into
 pages as they are written, attention over the pages (with a sliding window and sinks if asked for), the SPD fold X + Y_r in the second norm, the
-partial MLP output added onto Y_r, and the one sync point that an SPD block keeps as a sum over the ranks' slots.
+partial MLP output added onto Y_r, and the one sync point that an SPD block keeps as a sum over the ranks' slots.  Decode steps then run as
+one captured graph whose plan is made on the device: requests grow into new pages and end without the host looking at a length.
 
     python examples/paged_q8_block.py            # LLaMA2-70B rank of 8: two prompts in chunks of 256, four sequences decoding beside them
+    python examples/paged_q8_block.py e2m1       # the same over pages of 4 bits (e4m3: 8 bits; bf16)
 """
 from __future__ import annotations
 
 import os
 import sys
 import time
-from typing import Dict, Sequence
+from typing import Dict, Sequence, Union
 
 import numpy as np
 import torch
@@ -67,8 +69,9 @@ class Q8Block:
         k, n = self.widths[name]
         B.spd_q8_matmul(self.codes[:len(out), :k], self.scales[:len(out)], self.weights[name], n, add, out, self.scratch)
 
-    def forward(self, plan: B.PagePlan, x, slots, x_out) -> None:
-        """x, x_out [tokens, hidden], slots [tp, tokens, hidden], fp32; the peers' slots are given, slot `rank` is written."""
+    def forward(self, plan: Union[B.PagePlan, B.DevicePlan], x, slots, x_out) -> None:
+        """x, x_out [tokens, hidden], slots [tp, tokens, hidden], fp32; the peers' slots are given, slot `rank` is written.  (Of a plan made on
+        the device the rows behind the last request's go through the products too: what they hold stays their own.)"""
         n, w = plan.tokens, self.w
         qkv, q, att, y, gu = (t[:n] for t in (self.qkv, self.q, self.att, self.y, self.gu))
         codes, scales = self.codes[:n], self.scales[:n]
@@ -92,11 +95,52 @@ class Q8Block:
         self.pages.close()
 
 
+class GraphSteps:
+    """Steps of a fixed number of requests as one captured graph.  Lengths, page table, free list and positions live on the device; a step reads
+    `q_lens` (new tokens of a request, 0: none, B.SPD_STEP_RELEASE: it has ended) and `x`, and leaves its output in `out`."""
+
+    def __init__(self, block: Q8Block, pool: PagedPool, done: Sequence[int], slots, q_len: int = 1, window: int = 0, sinks: int = 0):
+        """Takes over the requests with their pages and the free pages of the pool; slots [tp, tokens, hidden], whose tokens is the most of a step."""
+        c, dev, batch = block.pages.cfg, block.pages.device, len(done)
+        entries = -(-c.max_ctx // c.page_size)
+        self.block, self.slots = block, slots
+        self.plan = B.DevicePlan(block.pages, B.spd_pages_limits(batch, slots.shape[1], q_len, entries, window, sinks))
+
+        def held(values, n=None, dtype=torch.int32):
+            t = torch.full((len(values) if n is None else n,), -1, dtype=dtype)
+            t[:len(values)] = torch.tensor(list(values), dtype=dtype)
+            return t.to(dev)
+        self.positions, self.q_lens, self.served = held(done), held([0] * batch), held([0] * batch)
+        self.free, self.n_free = held(pool.free, c.n_pages), held([len(pool.free)])
+        self.table = torch.stack([held(pool.table.get(s, []), entries) for s in range(batch)])
+        pool.free, pool.table = [], {}
+        self.x = torch.zeros(slots.shape[1], block.w.hidden, device=dev)
+        self.out = torch.zeros_like(self.x)
+        side = torch.cuda.Stream(dev)
+        side.wait_stream(torch.cuda.current_stream(dev))
+        with torch.cuda.stream(side):
+            self._step()                          # (no request has new tokens)
+        torch.cuda.current_stream(dev).wait_stream(side)
+        self.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(self.graph):
+            self._step()
+
+    def _step(self) -> None:
+        B.spd_pages_build(self.block.pages.ctx, self.plan, self.positions, self.q_lens, self.table, self.free, self.n_free, n_free_out=self.n_free,
+                          positions_out=self.positions, served=self.served)
+        self.block.forward(self.plan, self.x, self.slots, self.out)
+
+    def step(self):
+        self.graph.replay()
+        return self.out
+
+
 def main() -> None:
+    cache = {"e4m3": B.SPD_E4M3, "e2m1": B.SPD_E2M1, "bf16": B.SPD_BF16}[sys.argv[1] if len(sys.argv) > 1 else "e4m3"]
     w = Workload(name="70b-rank", hidden=8192, n_q_heads=64, n_kv_heads=8, head_dim=128, ffn=28672, n_layers=1, tp=8, dtype=BF16, seed=3,
                  batch=6, q_len=1, ctx=2048, mask=(1,))
     rank, chunk, prompt = 0, 256, 1024
-    block = Q8Block(w, inputs.layer_shard(w, 0, rank), rank, max_tokens=2 * chunk + 4, n_pages=256, max_ctx=4096)
+    block = Q8Block(w, inputs.layer_shard(w, 0, rank), rank, max_tokens=2 * chunk + 4, n_pages=256, max_ctx=4096, cache=cache)
     pool = PagedPool(256, 64)
     g = torch.Generator(device="cuda").manual_seed(0)
     done: Dict[int, int] = {s: 0 for s in range(6)}
@@ -122,6 +166,22 @@ def main() -> None:
         step([1] * 4 + [chunk] * 2)
     for _ in range(4):
         step([1] * 6)
+
+    # the same six as a graph; the second one ends on the way, and its pages go to whoever needs one next
+    steps = GraphSteps(block, pool, [done[s] for s in range(6)], 0.05 * torch.randn(w.tp, 6, w.hidden, generator=g, device="cuda"), window=2048, sinks=4)
+    steps.q_lens.fill_(1)
+    for i in range(200):
+        if i in (100, 101):
+            steps.q_lens[1] = B.SPD_STEP_RELEASE if i == 100 else 0
+        if i in (0, 100, 102):
+            torch.cuda.synchronize()
+            t, first = time.perf_counter(), i
+        steps.x.normal_(generator=g)
+        steps.step()
+        if i in (99, 199):
+            torch.cuda.synchronize()
+            print(f"steps {first} to {i} as a graph: {(time.perf_counter() - t) / (i + 1 - first) * 1e6:8.1f} us each, then at {steps.positions.tolist()}, "
+                  f"{int(steps.n_free)} pages free, output rms {float(steps.out[:5].square().mean().sqrt()):.3f}", flush=True)
     block.close()
 
 

@@ -1,7 +1,7 @@
 /*
- * spd_q8.h - 8-bit serving operators of the SPD library: a paged KV cache that is quantised as it
- * is written, attention of chunks of new tokens over its pages, rows brought to 8-bit integers, and
- * the product of such rows with 8-bit weights.
+ * spd_q8.h - 8-bit serving operators of the SPD library: a paged KV cache that is quantised (to 8 or 4 bits) as it
+ * is written, attention of chunks of new tokens over its pages, plans of steps on the host or the device, rows
+ * brought to 8-bit integers, and the product of such rows with 8-bit weights.
  *
  * Together they make up a rank's share of a decoder block (spd.h) with 8-bit projections:
  *
@@ -17,8 +17,9 @@
  * The conventions are those of spd.h: error codes, host checks before anything is enqueued, caller-owned
  * buffers, nothing allocated, freed or waited for by a device call, work enqueued on `stream` alone.
  * A call that has nothing to do (no tokens, no rows) needs no addresses but its plan's.
- * The device calls may be captured into a HIP graph, which is then bound to what its calls were given on the host: a plan's launches
- * are those of its lengths, another plan takes another capture.  Results are bit-reproducible.
+ * The device calls may be captured into a HIP graph, which is then bound to what its calls were given on the host: the launches of a plan made
+ * there are those of its lengths, another such plan takes another capture; a graph with plans made on the device holds for every step
+ * within their limits.  Results are bit-reproducible.
  */
 #ifndef SPD_Q8_H
 #define SPD_Q8_H
@@ -129,7 +130,7 @@ int spd_pages_plan_get_info(const spd_pages *pages, const void *plan_host, spd_p
 typedef struct spd_pages_limits {
     int32_t batch;    /* requests: entries of the arrays below; at most 4096 */
     int32_t tokens;   /* rows of the step's matrices */
-    int32_t q_len;    /* new tokens of a request.  Up to 16 / (query heads per KV head) steps take one launch of attention, else three */
+    int32_t q_len;    /* new tokens of a request.  With up to 16 / (query heads per KV head) steps take one launch of attention, else two */
     int32_t entries;  /* pages of a request: columns of the page table */
     int32_t window, sinks;      /* as for spd_pages_plan() */
 } spd_pages_limits;

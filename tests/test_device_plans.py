@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_2502_20727_amd import binding as B
-from tests.test_q8_serving import LENGTHS, T16, config, tables
+from tests.test_q8_serving import LENGTHS, T16, _example, config, rotate, tables
 
 gpu_test = pytest.mark.gpu
 RELEASE, BAD_LENGTHS, BAD_PAGE, NO_PAGES = B.SPD_STEP_RELEASE, B.SPD_STEP_LENGTHS, B.SPD_STEP_PAGE, B.SPD_STEP_NO_PAGES
@@ -491,3 +491,120 @@ def test_another_stream_than_the_current_one(gpu):
     B.spd_pages_build(built.dp.ctx, built.plan, pos, lens, dev_table, **out, stream=side)
     side.synchronize()
     check_tables(built, {**out, "page_table": dev_table}, want)
+
+
+def block_of(ex, cache, max_tokens, n_pages, max_ctx, seed=11):
+    from paper_2502_20727_amd import inputs, workloads
+    w = workloads.Workload(name="q8-block", hidden=512, n_q_heads=16, n_kv_heads=4, head_dim=64, ffn=1376, n_layers=1, tp=2, dtype=workloads.BF16,
+                           seed=seed, batch=3, q_len=1, ctx=64, mask=(1,))
+    shard = inputs.layer_shard(w, 0, 1)
+    return w, shard, ex.Q8Block(w, shard, 1, max_tokens=max_tokens, n_pages=n_pages, page_size=16, max_ctx=max_ctx, cache=cache)
+
+
+@gpu_test
+@pytest.mark.parametrize("q_len", [1, 12])
+@pytest.mark.parametrize("cache", [B.SPD_E2M1, B.SPD_E4M3, B.SPD_BF16], ids=["e2m1", "e4m3", "bf16"])
+def test_block_as_one_graph(gpu, cache, q_len):
+    """A whole block by a plan made on the device, in one graph, against the block step by step with plans of the host: the same bits, since sums of integers
+    are exact, work is cut alike and everything else goes row by row."""
+    ex = _example()
+    w, _, block = block_of(ex, cache, 40, 60, 300)
+    _, _, mirror = block_of(ex, cache, 40, 60, 300)
+    batch, rows, g = 5, 20, torch.Generator().manual_seed(7)
+    slots = (0.05 * torch.randn(w.tp, rows, w.hidden, generator=g)).to(gpu)
+    pool = ex.PagedPool(60, 16)
+    steps = ex.GraphSteps(block, pool, [0] * batch, slots, q_len=q_len, window=50, sinks=2)
+    r, done = random.Random(q_len), [0] * batch
+    for i in range(30):
+        lens = [B.SPD_STEP_RELEASE if done[b] > 40 and r.random() < 0.1 else r.randint(0, min(q_len, rows // batch)) for b in range(batch)]
+        if q_len > 1 and i % 3 == 0:
+            lens = [q_len] + [n if n < 0 else min(n, 2) for n in lens[1:]]
+        x = torch.randn(rows, w.hidden, generator=g).to(gpu)
+        steps.x.copy_(x)
+        steps.q_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        out = steps.step()
+        assert steps.served.tolist() == [max(n, 0) for n in lens]
+        live = [b for b in range(batch) if lens[b] > 0]
+        n = sum(lens[b] for b in live)
+        if n:
+            plan = B.PagePlan(mirror.pages, [done[b] for b in live], [lens[b] for b in live], steps.table[live].cpu().numpy(), window=50, sinks=2)
+            peers, again = slots[:, :n].contiguous(), torch.empty(n, w.hidden, device=gpu)
+            mirror.forward(plan, x[:n], peers, again)
+            assert torch.equal(out[:n], again) and torch.equal(slots[1, :n], peers[1])
+            assert torch.equal(block.pages.pool, mirror.pages.pool)
+        done = [0 if lens[b] < 0 else done[b] + lens[b] for b in range(batch)]
+        assert steps.positions.tolist() == done
+        assert int(steps.n_free) == 60 - sum(-(-p // 16) for p in done)
+    block.close()
+    mirror.close()
+
+
+@gpu_test
+def test_block_over_pages_of_4_bits(gpu):
+    """A prompt, then steps as a graph, against the same block in 64 bits with nothing rounded.
+
+    A key or value row of a normal distribution is 11 % off in the root mean square (at most 12 % taken), a row of 8-bit integers 1 %, a product of such rows
+    and weights 1.5 %.  An output is a sum of values with probabilities: errors of single values average out as the values themselves do, 12 % of it; an error
+    of 12 % of scores of deviation s is one of 12 % s of the probabilities.  Queries, keys, values and the product with O: 1.5 % each.
+    In the MLP, gate and up are products of a norm whose error is Y's over X + Y and 1 %, each 1.5 % more, and silu changes by at most 1.1 of its input's change."""
+    ex = _example()
+    w, shard, block = block_of(ex, B.SPD_E2M1, 200, 60, 300)
+    W = {n: torch.from_numpy(a).double() for n, a in shard.items()}
+    q, kv, d = w.q_per_rank, w.kv_per_rank, w.head_dim
+    pool, g = ex.PagedPool(60, 16), torch.Generator().manual_seed(0)
+    past = [[torch.zeros(0, kv, d, dtype=torch.float64) for _ in range(2)] for _ in range(3)]
+    done, steps = [0, 0, 0], None
+
+    def norm(t, gain):
+        return t / (t.square().mean(-1, keepdim=True) + w.rms_eps).sqrt() * gain
+
+    for lens in ([90, 20, 60], [1, 1, 1], [1, 0, 1], [1, 1, 1]):
+        n = sum(lens)
+        x = torch.randn(n, w.hidden, generator=g)
+        peers = 0.05 * torch.randn(w.tp, n, w.hidden, generator=g)
+        if n > 3:
+            for s, m in enumerate(lens):
+                pool.grow(s, m)
+            plan = B.PagePlan(block.pages, done, lens, [pool.table[s] for s in range(3)], window=100, sinks=4)
+            slots, out = peers.to(gpu), torch.empty(n, w.hidden, device=gpu)
+            block.forward(plan, x.to(gpu), slots, out)
+            got = slots[1].cpu().double()
+        else:
+            if steps is None:
+                steps = ex.GraphSteps(block, pool, done, torch.zeros(w.tp, 3, w.hidden, device=gpu), window=100, sinks=4)
+            steps.slots[:, :n].copy_(peers)
+            steps.x[:n].copy_(x)
+            steps.q_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+            out = steps.step()[:n]
+            got = steps.slots[1, :n].cpu().double()
+        X = x.double()
+        qkv = norm(X, W["g1"])
+        Q, K, V = ((qkv @ W[name]).unflatten(-1, (-1, d)) for name in ("wq", "wk", "wv"))
+        att, first, spread = [], 0, []
+        for s, m in enumerate(lens):
+            at = torch.arange(done[s], done[s] + m)
+            mine = slice(first, first + m)
+            first += m
+            past[s][0] = torch.cat([past[s][0], rotate(K[mine], at, w.rope_base)])
+            past[s][1] = torch.cat([past[s][1], V[mine]])
+            key = torch.arange(done[s] + m)
+            seen = (key <= at[:, None]) & ((key > at[:, None] - 100) | (key < 4))
+            qs, o = rotate(Q[mine], at, w.rope_base), torch.zeros(m, q, d, dtype=torch.float64)
+            for j in range(q):
+                sc = qs[:, j] @ past[s][0][:, j // (q // kv)].t() / math.sqrt(d)
+                spread.append(sc[seen])
+                o[:, j] = sc.masked_fill(~seen, -math.inf).softmax(-1) @ past[s][1][:, j // (q // kv)]
+            att.append(o.flatten(1))
+            done[s] += m
+        y = torch.cat(att) @ W["wo"]
+        m = norm(X + y, W["g2"])
+        gate = m @ W["wg"]
+        z = (gate * torch.sigmoid(gate) * (m @ W["wu"])) @ W["wd"]
+        s2 = float(torch.cat(spread).square().mean())
+        of_y = math.sqrt(0.12 ** 2 * (1 + s2) + 4 * 0.015 ** 2)
+        of_m = of_y * float(y.norm() / (X + y).norm()) + 0.01
+        bound = of_y * float(y.norm()) + (2.1 * (of_m + 0.015) + 0.015) * float(z.norm())
+        assert float((got - (y + z)).norm()) < bound
+        assert float((out.cpu().double() - (X + peers[0].double() + got)).abs().max()) < 1e-5
+    assert steps.positions.tolist() == done
+    block.close()
