@@ -483,8 +483,11 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Reading back.  One workgroup per four 16-position blocks and KV head, a wave per block.  A lane's keys are pieces of rows; its values
-// (four positions of several features) change places in the LDS.  16 contexts of up to 4096 of one KV head, bf16: 8.7 us (33 MB: 3.8 TB/s, a launch of 3 us among them).
+// Reading back.  One workgroup per four 16-position blocks and KV head, a wave per block; the heads of a block next to each other, since their rows are that in
+// the output.  A lane's keys are pieces of rows; its values (four positions of several features) change places in the LDS, and so do keys of 4
+// bits.  Bound by what is read and written.  The output goes past the caches, which cannot hold it, and leaves them to the codes.  4 bits, us a call: 24 contexts
+// of up to 8000 on 5 heads, fp16, 421 MB: 92 -> 83 (heads next to each other) -> 66 (past the caches; 6.3 TB/s; codes read past them too 75); 16 of up to
+// 4096 on one head, bf16, 29.5 MB: 7.0 -> 6.5.  e4m3, the latter (33 MB): 9.3 -> 7.9.
 // ------------------------------------------------------------------------------------------
 template <class Out, int D, int C, bool F16>
 __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_out) {
@@ -496,7 +499,8 @@ __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_
     __shared__ __attribute__((aligned(16))) Out turned[4][16 * ROW];
     const spd_plan_seq s = ((const spd_plan_seq *)(P.plan + P.seqs))[blockIdx.y];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int block = blockIdx.x * 4 + wave, head = blockIdx.z, r = lane & 15, g = lane >> 4;
+    const int head = blockIdx.x % P.kv, r = lane & 15, g = lane >> 4;
+    const int block = blockIdx.x / P.kv * 4 + wave;
     if (block * 16 >= s.end) return;             // (a wave works by itself)
     const Block B = block_at(P, s, head, block);
     Out *mine = turned[wave];
@@ -508,7 +512,7 @@ __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_
         for (int i = lane; i < 16 * PIECES; i += 64) {
             const int pr = i / PIECES, f = (i % PIECES) * (16 / (int)sizeof(Out));
             if (pr < n)
-                *(Piece *)__builtin_assume_aligned(to + row0 + pr * pitch + f, 16) = *(const Piece *)__builtin_assume_aligned(mine + pr * ROW + f, 16);
+                __builtin_nontemporal_store(*(const i32x4 *)__builtin_assume_aligned(mine + pr * ROW + f, 16), (i32x4 *)__builtin_assume_aligned(to + row0 + pr * pitch + f, 16));
         }
         __builtin_amdgcn_wave_barrier();
     };
@@ -586,7 +590,7 @@ __global__ void __launch_bounds__(256) k_pages_read(Pages P, Out *k_out, Out *v_
                 Piece q;
 #pragma unroll
                 for (int e = 0; e < 16 / (int)sizeof(Out); ++e) q.v[e] = piece[i + e];
-                *(Piece *)__builtin_assume_aligned(k_out + row0 + r * pitch + c * 4 * E + g * E + i, 16) = q;
+                __builtin_nontemporal_store(__builtin_bit_cast(i32x4, q), (i32x4 *)__builtin_assume_aligned(k_out + row0 + r * pitch + c * 4 * E + g * E + i, 16));
             }
         }
     }
@@ -1505,7 +1509,7 @@ int spd_pages_read(const spd_pages *pages, const void *plan_host, const void *pl
     if (!pool || !k_out || !v_out || !aligned(pool, 256) || !aligned(k_out, 16) || !aligned(v_out, 16)) return SPD_EINVAL;
     (void)hipGetLastError();
     const Pages P = pages_args(pages, h, plan_dev, pool, 0);
-    const dim3 grid((h.max_end + 63) / 64, h.batch, c.n_kv_heads);
+    const dim3 grid((h.max_end + 63) / 64 * c.n_kv_heads, h.batch);
     SPD_HIP(by_kind(pages, [&](auto d, auto e, auto f) {
         constexpr int D = decltype(d)::value;
         constexpr int E = decltype(e)::value;

@@ -78,7 +78,7 @@ __device__ __forceinline__ void scan(unsigned (&v)[N], unsigned (&total)[N], uns
 }
 
 // n / d rounded up, less one, of whole numbers in floats, `inverse` = 1 / d rounded to the nearest.  (n - 0.5) / d is 0.5 / d from a whole number at least, and the
-// result less than n / d * 2^-23 off: exact for n below 2^22, which is the blocks of the longest sequence.
+// result less than n / d * 2^-23 off: exact for n up to 2^22, which is the blocks of the longest sequence.
 __device__ __forceinline__ float times_less_one(float n, float inverse) { return floorf(fmaf(n, inverse, -0.5f * inverse)); }
 
 // The first kernel.  PER requests a thread, one after the other.  Bound by how long one thing waits for another: loads, about six
