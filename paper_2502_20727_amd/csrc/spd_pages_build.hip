@@ -4,7 +4,7 @@
 // Two kernels.  The first, a single workgroup, adds up: everything that one request has to know of the others is a prefix sum over them (rows, pages
 // needed, pages that come back, blocks written, items), and the chunk that work is cut into is a search over sums, as on the host
 // (spd_pages.h).  The second has a workgroup per request, checks its pages and writes what is the request's.  A request whose pages are not of
-// the pool is found out there and leaves its items empty.
+// the pool is found out there and leaves its items empty.  (A single request of few rows takes both in one launch.)
 #include <algorithm>
 #include <cstring>
 
@@ -82,9 +82,14 @@ __device__ __forceinline__ void scan(unsigned (&v)[N], unsigned (&total)[N], uns
 __device__ __forceinline__ float times_less_one(float n, float inverse) { return floorf(fmaf(n, inverse, -0.5f * inverse)); }
 
 // The first kernel.  PER requests a thread, one after the other.  Bound by how long one thing waits for another: loads, about six
-// sums over the workgroup, barriers, and the fetching of its own instructions, which is why little of it is unrolled or divides in 64 bits.
+// sums over the workgroup, barriers, and the fetching of its own instructions, which is why little of it is unrolled or divides in 64 bits.  us, one
+// request / 256 with four chunks of prompts / 2048 with 64: 4.8 / 11.0 / 24, both launches 11.4 / 17.6 / 33.1 (chunks tried one after the other by the whole workgroup, dividing in 64
+// bits: 32.0 / 57.1 / 119.8).
+struct Sums {
+    int rows, free0, top, n_backs, sorted;      // as in the header
+};
 template <int PER>
-__global__ void __launch_bounds__(THREADS) k_build_sums(BuildArgs A) {
+__device__ __forceinline__ Sums build_sums(const BuildArgs &A) {
     __shared__ unsigned lds[3][WAVES * 8];
     __shared__ int many_pos[PER * THREADS], many_rows[PER * THREADS], many_first[PER * THREADS];      // requests of many rows: position, rows, first piece
     // Of the pieces of few rows, of many: blocks; the most items that each may be cut into, later those that it is, less one.  Whole numbers in floats, which
@@ -420,38 +425,40 @@ __global__ void __launch_bounds__(THREADS) k_build_sums(BuildArgs A) {
         if (lane == 0) atomicAdd(&took, taken);
         __syncthreads();
     }
+    const Sums now = {(int)t[0] < A.tokens ? (int)t[0] : A.tokens, free0, top, (int)t[2], sorted};
     if (tid == 0) {
         H.n_small = n_small;
         H.n_large = n_large;
         H.n_merge = n_merge;
         H.n_write = t[6];
-        H.rows = (int)t[0] < A.tokens ? (int)t[0] : A.tokens;
+        H.rows = now.rows;
         H.free0 = free0;
         H.top = top;
-        H.n_backs = t[2];
+        H.n_backs = now.n_backs;
         H.sorted = sorted;
         if (A.n_free_out) *A.n_free_out = top - (int)(short_of_pages ? took : t[3]);
-        if (A.first_row) A.first_row[A.batch] = (int)t[0] < A.tokens ? (int)t[0] : A.tokens;
+        if (A.first_row) A.first_row[A.batch] = now.rows;
     }
+    return now;
 }
+template <int PER>
+__global__ void __launch_bounds__(THREADS) k_build_sums(BuildArgs A) { build_sums<PER>(A); }
 
 constexpr int CHUNK_ROWS = 2048, CHUNK_PAGES = CHUNK_ROWS / 16 + 1;
 
-// The second kernel: a workgroup per request and 2048 of its rows.
-__global__ void __launch_bounds__(256) k_build_requests(BuildArgs A) {
-    const spd_plan_header &H = *(const spd_plan_header *)A.plan;
-    const int tid = threadIdx.x, chunk = blockIdx.y;
-    auto no_row = [&](int row) {
-        if (A.row_seq) A.row_seq[row] = -1;
-        if (A.row_pos) A.row_pos[row] = -1;
-        if (A.row_slot) A.row_slot[row] = -1;
-    };
-    if ((int)blockIdx.x >= A.batch) {            // rows behind the last request
-        const int n = gridDim.y * A.tails;
-        for (int row = H.rows + ((blockIdx.x - A.batch) * gridDim.y + chunk) * 256 + tid; row < A.tokens; row += n * 256) no_row(row);
-        return;
-    }
-    const int b = blockIdx.x, free0 = H.free0, top = H.top;
+// rows behind the last request: the i-th of n workgroups
+__device__ __forceinline__ void no_row(const BuildArgs &A, int row) {
+    if (A.row_seq) A.row_seq[row] = -1;
+    if (A.row_pos) A.row_pos[row] = -1;
+    if (A.row_slot) A.row_slot[row] = -1;
+}
+__device__ __forceinline__ void build_tail(const BuildArgs &A, int rows, int i, int n) {
+    for (int row = rows + i * 256 + threadIdx.x; row < A.tokens; row += n * 256) no_row(A, row);
+}
+
+// A request and 2048 of its rows, by 256 threads.
+__device__ __forceinline__ void build_request(const BuildArgs &A, const Sums &H, int b, int chunk) {
+    const int tid = threadIdx.x, free0 = H.free0, top = H.top;
     const spd_plan_req *reqs = (const spd_plan_req *)(A.plan + A.reqs);
     const spd_plan_back *backs = (const spd_plan_back *)(A.plan + A.backs);
     int32_t *row = A.page_table + b * A.ld_table;
@@ -519,7 +526,7 @@ __global__ void __launch_bounds__(256) k_build_requests(BuildArgs A) {
             const int at = r.tok0 + row0 + i, p = r.pos + row0 + i;
             if (at >= A.tokens) break;
             if (!served) {
-                no_row(at);
+                no_row(A, at);
                 continue;
             }
             if (A.row_seq) A.row_seq[at] = b;
@@ -563,6 +570,24 @@ __global__ void __launch_bounds__(256) k_build_requests(BuildArgs A) {
         for (int i = tid & 7; i < c.parts; i += 8) item((spd_plan_item *)(A.plan + A.large) + c.item0 + i, w, first_row, 4, c.parts, i, c.slot0, c.merge);
         if (c.parts > 1 && (tid & 7) == 0) ((spd_plan_merge *)(A.plan + A.merge))[c.merge] = spd_plan_merge{s, first_row, served ? mine : 0, c.slot0, c.parts};
     }
+}
+
+// The second kernel: a workgroup per request and 2048 of its rows, and some for the rows behind.  Three loads that wait for each other (request, page, the rows of those
+// whose pages came back): us, one request / 256 / 2048 of up to 2000 positions 3.7 / 5.7 / 8.9.
+__global__ void __launch_bounds__(256) k_build_requests(BuildArgs A) {
+    const spd_plan_header &h = *(const spd_plan_header *)A.plan;
+    const Sums H = {h.rows, h.free0, h.top, h.n_backs, h.sorted};
+    if ((int)blockIdx.x < A.batch) return build_request(A, H, blockIdx.x, blockIdx.y);
+    build_tail(A, H.rows, (blockIdx.x - A.batch) * gridDim.y + blockIdx.y, gridDim.y * A.tails);
+}
+
+// Both for a single request of few rows (interactive decoding): a launch less, whose enqueuing is what a call outside of a graph waits for.  us a call, this / two
+// kernels: 9.0 / 11.4, in a graph 7.6 / 8.1; a second request would have to wait for the first: 10.6 / 11.0, 10.6 / 8.6.
+__global__ void __launch_bounds__(256) k_build_one(BuildArgs A) {
+    const Sums H = build_sums<1>(A);
+    __syncthreads();
+    build_request(A, H, 0, 0);
+    if (A.tails) build_tail(A, H.rows, 0, 1);
 }
 
 inline bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -640,6 +665,11 @@ extern "C" int spd_pages_build(const spd_pages *pages, const void *plan_host, vo
     const bool by_row = t.row_seq || t.row_pos || t.row_slot;
     A.tails = by_row ? std::min(64, (h.tokens + 255) / 256) : 0;
     hipStream_t s = (hipStream_t)stream;
+    if (!h.n_large && h.batch == 1) {
+        hipLaunchKernelGGL(k_build_one, dim3(1), dim3(256), 0, s, A);
+        SPD_HIP(hipGetLastError());
+        return SPD_OK;
+    }
     const int threads = h.n_large ? THREADS : std::min(THREADS, (h.batch + 63) / 64 * 64);
     if (h.batch <= THREADS) hipLaunchKernelGGL((k_build_sums<1>), dim3(1), dim3(threads), 0, s, A);
     else hipLaunchKernelGGL((k_build_sums<SPD_BUILD_BATCH / THREADS>), dim3(1), dim3(THREADS), 0, s, A);

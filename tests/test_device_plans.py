@@ -259,6 +259,51 @@ def test_tables_are_those_of_a_stack(gpu, batch, wrong):
 
 
 @gpu_test
+@pytest.mark.parametrize("page,n_ctx", [(16, 100), (64, 700), (16, 40000), (256, 2000)])
+def test_tables_of_a_single_request(gpu, page, n_ctx):
+    r = random.Random(n_ctx)
+    for i in range(16):
+        positions, q_lens, table, free, n_free, n_pages, entries = scenario(r, 1, page, n_ctx, 4, r.choice([1.0, 0.0]), i % 4 == 3)
+        tokens = 4 + r.choice([0, 0, 3, 700])
+        cfg = config(q=8, kv=2, d=64, page=page, n_pages=n_pages, cache=B.SPD_E2M1, max_ctx=entries * page)
+        lim = limits(1, tokens, 4, entries)
+        built = Built(gpu, cfg, lim, rope=False)
+        check_tables(built, built.build(positions, q_lens, table, free, n_free), model(cfg, lim, positions, q_lens, table, free, n_free))
+        check_tables(built, built.build(positions, q_lens, table), model(cfg, lim, positions, q_lens, table))
+
+
+@gpu_test
+def test_a_single_request_in_a_graph(gpu):
+    """Grows token by token, ends, and begins anew, by replays of one graph."""
+    cfg = config(q=8, kv=2, d=64, page=16, n_pages=12, cache=B.SPD_E2M1, max_ctx=160)
+    lim = limits(1, 5, 3, 10)
+    built = Built(gpu, cfg, lim, rope=False)
+    at, q_lens, n_free, free, table = (built.put(x) for x in ([0], [0], [12], np.arange(12)[::-1], np.full((1, 10), -1)))
+    out = dict(built.out, n_free_out=n_free, positions_out=at)
+
+    def step():
+        B.spd_pages_build(built.dp.ctx, built.plan, at, q_lens, table, free_pages=free, n_free=n_free, **out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    position, rows, stack, n = [0], np.full((1, 10), -1, dtype=np.int32), free.cpu().numpy(), 12
+    r = random.Random(5)
+    for _ in range(60):
+        lens = [RELEASE if position[0] > 100 and r.random() < 0.2 else r.choice([0, 1, 1, 2, 3, 3, 3])]
+        want = model(cfg, lim, position, lens, rows, stack, n)
+        q_lens.copy_(built.put(lens))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_tables(built, {**out, "page_table": table, "free_pages": free}, want)
+        position, rows, stack, n = want["positions_out"].tolist(), want["page_table"], want["free_pages"], int(want["n_free_out"][0])
+
+
+@gpu_test
 @pytest.mark.parametrize("n_free", [-3, 0, 40, 41, 1 << 30])
 def test_counts_of_free_pages_that_cannot_be(gpu, n_free):
     cfg = config(page=16, n_pages=40)
@@ -346,6 +391,13 @@ def both_ways(dev, cfg, positions, q_lens, window=0, sinks=0, spare=5, idle=0, s
 @pytest.mark.parametrize("positions,q_lens", LENGTHS, ids=lambda v: "-".join(map(str, v)))
 def test_same_bits_as_planned_on_the_host(gpu, dtype, cache, positions, q_lens):
     both_ways(gpu, config(dtype=dtype, cache=cache, page=32, n_pages=60), list(positions), list(q_lens), idle=2, seed=sum(q_lens))
+
+
+@gpu_test
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("position,q_len", [(0, 1), (15, 1), (16, 2), (1500, 1), (1000, 4)])
+def test_same_bits_for_a_single_request(gpu, dtype, cache, position, q_len):
+    both_ways(gpu, config(q=8, kv=2, dtype=dtype, cache=cache, page=32, n_pages=60, max_ctx=1600), [position], [q_len], spare=300, seed=position)
 
 
 @gpu_test
