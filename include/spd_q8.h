@@ -169,7 +169,8 @@ typedef struct spd_pages_step {
  * are left and for all that need any after them none (SPD_STEP_NO_PAGES).  A request that is not served keeps its positions (and pages that were handed to it), its
  * rows of outputs stay as they were.  Two requests may share pages for reading; that the page of a new token is one request's alone, and a page at most once in the
  * free list and the tables of those that have ended, is the caller's to see to: it is not checked.
- * plan_dev: device_bytes, 16-byte aligned.  Arrays may share no memory but for what is said above.
+ * plan_dev: device_bytes, 16-byte aligned; calls on other streams that still read the plan of the step before have to be over.  Arrays may share no memory but
+ * for what is said above.
  * SPD_EINVAL: NULL, a plan made on the host, alignment, ld_table, shared memory. */
 int spd_pages_build(const spd_pages *pages, const void *plan_host, void *plan_dev, const spd_pages_step *step, void *stream);
 

@@ -196,7 +196,8 @@ __device__ __forceinline__ Block block_at(const Pages &P, const spd_plan_seq &s,
 // Writing.  One workgroup per 16-position block and a few heads: sixteen threads per token, D / 16 of them to a row of D features, each with
 // eight of one rotary half and the eight that they turn with.  A workgroup of KV heads has keys and values side by side; one of
 // query heads keeps its angles for all of its heads.  Bound by what is read and written: four prompts of 2048 tokens, 64 + 2 x 8 heads in bf16,
-// 68 us (319 MB: 4.7 TB/s).
+// 68 us (319 MB: 4.7 TB/s), over pages of 4 bits 58 to 62 (311 MB, 5 TB/s; the rotation in 64 bits hides behind the memory).  (Rotated queries written past the caches: 4 less, but
+// the attention behind it fetches them again: both together 364 -> 374.)
 // ------------------------------------------------------------------------------------------
 struct WriteArgs {
     Pages P;
@@ -694,6 +695,10 @@ __device__ __forceinline__ float2 part_get(const float *p) {
 // Few rows (a decode step, a short draft): one workgroup per item and KV head, its eight waves take pairs of blocks in turn and merge
 // their states in the LDS.  Rows cut into several items are joined, in the items' order, by the workgroup that ends last.
 // Lane = 16 g + row.
+// Bound by HBM where there is enough to read, else by loads that wait for each other (plan, page, keys, values, the join: 7.8 us for one sequence of 2048).  4 bits: keys
+// and values are asked for as soon as those in their registers are done with, 118 registers, two workgroups to a compute unit; outputs are scaled only where
+// the maximum has grown by 2^8.  16 sequences of 8001 on 32 heads 87 us (557 MB: 6.4 TB/s; 105 with pairs of blocks in registers of their own and one
+// workgroup), 48 of up to 16000 on one 19.4 (21.8).
 // (so, sm, sl, ended: its LDS, objects of the kernel of their own, which the compiler then knows to lie apart)
 template <int D>
 using SmallOutputs = float[SPD_SMALL_WAVES][16][D + 4];
@@ -1027,6 +1032,9 @@ __global__ void __launch_bounds__(512, C == SPD_E2M1 ? 4 : 1) k_attend_small(Att
 // four prompts of 2048 tokens on 64 heads of 8 in 335 us, 0.82 PFLOP/s, where nothing but MFMAs on such data does 1.7.  (Two row tiles per wave
 // and one workgroup per compute unit, which read the LDS half as often: 541 us beside 363, no second wave to work beside the first's softmax.)
 // 16-bit pages need no scales, a bad row's key is NaN instead: three windowed chunks of 333 tokens 26.8 -> 23.7 us.
+// 4-bit pages are 16-bit values once they are in the LDS (code and scale widened in one instruction): the prompts 310 to 318 us, 0.87 PFLOP/s; 1.97 us a tile
+// with two workgroups on a compute unit, 51 of the 318 starts and ends of the 4096 workgroups, clock 1.97 GHz.  (The scores contracted in 4 bits, with queries in 8: no faster, and
+// that instruction's own sum is good to 2^-12 of its largest product only.  Scores of the next tile beside the softmax of this one: 256 registers, 326 beside 321.)
 template <int D, int C, bool F16>
 __global__ void __launch_bounds__(256, 2) k_attend_large(AttendArgs A) {
     constexpr bool E4M3 = C == SPD_E4M3, E2M1 = C == SPD_E2M1;
