@@ -660,3 +660,53 @@ def test_block_over_pages_of_4_bits(gpu):
         assert float((out.cpu().double() - (X + peers[0].double() + got)).abs().max()) < 1e-5
     assert steps.positions.tolist() == done
     block.close()
+
+
+@gpu_test
+@pytest.mark.parametrize("cache", [B.SPD_E2M1, B.SPD_E4M3], ids=["e2m1", "e4m3"])
+def test_two_plans_on_two_streams(gpu, cache):
+    """Sequences of one pool served in two halves, each with a plan, a scratch and a stream of its own, against one stream after the other."""
+    cfg = config(page=16, n_pages=400, cache=cache, max_ctx=1200)
+    dp = B.DevicePages(cfg, gpu)
+    width, cols, t = (cfg.n_q_heads + 2 * cfg.n_kv_heads) * cfg.head_dim, cfg.n_q_heads * cfg.head_dim, T16[cfg.dtype]
+    lim, dev = limits(4, 90, 60, 75), gpu
+    lens = [[700, 3, 0, 90], [1, 900, 333, 40]], [[1, 60, 5, 1], [1, 1, 1, 50]]
+    order = np.random.RandomState(3).permutation(400)
+    g = torch.Generator().manual_seed(4)
+    halves, first = [], 0
+    for h in range(2):
+        positions, q_lens = lens[0][h], lens[1][h]
+        rows = []
+        for p, n in zip(positions, q_lens):
+            pages = -(-(p + n) // 16)
+            rows.append([int(x) for x in order[first:first + pages]])
+            first += pages
+        table = np.full((4, 75), -1, dtype=np.int32)
+        for b, row in enumerate(rows):
+            table[b, :len(row)] = row
+        past = torch.randn(sum(positions), width, generator=g).to(t).to(dev)
+        B.spd_pages_write(dp.ctx, B.PagePlan(dp, [0] * 4, positions, rows), past, dp.rope, dp.pool)
+        put = lambda x: torch.as_tensor(np.asarray(x, dtype=np.int32)).to(dev)      # noqa: E731
+        halves.append(dict(plan=B.DevicePlan(dp, lim), at=put(positions), n=put(q_lens), table=put(table), tokens=sum(q_lens),
+                           qkv=torch.randn(90, width, generator=g).to(t).to(dev), q=torch.zeros(90, cols, dtype=t, device=dev), o=torch.zeros(90, cols, dtype=t, device=dev)))
+
+    def run(h, stream):
+        B.spd_pages_build(dp.ctx, h["plan"], h["at"], h["n"], h["table"], stream=stream)
+        B.spd_pages_write(dp.ctx, h["plan"], h["qkv"], dp.rope, dp.pool, h["q"], stream=stream)
+        B.spd_pages_attention(dp.ctx, h["plan"], h["q"], dp.pool, h["o"], h["plan"].workspace, stream=stream)
+    start = dp.pool.clone()
+    for h in halves:
+        run(h, None)
+    torch.cuda.synchronize()
+    want, pool = [h["o"].clone() for h in halves], dp.pool.clone()
+    assert all(bool(o[:h["tokens"]].float().abs().sum(1).gt(0).all()) and not bool(o[h["tokens"]:].any()) for o, h in zip(want, halves))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        dp.pool.copy_(start)
+        for h in halves:
+            h["o"].zero_()
+        torch.cuda.synchronize()
+        for h, s in zip(halves, streams):
+            run(h, s)
+        torch.cuda.synchronize()
+        assert torch.equal(dp.pool, pool) and all(torch.equal(h["o"], o) for h, o in zip(halves, want))
