@@ -166,8 +166,11 @@ typedef struct spd_pages_step {
 
 /* Device call.  Rows go to requests in order, max(q_len, 0) to each, whether it is served or not (within the limit).  Pages that come back are pushed in the
  * requests' order, each request's in the order of its positions; then pages are popped in the same order, for requests that need more than
- * are left and for all that need any after them none (SPD_STEP_NO_PAGES).  A request that is not served keeps its positions (and pages that were handed to it), its
- * rows of outputs stay as they were.  Two requests may share pages for reading; that the page of a new token is one request's alone, and a page at most once in the
+ * are left and for all that need any after them none (SPD_STEP_NO_PAGES).  A request that is not served keeps its positions, its rows of outputs stay as they were.
+ * SPD_STEP_PAGE tells of a table or a free list that is not sound: new pages have been written into the request's row all the same.  Where the page that is none is one that
+ * it had, later steps hand it no others as long as a page lies in the first place behind ceil(positions / page_size); where it came from the free list (of
+ * which a request that ended with such an entry makes it part) it is gone with the step, and so are the new pages beside it.  Who mends the table makes the free list anew of the pages that
+ * are in nobody's first ceil(positions / page_size) entries.  Two requests may share pages for reading; that the page of a new token is one request's alone, and a page at most once in the
  * free list and the tables of those that have ended, is the caller's to see to: it is not checked.
  * plan_dev: device_bytes, 16-byte aligned; calls on other streams that still read the plan of the step before have to be over.  Arrays may share no memory but
  * for what is said above.

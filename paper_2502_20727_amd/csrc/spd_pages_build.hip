@@ -115,17 +115,64 @@ __device__ __forceinline__ Sums build_sums(const BuildArgs &A) {
     if (tid < 9) counts[tid / 3][tid % 3] = 0;
     if (tid < 64) fits[tid / SPD_LONGER][tid % SPD_LONGER] = 0;
     for (int i = tid; i < 512; i += blockDim.x) buckets[i >> 8][i & 255] = 0;
-    bool fine[PER], got[PER];                              // its lengths are within the limits; there are pages for it
+    bool fine[PER], got[PER], stuck[PER];                  // its lengths are within the limits; there are pages for it; it has a page that is none, and new ones already
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
-        fine[k] = got[k] = pos[k] >= 0 && q[k] >= SPD_STEP_RELEASE && q[k] <= A.q_len && pos[k] <= A.most_end - (q[k] > 0 ? q[k] : 0);
+    for (int k = 0; k < PER; ++k) {
+        fine[k] = pos[k] >= 0 && q[k] >= SPD_STEP_RELEASE && q[k] <= A.q_len && pos[k] <= A.most_end - (q[k] > 0 ? q[k] : 0);
+        stuck[k] = false;
+    }
     auto rows_of = [&](int k) { return q[k] > 0 && q[k] <= A.q_len ? q[k] : 0; };
     auto held_of = [&](int k) { return (pos[k] + A.page_size - 1) >> A.page_shift; };
     auto back_of = [&](int k) { return A.free_pages && fine[k] && q[k] < 0 ? held_of(k) : 0; };
-    auto need_of = [&](int k) { return A.free_pages && fine[k] && q[k] > 0 ? ((pos[k] + q[k] + A.page_size - 1) >> A.page_shift) - held_of(k) : 0; };
+    auto need_of = [&](int k) { return A.free_pages && fine[k] && !stuck[k] && q[k] > 0 ? ((pos[k] + q[k] + A.page_size - 1) >> A.page_shift) - held_of(k) : 0; };
     auto few_of = [&](int k) { return got[k] && q[k] > 0 && q[k] * A.group <= SPD_SMALL_ROWS; };
     auto pieces_of = [&](int k) { return got[k] && q[k] > 0 && q[k] * A.group > SPD_SMALL_ROWS ? (q[k] * A.group + SPD_LARGE_ROWS - 1) / SPD_LARGE_ROWS : 0; };
     auto writes_of = [&](int k) { return got[k] && q[k] > 0 ? (pos[k] + q[k] - 1) / 16 - pos[k] / 16 + 1 : 0; };
+    // A request that has a page that is none is refused by the second kernel, when new pages are in its row already.  Its positions stay, so that the next step would hand
+    // it others and the first would be nobody's: where a page lies in the first new place it is refused here and takes none.  Each wave looks by itself, through the entries of
+    // those of its requests that want pages (in most steps few do), sixteen lanes a request: of 1 / 64 / 256 / 2048 requests 0 / 0.7 / 1.7 / 2.7 us a plan.
+    {
+        auto a_page = [&](int page) { return (unsigned)page < (unsigned)A.n_pages; };
+        int *mine = many_first + wave * 64 * PER, *held = many_rows + wave * 64 * PER, *found = many_pos + wave * 64 * PER;      // request, its entries, is it so?
+        int n = 0, at[PER];
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const bool asks = need_of(k) && held_of(k);
+            const unsigned long long who = __builtin_amdgcn_ballot_w64(asks);
+            at[k] = asks ? n + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0)) : -1;
+            if (asks) {
+                mine[at[k]] = tid * PER + k;
+                held[at[k]] = held_of(k);
+                found[at[k]] = 0;
+            }
+            n += __builtin_popcountll(who);
+        }
+        if (n) {
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (int i = lane >> 4; i < n; i += 4) {
+                const int32_t *row = A.page_table + mine[i] * A.ld_table;
+                const int h = held[i], next = row[h];
+                bool bad = false;
+                constexpr int N = 16;            // asked for at a time (those behind the last are the last)
+#pragma unroll 1
+                for (int e = lane & 15; e < h; e += 16 * N) {
+                    int page[N];
+#pragma unroll
+                    for (int u = 0; u < N; ++u) page[u] = row[e + 16 * u < h ? e + 16 * u : h - 1];
+#pragma unroll
+                    for (int u = 0; u < N; ++u) bad |= !a_page(page[u]);
+                }
+                if (bad && a_page(next)) found[i] = 1;
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (at[k] >= 0) stuck[k] = found[at[k]];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) got[k] = fine[k] && !stuck[k];
     // Rows, pages that come back, those of whom; pages needed; pieces of few rows, of many, blocks written; requests of many rows.  Who has no rows or no pages left is found by
     // sums of those before it, after which there are new ones to be taken: in most steps nobody is.
     unsigned v[8], t[8];
@@ -178,7 +225,7 @@ __device__ __forceinline__ Sums build_sums(const BuildArgs &A) {
             const int b = tid * PER + k, tok0 = (int)row < A.tokens ? (int)row : A.tokens;
             if (b < A.batch) {
                 spd_plan_req &r = reqs[b];
-                *(i32x4 *)&r.pos = (i32x4){pos[k], rows_of(k), tok0, !fine[k] ? SPD_STEP_LENGTHS : !got[k] ? SPD_STEP_NO_PAGES : q[k] < 0 ? 1 : 0};
+                *(i32x4 *)&r.pos = (i32x4){pos[k], rows_of(k), tok0, !fine[k] ? SPD_STEP_LENGTHS : stuck[k] ? SPD_STEP_PAGE : !got[k] ? SPD_STEP_NO_PAGES : q[k] < 0 ? 1 : 0};
                 *(i32x4 *)&r.need0 = (i32x4){(int)need, (int)back, back_of(k), few};
                 *(i32x4 *)&r.piece0 = (i32x4){piece, pieces_of(k), write, writes_of(k)};
                 if (back_of(k)) ((spd_plan_back *)(A.plan + A.backs))[backs] = spd_plan_back{(int)back, b};
