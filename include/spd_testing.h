@@ -136,6 +136,11 @@ int spd_prefill_attention_workgroups(int32_t head_dim);
  * long K.  SPD_EINVAL: sizes that spd_q8_matmul() refuses or no rows.  Host only. */
 int spd_q8_kernel_of(int32_t rows, int32_t K, int32_t N, int64_t ld_codes);
 
+/* ---------------------------------------------------------------- cut of many rows' attention over pages
+ * The time in ns that a plan expects of `items` pieces of work per KV head, the longest of `longest` blocks, `slots` of them parts that are joined: of three
+ * cuts it takes the first that expects the least, on the host and on the device.  SPD_EINVAL: sizes that are not positive (slots: negative).  Host only. */
+int64_t spd_pages_estimate(int32_t longest, int32_t items, int32_t slots, int32_t n_kv_heads);
+
 #ifdef __cplusplus
 }
 #endif

@@ -144,6 +144,7 @@ _PROTOS = {
     "spd_pages_plan_get_info": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(spd_pages_plan_info)]),
     "spd_pages_reserve": (C.c_int, [C.c_void_p, C.POINTER(spd_pages_limits), C.c_void_p, C.c_size_t, C.POINTER(C.c_size_t),
                                     C.POINTER(C.c_size_t)]),
+    "spd_pages_estimate": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
     "spd_pages_build": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(spd_pages_step), C.c_void_p]),
     "spd_pages_write": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_int64, C.c_void_p]),

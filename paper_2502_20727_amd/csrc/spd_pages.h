@@ -98,16 +98,16 @@ SPD_HD int spd_most_small(int blocks, int sets) {
     return n < blocks / 8 ? n : blocks / 8;
 }
 // Many rows: cut so that a workgroup per compute unit has work, or one and a half, or two (halves = 2, 3, 4), whichever is estimated to end first: the time
-// in us of `items` whose longest has `longest` blocks, `slots` of them parts.  A tile of four
+// in ns of `items` whose longest has `longest` blocks, `slots` of them parts; in whole numbers, since floating-point products are rounded differently on the host
+// and on the device, and of two cuts that take as long the one would choose the first and the other the second.  A tile of four
 // blocks takes a workgroup 1.65 us by itself and 2.35 beside another; a join costs a launch and its partial results twice (66 KB each, 0.018 us).
 // us a call, cut for 256 / 384 / 512 workgroups: three windowed chunks of 333 tokens, 5 heads 23.2 / 26.3 / 26.1, without the window 38.8 / 37.2 / 35.4, the
 // same over e4m3 41.3 / 37.8 / 34.6, d 64 28.7 / 27.2 / 27.9, two of 333 behind 16000 64.3 / 62.1 / 55.7, one of 300 behind 2000, 8 heads of 8 63.3 / 49.1 /
 // 41.9.  Of 200 calls of all types and widths that the three cut differently this picks cuts that are 1 % slower than the best of them on average, 15 % at
 // most (with a part at 0.04 us: 3 % and 39 %).
-SPD_HD double spd_estimate_large(int longest, int64_t items, int64_t slots, int kv) {
-    const int64_t groups = items * kv;
-    const double tiles = (longest + 3) / 4, rounds = (double)((groups + 2 * SPD_COMPUTE_UNITS - 1) / (2 * SPD_COMPUTE_UNITS));
-    return tiles * (groups <= SPD_COMPUTE_UNITS ? 1.65 : 2.35 * rounds) + (slots ? 3.0 + 0.018 * slots * kv : 0.0);
+SPD_HD int64_t spd_estimate_large(int longest, int64_t items, int64_t slots, int kv) {
+    const int64_t groups = items * kv, tiles = (longest + 3) / 4, rounds = (groups + 2 * SPD_COMPUTE_UNITS - 1) / (2 * SPD_COMPUTE_UNITS);
+    return tiles * (groups <= SPD_COMPUTE_UNITS ? 1650 : 2350 * rounds) + (slots ? 3000 + 18 * slots * kv : 0);
 }
 // blocks of the i-th of `parts` items of a piece of `total` blocks
 SPD_HD int spd_item_first(int total, int unit, int parts, int i) {      // i * units / parts whole units (parts: some hundred at most)

@@ -362,8 +362,8 @@ __device__ __forceinline__ Sums build_sums(const BuildArgs &A) {
         }
         __syncthreads();
         const int h = lane < 3 ? lane : 0;
-        const double us = spd_estimate_large(counts[h][2], counts[h][0], counts[h][1], A.kv), us0 = __shfl(us, 0), us1 = __shfl(us, 1), us2 = __shfl(us, 2);
-        halves = us1 < us0 ? us2 < us1 ? 2 : 1 : us2 < us0 ? 2 : 0;
+        const long long ns = spd_estimate_large(counts[h][2], counts[h][0], counts[h][1], A.kv), ns0 = __shfl(ns, 0), ns1 = __shfl(ns, 1), ns2 = __shfl(ns, 2);
+        halves = ns1 < ns0 ? ns2 < ns1 ? 2 : 1 : ns2 < ns0 ? 2 : 0;
     }
     {
         const float few_inverse = cut_few ? chosen(0) : 0.f, many_inverse = n_many ? chosen(halves + 1) : 0.f;      // (few rows: uncut where there are not enough counters)

@@ -66,15 +66,15 @@ void cut(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs
 void cut_large(const std::vector<Piece> &pieces, const std::vector<spd_plan_seq> &seqs, int kv, std::vector<spd_plan_item> &items,
                std::vector<spd_plan_merge> &merges, int &slots) {
     if (pieces.empty()) return;
-    double least = 0.0;
+    int64_t least = 0;
     for (int halves = 2; halves <= 4; ++halves) {
         std::vector<spd_plan_item> i;
         std::vector<spd_plan_merge> m;
         int n = 0;
         cut(pieces, seqs, kv, SPD_COMPUTE_UNITS * halves / 2, 4, spd_most_large, i, m, n);
-        const double us = spd_estimate_large(i[0].count, (int64_t)i.size(), n, kv);
-        if (halves == 2 || us < least) {
-            least = us;
+        const int64_t ns = spd_estimate_large(i[0].count, (int64_t)i.size(), n, kv);
+        if (halves == 2 || ns < least) {
+            least = ns;
             items.swap(i);
             merges.swap(m);
             slots = n;
@@ -287,6 +287,11 @@ int spd_pages_plan_get_info(const spd_pages *pages, const void *plan_host, spd_p
     out->held = h.held;
     out->workspace_bytes = h.workspace;
     return SPD_OK;
+}
+
+int64_t spd_pages_estimate(int32_t longest, int32_t items, int32_t slots, int32_t n_kv_heads) {
+    if (longest <= 0 || items <= 0 || slots < 0 || n_kv_heads <= 0) return SPD_EINVAL;
+    return spd_estimate_large(longest, items, slots, n_kv_heads);
 }
 
 int spd_pages_reserve(const spd_pages *pages, const spd_pages_limits *limits, void *plan_host, size_t capacity, size_t *bytes, size_t *device_bytes) {

@@ -70,6 +70,24 @@ def check_lists(dev, cfg, positions, q_lens, window, sinks):
     return want
 
 
+def test_cuts_that_take_as_long_are_told_apart_by_their_order_alone():
+    """Of three cuts a plan takes the first that is expected to take the least: in whole numbers, so that host and device agree where two take the same.  (In 64-bit
+    floating point the products of such pairs are apart by a rounding, and by another one where they are fused with their sum.)"""
+    l = B.lib()
+    ties = 0
+    for t1 in range(1, 60):
+        for s1 in range(2, 257, 3):
+            for t2 in range(1, t1 + 1):
+                s2, rest = divmod(1650 * t1 + 18 * s1 - 2350 * t2, 18)
+                if rest == 0 and 2 <= s2 <= 512:
+                    ties += 1
+                    assert l.spd_pages_estimate(4 * t1, 256, s1, 1) == l.spd_pages_estimate(4 * t2 - 3, 257, s2, 1) == 1650 * t1 + 3000 + 18 * s1
+    assert ties > 1000
+    assert l.spd_pages_estimate(9, 200, 0, 3) == 3 * 2 * 2350 and l.spd_pages_estimate(1 << 22, 8704, 512, 1024) == (1 << 20) * 17408 * 2350 + 3000 + 18 * 512 * 1024
+    for bad in ((0, 1, 0, 1), (1, 0, 0, 1), (1, 1, -1, 1), (1, 1, 0, 0)):
+        assert l.spd_pages_estimate(*bad) == B.SPD_EINVAL
+
+
 def prompts(r, batch, n_long, q_len, ctx, far, far_ctx):
     """`batch` requests of which `n_long` have chunks, the others single tokens; `far` of either kind, short chunks, lie far behind the rest."""
     q_lens = [r.randint(17, 20) if b < far else r.randint(17, q_len) if b < n_long else r.choice([1, 1, 1, 0, 2]) for b in range(batch)]
