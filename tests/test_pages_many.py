@@ -114,6 +114,19 @@ def test_pieces_are_the_hosts(gpu, q, kv, batch, n_long, q_len, ctx, far, far_ct
 
 
 @gpu_test
+@pytest.mark.parametrize("kv,blocks", [(2, {2: 15, 57: 3, 368: 7}), (1, {39: 44, 379: 9, 10: 29}), (2, {11: 18, 91: 11, 571: 3}),
+                                       (2, {4: 14, 526: 3, 46: 25}), (1, {12: 30, 1284: 1, 197: 21}), (1, {43: 53, 1003: 3, 9: 39})])
+def test_cuts_that_are_expected_to_take_as_long(gpu, kv, blocks):
+    """Chunks of two tokens behind so many blocks: of the cuts for 256 and 512 workgroups (28 blocks an item, 12) each is expected to take what the other does, and the first
+    is taken on both sides."""
+    ends = [16 * n for n, times in blocks.items() for _ in range(times)]
+    cfg = config(q=16 * kv, kv=kv, d=64, page=64, n_pages=sum(-(-e // 64) for e in ends), max_ctx=max(ends))
+    want = check_lists(gpu, cfg, [e - 2 for e in ends], [2] * len(ends), 0, 0)[1]
+    longest, items, slots = max(row[8] for row in want), len(want), sum(row[10] > 1 for row in want)
+    assert longest == 28 and items * kv <= 256 and B.lib().spd_pages_estimate(longest, items, slots, kv) == B.lib().spd_pages_estimate(12, 512 // kv, slots + 250 // kv, kv)
+
+
+@gpu_test
 def test_pieces_up_to_the_limit(gpu):
     """As many pieces as plans made on the device have room for: 8192."""
     positions, q_lens = [7 * b for b in range(80)], [810 + b % 3 for b in range(80)]
