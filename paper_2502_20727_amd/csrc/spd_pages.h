@@ -49,8 +49,9 @@ constexpr int SPD_LARGE_ROWS = 128;      // ... and of the kernel for many
 constexpr int SPD_SMALL_TARGET = 256, SPD_COMPUTE_UNITS = 256;
 constexpr int SPD_LARGE_MIN_BLOCKS = 8;
 // Of the kernel for few rows over 4-bit pages two fit on a compute unit.  It is cut for them where there are pieces (times KV heads) enough that
-// half as many would be uneven: us a call, cut for 256 / 512 workgroups: 200 sequences of up to 8000 35.3 / 30.2, 24 on 8 heads 18.0 / 18.4; fewer, where
-// more parts are more to join: 48 of up to 16000 19.5 / 20.4, 8 on 5 heads 11.4 / 11.7.
+// half as many would be uneven: us a call (means of three draws of lengths), cut for 256 / 512 workgroups: 136 sequences of up to 8000 22.4 / 19.8, 200 34.4 / 26.4, 300 44.3 / 37.2, 24 on
+// 8 heads 32.3 / 26.0, 64 on 8 53.0 / 53.1; short ones gain nothing, 192 of up to 2000 12.0 / 12.4.  Of fewer pieces more parts are more to join: 48 of up to 16000 15.4 / 16.2 (though
+// 100 of up to 8000 17.5 / 16.7, 40 on 5 heads, which are more, 34.6 / 26.8).
 SPD_HD int spd_small_target(int cache_dtype, int64_t pieces) { return cache_dtype == SPD_E2M1 && pieces > SPD_SMALL_TARGET / 2 ? 2 * SPD_SMALL_TARGET : SPD_SMALL_TARGET; }
 
 // the visible blocks of rows row0 .. row0 + rows - 1 of a sequence whose first new position is `pos`

@@ -198,7 +198,7 @@ __device__ __forceinline__ Block block_at(const Pages &P, const spd_plan_seq &s,
 // Writing.  One workgroup per 16-position block and a few heads: sixteen threads per token, D / 16 of them to a row of D features, each with
 // eight of one rotary half and the eight that they turn with.  A workgroup of KV heads has keys and values side by side; one of
 // query heads keeps its angles for all of its heads.  Bound by what is read and written: four prompts of 2048 tokens, 64 + 2 x 8 heads in bf16,
-// 68 us (319 MB: 4.7 TB/s), over pages of 4 bits 58 to 62 (311 MB, 5 TB/s; the rotation in 64 bits hides behind the memory).  (Rotated queries written past the caches: 4 less, but
+// 68 us (319 MB: 4.7 TB/s), over pages of 4 bits as long (311 MB; the rotation in 64 bits hides behind the memory; 57 for the same rows over and over).  (Rotated queries written past the caches: 4 less, but
 // the attention behind it fetches them again: both together 364 -> 374.)
 // ------------------------------------------------------------------------------------------
 struct WriteArgs {

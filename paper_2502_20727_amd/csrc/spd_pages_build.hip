@@ -83,7 +83,7 @@ __device__ __forceinline__ float times_less_one(float n, float inverse) { return
 
 // The first kernel.  PER requests a thread, one after the other.  Bound by how long one thing waits for another: loads, about six
 // sums over the workgroup, barriers, and the fetching of its own instructions, which is why little of it is unrolled or divides in 64 bits.  us, one
-// request / 256 with four chunks of prompts / 2048 with 64: 4.8 / 12.0 / 22.6, both launches 11.4 / 17.6 / 31.2 (chunks tried one after the other by the whole workgroup, dividing in 64
+// request / 256 with four chunks of prompts / 2048 with 64: 4.8 / 13.8 / 25.3, both launches 11.4 / 19.5 / 34.0 (chunks tried one after the other by the whole workgroup, dividing in 64
 // bits: 32.0 / 57.1 / 119.8).
 struct Sums {
     int rows, free0, top, n_backs, sorted;      // as in the header
