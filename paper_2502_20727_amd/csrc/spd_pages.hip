@@ -374,56 +374,56 @@ __global__ void __launch_bounds__(256) k_pages_write(WriteArgs A) {
                 e[D / 64] = (char)eb;
             }
         } else {
-        if (kind == 0) rotate(a, b);
-        if constexpr (!E4M3) {       // what the 16-bit type makes of it decides whether the row is finite
+            if (kind == 0) rotate(a, b);
+            if constexpr (!E4M3) {       // what the 16-bit type makes of it decides whether the row is finite
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const int pa = Half<F16>::pack(a[i], a[i + 1]), pb = Half<F16>::pack(b[i], b[i + 1]);
-                a[i] = Half<F16>::low(pa);
-                a[i + 1] = Half<F16>::high(pa);
-                b[i] = Half<F16>::low(pb);
-                b[i + 1] = Half<F16>::high(pb);
+                for (int i = 0; i < 8; i += 2) {
+                    const int pa = Half<F16>::pack(a[i], a[i + 1]), pb = Half<F16>::pack(b[i], b[i + 1]);
+                    a[i] = Half<F16>::low(pa);
+                    a[i + 1] = Half<F16>::high(pa);
+                    b[i] = Half<F16>::low(pb);
+                    b[i + 1] = Half<F16>::high(pb);
+                }
             }
-        }
-        // largest magnitude over the threads of the row, infinity if any holds a value that is not finite
-        float amax = 0.f;
-        bool fine = true;
+            // largest magnitude over the threads of the row, infinity if any holds a value that is not finite
+            float amax = 0.f;
+            bool fine = true;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            amax = fmaxf(amax, fmaxf(fabsf(a[i]), fabsf(b[i])));
-            fine = fine && fabsf(a[i]) <= 3.402823466e38f && fabsf(b[i]) <= 3.402823466e38f;
-        }
-        if (!fine) amax = __builtin_inff();
-#pragma unroll
-        for (int d = 1; d < TPR; d <<= 1) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
-        fine = amax < __builtin_inff();
-        float scale = 1.f;
-        char *to = codes[unit] + (r * D + f0) * W;
-        if constexpr (E4M3) {
-            amax = fmaxf(amax, 0x1p-90f);
-            scale = amax / 448.f;
-            const float up = 448.f / amax;
-            i32x2 x, y;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[i] = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i] * up, a[4 * i + 1] * up, 0, false);
-                x[i] = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i + 2] * up, a[4 * i + 3] * up, x[i], true);
-                y[i] = __builtin_amdgcn_cvt_pk_fp8_f32(b[4 * i] * up, b[4 * i + 1] * up, 0, false);
-                y[i] = __builtin_amdgcn_cvt_pk_fp8_f32(b[4 * i + 2] * up, b[4 * i + 3] * up, y[i], true);
+            for (int i = 0; i < 8; ++i) {
+                amax = fmaxf(amax, fmaxf(fabsf(a[i]), fabsf(b[i])));
+                fine = fine && fabsf(a[i]) <= 3.402823466e38f && fabsf(b[i]) <= 3.402823466e38f;
             }
-            *(i32x2 *)to = fine ? x : (i32x2){0, 0};
-            *(i32x2 *)(to + D / 2) = fine ? y : (i32x2){0, 0};
-        } else {
-            i32x4 x, y;
+            if (!fine) amax = __builtin_inff();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[i] = Half<F16>::pack(a[2 * i], a[2 * i + 1]);
-                y[i] = Half<F16>::pack(b[2 * i], b[2 * i + 1]);
+            for (int d = 1; d < TPR; d <<= 1) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
+            fine = amax < __builtin_inff();
+            float scale = 1.f;
+            char *to = codes[unit] + (r * D + f0) * W;
+            if constexpr (E4M3) {
+                amax = fmaxf(amax, 0x1p-90f);
+                scale = amax / 448.f;
+                const float up = 448.f / amax;
+                i32x2 x, y;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    x[i] = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i] * up, a[4 * i + 1] * up, 0, false);
+                    x[i] = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i + 2] * up, a[4 * i + 3] * up, x[i], true);
+                    y[i] = __builtin_amdgcn_cvt_pk_fp8_f32(b[4 * i] * up, b[4 * i + 1] * up, 0, false);
+                    y[i] = __builtin_amdgcn_cvt_pk_fp8_f32(b[4 * i + 2] * up, b[4 * i + 3] * up, y[i], true);
+                }
+                *(i32x2 *)to = fine ? x : (i32x2){0, 0};
+                *(i32x2 *)(to + D / 2) = fine ? y : (i32x2){0, 0};
+            } else {
+                i32x4 x, y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = Half<F16>::pack(a[2 * i], a[2 * i + 1]);
+                    y[i] = Half<F16>::pack(b[2 * i], b[2 * i + 1]);
+                }
+                *(i32x4 *)to = fine ? x : (i32x4){0, 0, 0, 0};
+                *(i32x4 *)(to + D) = fine ? y : (i32x4){0, 0, 0, 0};
             }
-            *(i32x4 *)to = fine ? x : (i32x4){0, 0, 0, 0};
-            *(i32x4 *)(to + D) = fine ? y : (i32x4){0, 0, 0, 0};
-        }
-        if (there && f0 == 0) scales_of(B0)[(size_t)(head - head0) * (P.head_bytes / 4) + kind * P.page_size + r] = fine ? scale : __builtin_nanf("");
+            if (there && f0 == 0) scales_of(B0)[(size_t)(head - head0) * (P.head_bytes / 4) + kind * P.page_size + r] = fine ? scale : __builtin_nanf("");
         }
     }
     __syncthreads();
