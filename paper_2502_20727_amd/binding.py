@@ -921,8 +921,8 @@ class PagePlan:
 
 
 class DevicePlan:
-    """Plans of steps that spd_pages_build() makes on the device, one after the other in the same place, for steps within the limits; their scratch, cleared on
-    torch's current stream.  Takes the place of a PagePlan in spd_pages_write() and spd_pages_attention(), whose matrices have `limits.tokens` rows: those that are no
+    """Plans of steps that spd_pages_build() makes on the device, one after the other in the same place, for steps within the limits; their scratch.  Both are cleared on
+    torch's current stream, which other streams wait for before their first call.  Takes the place of a PagePlan in spd_pages_write() and spd_pages_attention(), whose matrices have `limits.tokens` rows: those that are no
     request's are neither read nor written.  A plan that is built anew while calls of the step before may still run (on other streams) needs a second object, as do
     calls that may overlap a scratch each.  The object has to live until its calls, and graphs that hold them, are over."""
 
