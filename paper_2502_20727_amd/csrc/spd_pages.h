@@ -100,7 +100,7 @@ SPD_HD int spd_most_small(int blocks, int sets) {
 }
 // Many rows: cut so that a workgroup per compute unit has work, or one and a half, or two (halves = 2, 3, 4), whichever is estimated to end first: the time
 // in ns of `items` whose longest has `longest` blocks, `slots` of them parts; in whole numbers, since floating-point products are rounded differently on the host
-// and on the device, and of two cuts that take as long the one would choose the first and the other the second.  A tile of four
+// and on the device, and of two cuts that take as long (in one of eighty such pairs) the one would choose the first and the other the second.  A tile of four
 // blocks takes a workgroup 1.65 us by itself and 2.35 beside another; a join costs a launch and its partial results twice (66 KB each, 0.018 us).
 // us a call, cut for 256 / 384 / 512 workgroups: three windowed chunks of 333 tokens, 5 heads 23.2 / 26.3 / 26.1, without the window 38.8 / 37.2 / 35.4, the
 // same over e4m3 41.3 / 37.8 / 34.6, d 64 28.7 / 27.2 / 27.9, two of 333 behind 16000 64.3 / 62.1 / 55.7, one of 300 behind 2000, 8 heads of 8 63.3 / 49.1 /
